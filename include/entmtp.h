@@ -54,6 +54,14 @@ extern "C" {
 #define ENTMTP_MASK_WORDS 8    /* uint32 words per mask row (ENTMTP_T_MAX / 32) */
 #define ENTMTP_HEAD_DIM   128  /* the head dimension the attention kernels are built for */
 #define ENTMTP_B_MAX      16   /* sequences per batched call */
+#define ENTMTP_PAGED_B_MAX 256 /* sequences per call over a page pool */
+
+/* status[b] of entmtp_page_map (and entmtp_tree_attn_paged_plan) */
+#define ENTMTP_PAGE_OK    0
+#define ENTMTP_PAGE_NONE  1    /* topo[b] outside the bank: no rows (a padded batch) */
+#define ENTMTP_PAGE_RANGE 2    /* prefix or rows do not fit (max_pages, rows_cap, a negative length) */
+#define ENTMTP_PAGE_FULL  3    /* not enough free pages */
+#define ENTMTP_PAGE_BAD   4    /* a page number outside the pool, or a prefix page missing */
 
 typedef uint16_t entmtp_bf16;
 typedef struct entmtp_bank entmtp_bank;
@@ -480,6 +488,155 @@ int32_t entmtp_kv_compact_batched_device(int32_t B, const int32_t* path, int32_t
                                          entmtp_bf16* const* v_caches, int32_t n_layers,
                                          int64_t layer_stride, int32_t Hkv, int32_t cap,
                                          int32_t d, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Serving from a page pool (§4: a tree per sequence and step; here the       */
+/* sequences of a batch share one pool of cache pages, and every choice --    */
+/* trees, prefix lengths, pages, rows -- stays in device memory).             */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * The pool of one layer is k_pool / v_pool [n_pages][Hkv][page_size][d] bf16
+ * (page_size 16, 32, 64, 128 or 256, n_pages * page_size < 2^31).  Row b of
+ * block_table [B][max_pages] (device int32) names the pages of sequence b in
+ * order: position p lies in slot table[b][p / page_size] * page_size +
+ * p % page_size of the pool; entries below zero hold no page.  A batch has up
+ * to ENTMTP_PAGED_B_MAX sequences, the bank up to 32 trees.  The order of one
+ * step is
+ *   entmtp_page_map              rows, slots and pages of the step's trees
+ *   entmtp_tree_attn_paged_plan  the attention's work list, for all layers
+ *   entmtp_tree_attn_paged       layer by layer
+ *   entmtp_verify_logits, entmtp_logit_adjust, entmtp_accept_batched_device
+ *                                (topo + 16 k, row_off + 16 k for sequences
+ *                                16 k .. 16 k + 15 of a larger batch)
+ *   entmtp_kv_compact_paged, entmtp_token_history_accept
+ * with prefix_len[b] += accept_len[b] + 1 before the next one.
+ * The current device is the one the bank and the tensors lie on.
+ */
+
+/*
+ * Rows, slots and pages of a step: sequence b verifies tree topo[b] (device
+ * int32[B]; outside the bank: an unused place of the batch, no rows) at prefix
+ * length prefix_len[b] (device int32[B]).
+ *   row_off   device int32[B + 1] out: first tree row of every sequence, the
+ *             trees' node counts summed up in order, at most rows_cap
+ *   slot_map  device int32[rows_cap] out: pool slot of every tree row (node i
+ *             of sequence b: position prefix_len[b] + i), -1 in a sequence
+ *             that is not mapped; rows behind the last sequence are left alone
+ *   status    device int32[B] out: ENTMTP_PAGE_OK, or why the sequence is not
+ *             mapped
+ *   block_table  device int32[B][max_pages] in/out: entries of the tree's
+ *             positions that are below zero are filled from the free pages;
+ *             the others, and prefixes, are left as they are
+ *   free_pages, n_free  device int32[free_cap] and int32[1], or both NULL (no
+ *             page is taken): a stack of free pages, its top at
+ *             free_pages[n_free[0] - 1] (n_free clamped to [0, free_cap]).
+ *             Sequences take theirs in order; sequence b is served when it and
+ *             those before it need at most the pages there are, else it takes
+ *             none (FULL), nor does a later one that needs any.  n_free[0] is
+ *             lowered by the pages taken.
+ * A sequence is RANGE when prefix_len[b] < 0, its last position lies past
+ * max_pages pages or its rows pass rows_cap (row_off then ends at rows_cap);
+ * BAD when an entry of the tree's positions is n_pages or more, the page that
+ * holds the prefix's last slots is missing, or a free page it would take lies
+ * outside the pool (those are dropped).  Pages are not shared by the call: two
+ * sequences may name one page for their prefixes, but a page that tree rows
+ * fall into belongs to one sequence.  A finished sequence's pages are given
+ * back by pushing them on the stack on the same stream.  Called again, the
+ * pages are there and nothing is taken.
+ * Errors (host-checked): EINVAL, ERANGE, EHIP.
+ */
+int32_t entmtp_page_map(const entmtp_bank* bank, int32_t B, const int32_t* topo,
+                        const int32_t* prefix_len, int32_t* block_table, int32_t max_pages,
+                        int32_t page_size, int32_t n_pages, const int32_t* free_pages,
+                        int32_t free_cap, int32_t* n_free, int32_t rows_cap, int32_t* row_off,
+                        int32_t* slot_map, int32_t* status, void* stream);
+
+/*
+ * entmtp_kv_compact over the pool: in every layer (layer l's pools start
+ * layer_stride elements after layer l - 1's), head and j = 0 .. accept_len[b],
+ *   pool[slot_map[row_off[b] + j]] <- pool[slot_map[row_off[b] + path[b][j]]]
+ * for keys and values, all reads before any write.  path [B][path_capacity],
+ * accept_len [B] (clamped to min(path_capacity, ENTMTP_D_MAX + 1) - 1; below
+ * zero: nothing moves), row_off [B + 1] and slot_map [rows] are device arrays
+ * of the step's entmtp_page_map and acceptance.  A row whose node does not lie
+ * in the sequence's rows, or whose slot is outside the pool, is skipped.
+ * Requirements: d % 8 == 0, 8 <= d <= 256, 16-byte aligned pools.
+ * Errors (host-checked): EINVAL, ERANGE, EHIP.
+ */
+int32_t entmtp_kv_compact_paged(int32_t B, const int32_t* path, int32_t path_capacity,
+                                const int32_t* accept_len, const int32_t* row_off,
+                                const int32_t* slot_map, int32_t rows, entmtp_bf16* k_pool,
+                                entmtp_bf16* v_pool, int32_t n_layers, int64_t layer_stride,
+                                int32_t n_pages, int32_t Hkv, int32_t page_size, int32_t d,
+                                void* stream);
+
+/*
+ * Penalties, biases and grammar masks on the logits of a batch's tree rows,
+ * and the statistics of the result (entmtp_logit_stats, at a temperature per
+ * sequence) in the same pass.  Row r = row_off[b] + i belongs to node i of
+ * tree topo[b]; its logits are the target's for the token after node i.  With
+ * c(v) = the count of v in the sequence's history plus the drafted tokens v
+ * among the nodes of i's path below the root (the root's token is in the
+ * history already), and seen(v) where c(v) > 0 or the prompt holds v:
+ *   z(v) = seen(v) ? (z(v) > 0 ? z(v) / rep : z(v) * rep) : z(v)
+ *   z(v) = (z(v) - freq * c(v)) - pres    where c(v) > 0
+ *   z(v) = z(v) + bias(v)
+ *   z(v) = -inf                           where the mask forbids v
+ * each step in fp32, rounded.
+ *   logits   [rows][V] fp32; out [rows][V] fp32, may be logits itself, or NULL
+ *            (statistics only)
+ *   params   device fp32[B][4]: rep, freq, pres, inv_temp (1, 0, 0: none; not
+ *            checked: rep and inv_temp are positive numbers)
+ *   history  device int32[B][V] (entmtp_token_history_*), or NULL: none
+ *   bias     device fp32[n_bias][V] with bias_idx int32[B], or both NULL: the
+ *            bias row of every sequence (outside [0, n_bias): none)
+ *   mask     device uint32[n_masks][mask_words] with mask_idx int32[rows], or
+ *            both NULL: bit v % 32 of word v / 32 allows token v; the mask of
+ *            every row (outside [0, n_masks): none), so that nodes may have
+ *            grammar states of their own
+ *   draft_tokens  device int32[rows] (outside [0, V): not counted)
+ *   entropy, top1p, argmax  [rows], each may be NULL.  A row whose every
+ *            logit is -inf has argmax -1, top1p 0 and entropy 0 (greedy
+ *            acceptance then ends there, with bonus -1); a NaN or +inf that no
+ *            mask hides shows as NaN in entropy and top1p.
+ *   workspace  entmtp_logit_adjust_workspace(rows, V) bytes, 16-byte aligned
+ *            (not needed when no statistics are asked for); used by this call
+ * Rows of no sequence (behind the last, or where the tree has fewer nodes) are
+ * left alone in every output.
+ * Errors (host-checked): EINVAL, ERANGE, ENOSPC, EHIP.
+ */
+size_t entmtp_logit_adjust_workspace(int32_t rows, int32_t V);
+int32_t entmtp_logit_adjust(const entmtp_bank* bank, int32_t B, const int32_t* topo,
+                            const int32_t* row_off, int32_t rows, const int32_t* draft_tokens,
+                            const float* logits, int32_t V, const float* params,
+                            const int32_t* history, const float* bias, int32_t n_bias,
+                            const int32_t* bias_idx, const uint32_t* mask, int32_t n_masks,
+                            int32_t mask_words, const int32_t* mask_idx, float* out,
+                            float* entropy, float* top1p, int32_t* argmax, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/*
+ * The token history of a batch, device int32[B][V], zero at first: bits 0-30
+ * of an entry count the token's emissions, bit 31 says that the prompt holds
+ * it.
+ * entmtp_token_history_prompt sets bit 31 for the tokens of the prompts:
+ * tokens[tok_off[b]] .. tokens[tok_off[b + 1] - 1] are sequence b's (device
+ * int32[n_tokens] and int32[B + 1], ascending).
+ * entmtp_token_history_accept counts what a step emitted: the drafted tokens
+ * of nodes path[b][1 .. accept_len[b]] (draft_tokens int32[rows], the rows of
+ * sequence b from row_off[b]) and bonus[b]; accept_len[b] < 0: nothing.
+ * Tokens outside [0, V), and nodes outside the sequence's rows, are skipped.
+ * Errors (host-checked): EINVAL, EHIP.
+ */
+int32_t entmtp_token_history_prompt(const int32_t* tokens, int32_t n_tokens,
+                                    const int32_t* tok_off, int32_t B, int32_t V,
+                                    int32_t* history, void* stream);
+int32_t entmtp_token_history_accept(int32_t B, const int32_t* row_off,
+                                    const int32_t* draft_tokens, int32_t rows,
+                                    const int32_t* path, int32_t path_capacity,
+                                    const int32_t* accept_len, const int32_t* bonus, int32_t V,
+                                    int32_t* history, void* stream);
 
 /* ------------------------------------------------------------------------ */
 /* Scheduler policy (§4 "Policy"), host only.                                 */

@@ -27,6 +27,8 @@ _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libentmtp.
 
 OK, EINVAL, ETREE, ERANGE, ENOSPC, EHIP, ETIMEDOUT = 0, -1, -2, -3, -4, -5, -6
 T_MAX, D_MAX, MASK_WORDS, HEAD_DIM, B_MAX = 256, 31, 8, 128, 16
+PAGED_B_MAX = 256
+PAGE_OK, PAGE_NONE, PAGE_RANGE, PAGE_FULL, PAGE_BAD = range(5)   # status of a mapped sequence
 
 _c_i32, _c_i64, _c_f32, _c_sz, _c_p = (ctypes.c_int32, ctypes.c_int64, ctypes.c_float,
                                        ctypes.c_size_t, ctypes.c_void_p)
@@ -97,6 +99,17 @@ _SIGNATURES = {
                                           _c_p, _c_p, _c_p, _c_p, _c_p, _c_p, _c_p, _c_p]),
     "entmtp_kv_compact": (_c_i32, [_c_p, _c_i32, _c_p, _c_i32, _c_p, _c_p, _c_i32, _c_i64, _c_i32,
                                    _c_i32, _c_i32, _c_p]),
+    "entmtp_page_map": (_c_i32, [_c_p, _c_i32, _c_p, _c_p, _c_p, _c_i32, _c_i32, _c_i32, _c_p, _c_i32,
+                                 _c_p, _c_i32, _c_p, _c_p, _c_p, _c_p]),
+    "entmtp_kv_compact_paged": (_c_i32, [_c_i32, _c_p, _c_i32, _c_p, _c_p, _c_p, _c_i32, _c_p, _c_p,
+                                         _c_i32, _c_i64, _c_i32, _c_i32, _c_i32, _c_i32, _c_p]),
+    "entmtp_logit_adjust_workspace": (_c_sz, [_c_i32, _c_i32]),
+    "entmtp_logit_adjust": (_c_i32, [_c_p, _c_i32, _c_p, _c_p, _c_i32, _c_p, _c_p, _c_i32, _c_p, _c_p,
+                                     _c_p, _c_i32, _c_p, _c_p, _c_i32, _c_i32, _c_p, _c_p, _c_p, _c_p,
+                                     _c_p, _c_p, _c_sz, _c_p]),
+    "entmtp_token_history_prompt": (_c_i32, [_c_p, _c_i32, _c_p, _c_i32, _c_i32, _c_p, _c_p]),
+    "entmtp_token_history_accept": (_c_i32, [_c_i32, _c_p, _c_p, _c_i32, _c_p, _c_i32, _c_p, _c_p, _c_i32,
+                                             _c_p, _c_p]),
     "entmtp_ladder_next": (_c_i32, [_c_i32, _c_i32, _c_f32, _c_f32, _c_f32]),
     "entmtp_ladder_next_batched": (_c_i32, [_c_i32, _c_p, _c_p, _c_i32, _c_f32, _c_f32]),
     "entmtp_step_workspace": (_c_sz, [_c_p, ctypes.POINTER(StepConfig)]),
@@ -728,6 +741,156 @@ def kv_compact(path, accept_len, prefix_len: int, k_cache, v_cache, stream=None)
         stride = Hkv * cap * d
     _check(lib.entmtp_kv_compact(_p(path), path.numel(), _p(accept_len), prefix_len, _p(k_cache),
                                  _p(v_cache), n_layers, stride, Hkv, cap, d, _stream(stream)))
+
+
+# ------------------------------------------------- serving from a page pool --
+
+def _here(*tensors):
+    """The tensors (None: skipped) lie on the current device: the stream the
+    call launches on belongs to it."""
+    dev = _torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != dev:
+            raise ValueError(f"a tensor lies on {t.device}, the current device is cuda:{dev}")
+
+
+def _paged_batch(topo, row_off=None):
+    _dev(topo, "topo", _torch.int32)
+    B = topo.numel()
+    _need(topo.dim() == 1 and 1 <= B <= PAGED_B_MAX, f"topo is [B] with 1 <= B <= {PAGED_B_MAX}")
+    if row_off is not None:
+        _dev(row_off, "row_off", _torch.int32, (B + 1,))
+    return B
+
+
+def page_map(bank: Bank, topo, prefix_len, block_table, page_size: int, n_pages: int, row_off,
+             slot_map, status, free_pages=None, n_free=None, stream=None) -> None:
+    """Rows, slots and pages of a step's trees: topo, prefix_len, status int32
+    [B], block_table int32 [B, max_pages] (entries below zero that the trees
+    need are taken from free_pages[:n_free], from its end), row_off int32
+    [B + 1] and slot_map int32 [rows_cap] out."""
+    i32 = _torch.int32
+    B = _paged_batch(topo, row_off)
+    _dev(prefix_len, "prefix_len", i32, (B,))
+    _dev(status, "status", i32, (B,))
+    _dev(block_table, "block_table", i32)
+    _need(block_table.dim() == 2 and block_table.shape[0] == B, "block_table is [B, max_pages]")
+    _dev(slot_map, "slot_map", i32, min_numel=1)
+    _need((free_pages is None) == (n_free is None), "free_pages and n_free go together")
+    if free_pages is not None:
+        _dev(free_pages, "free_pages", i32, min_numel=1)
+        _dev(n_free, "n_free", i32, (1,))
+    _here(topo, prefix_len, block_table, row_off, slot_map, status, free_pages, n_free)
+    _check(lib.entmtp_page_map(bank.handle, B, _p(topo), _p(prefix_len), _p(block_table),
+                               block_table.shape[1], page_size, n_pages, _p(free_pages),
+                               0 if free_pages is None else free_pages.numel(), _p(n_free),
+                               slot_map.numel(), _p(row_off), _p(slot_map), _p(status),
+                               _stream(stream)))
+
+
+def kv_compact_paged(path, accept_len, row_off, slot_map, k_pool, v_pool, stream=None) -> None:
+    """path [B, path_capacity] and accept_len [B]; row_off and slot_map of the
+    step's page_map; pools [n_pages, Hkv, page_size, d] (one layer) or
+    [n_layers, n_pages, Hkv, page_size, d] (bf16)."""
+    i32 = _torch.int32
+    _dev(path, "path", i32)
+    _need(path.dim() == 2 and 1 <= path.shape[0] <= PAGED_B_MAX, "path is [B, path_capacity]")
+    B = path.shape[0]
+    _dev(accept_len, "accept_len", i32, (B,))
+    _dev(row_off, "row_off", i32, (B + 1,))
+    _dev(slot_map, "slot_map", i32, min_numel=1)
+    _need(k_pool.dim() in (4, 5), "pools are 4-D or 5-D")
+    _dev(k_pool, "k_pool", _torch.bfloat16)
+    _dev(v_pool, "v_pool", _torch.bfloat16, k_pool.shape)
+    _here(path, accept_len, row_off, slot_map, k_pool, v_pool)
+    n_layers = 1 if k_pool.dim() == 4 else k_pool.shape[0]
+    n_pages, Hkv, page, d = k_pool.shape[-4:]
+    _check(lib.entmtp_kv_compact_paged(B, _p(path), path.shape[1], _p(accept_len), _p(row_off),
+                                       _p(slot_map), slot_map.numel(), _p(k_pool), _p(v_pool),
+                                       n_layers, n_pages * Hkv * page * d, n_pages, Hkv, page, d,
+                                       _stream(stream)))
+
+
+def logit_adjust_workspace(rows: int, V: int) -> int:
+    return int(lib.entmtp_logit_adjust_workspace(rows, V))
+
+
+def logit_adjust(bank: Bank, topo, row_off, draft_tokens, logits, params, out, entropy, top1p, argmax,
+                 workspace, history=None, bias=None, bias_idx=None, mask=None, mask_idx=None,
+                 stream=None) -> None:
+    """logits fp32 [rows, V] of the batch's tree rows -> out (logits itself, or
+    None) and their statistics (each may be None); params fp32 [B, 4] (rep,
+    freq, pres, inv_temp), history int32 [B, V], bias fp32 [n, V] with
+    bias_idx int32 [B], mask int32 [m, words] (bits) with mask_idx int32
+    [rows]."""
+    i32, f32 = _torch.int32, _torch.float32
+    B = _paged_batch(topo, row_off)
+    _need(logits.dim() == 2, "logits are [rows, V]")
+    rows, V = logits.shape
+    _dev(logits, "logits", f32)
+    _dev(draft_tokens, "draft_tokens", i32, (rows,))
+    _dev(params, "params", f32, (B, 4))
+    if out is not None:
+        _dev(out, "out", f32, (rows, V))
+    for name, t, dt in (("entropy", entropy, f32), ("top1p", top1p, f32), ("argmax", argmax, i32)):
+        if t is not None:
+            _dev(t, name, dt, (rows,))
+    if history is not None:
+        _dev(history, "history", i32, (B, V))
+    _need((bias is None) == (bias_idx is None), "bias and bias_idx go together")
+    if bias is not None:
+        _dev(bias, "bias", f32)
+        _need(bias.dim() == 2 and bias.shape[1] == V, "bias is [n, V]")
+        _dev(bias_idx, "bias_idx", i32, (B,))
+    _need((mask is None) == (mask_idx is None), "mask and mask_idx go together")
+    if mask is not None:
+        _dev(mask, "mask", i32)
+        _need(mask.dim() == 2, "mask is [m, words]")
+        _dev(mask_idx, "mask_idx", i32, (rows,))
+    if workspace is not None:
+        _need(workspace.is_cuda and workspace.is_contiguous(), "workspace must be a contiguous GPU tensor")
+    _here(topo, row_off, draft_tokens, logits, params, out, entropy, top1p, argmax, workspace, history,
+          bias, bias_idx, mask, mask_idx)
+    _check(lib.entmtp_logit_adjust(bank.handle, B, _p(topo), _p(row_off), rows, _p(draft_tokens),
+                                   _p(logits), V, _p(params), _p(history), _p(bias),
+                                   0 if bias is None else bias.shape[0], _p(bias_idx), _p(mask),
+                                   0 if mask is None else mask.shape[0],
+                                   0 if mask is None else mask.shape[1], _p(mask_idx), _p(out),
+                                   _p(entropy), _p(top1p), _p(argmax), _p(workspace),
+                                   0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                   _stream(stream)))
+
+
+def token_history_prompt(tokens, tok_off, history, stream=None) -> None:
+    """history int32 [B, V]: marks the prompts' tokens, sequence b's at
+    tokens[tok_off[b]:tok_off[b + 1]] (int32)."""
+    _dev(history, "history", _torch.int32)
+    _need(history.dim() == 2 and 1 <= history.shape[0] <= PAGED_B_MAX, "history is [B, V]")
+    B, V = history.shape
+    _dev(tokens, "tokens", _torch.int32)
+    _dev(tok_off, "tok_off", _torch.int32, (B + 1,))
+    _here(tokens, tok_off, history)
+    _check(lib.entmtp_token_history_prompt(_p(tokens), tokens.numel(), _p(tok_off), B, V, _p(history),
+                                           _stream(stream)))
+
+
+def token_history_accept(row_off, draft_tokens, path, accept_len, bonus, history, stream=None) -> None:
+    """history int32 [B, V]: counts the accepted drafts (path [B,
+    path_capacity], accept_len [B]) and the bonus tokens [B] of a step."""
+    i32 = _torch.int32
+    _dev(history, "history", i32)
+    _need(history.dim() == 2 and 1 <= history.shape[0] <= PAGED_B_MAX, "history is [B, V]")
+    B, V = history.shape
+    _dev(row_off, "row_off", i32, (B + 1,))
+    _dev(draft_tokens, "draft_tokens", i32, min_numel=1)
+    _dev(path, "path", i32)
+    _need(path.dim() == 2 and path.shape[0] == B, "path is [B, path_capacity]")
+    _dev(accept_len, "accept_len", i32, (B,))
+    _dev(bonus, "bonus", i32, (B,))
+    _here(row_off, draft_tokens, path, accept_len, bonus, history)
+    _check(lib.entmtp_token_history_accept(B, _p(row_off), _p(draft_tokens), draft_tokens.numel(),
+                                           _p(path), path.shape[1], _p(accept_len), _p(bonus), V,
+                                           _p(history), _stream(stream)))
 
 
 def ladder_next(rung: int, n_rungs: int, s: float, tau_on: float, tau_off: float) -> int:

@@ -9,6 +9,7 @@
 // registers before writing any.  The accept length is read on the device, so
 // the host does not wait for the verification result.
 #include "common.hpp"
+#include "paged.hpp"
 
 namespace entmtp {
 namespace {
@@ -106,6 +107,65 @@ int32_t launch_compact(const CompactArgs& a, int B, hipStream_t s) {
   const size_t lds = static_cast<size_t>(2) * rows * (a.d / 8) * sizeof(u32x4);
   hipLaunchKernelGGL(kv_compact_kernel, dim3(B * a.n_layers * a.Hkv), dim3(kCompactThreads), lds, s, a);
   return launch_status("kv_compact launch");
+}
+
+// The same over a page pool: row j of sequence b's path moves from the slot of
+// its node's tree row to the slot of tree row j (position L + j is tree row
+// j's slot, whatever node lies there).  A thread owns one 16-byte column (K or
+// V, head, chunk) of a (sequence, layer) and holds its rows of the path in
+// registers, so every read precedes every write without LDS or a barrier, and
+// all its loads are in flight at once: latency bound, a few rows a sequence.
+// ROWS: path entries held (registers), at least the path capacity's.
+struct CompactPagedArgs {
+  uint16_t* kp;   // [n_layers] pools [n_pages][Hkv][P][d], layer_stride apart
+  uint16_t* vp;
+  const int* path;
+  const int* accept_len;
+  const int* row_off;    // [B + 1]
+  const int* slot_map;   // [rows]
+  long long layer_stride;
+  int path_cap, rows, Hkv, d, shift, n_slots, groups;   // groups: workgroups per (sequence, layer)
+};
+
+template <int ROWS>
+__global__ __launch_bounds__(kCompactThreads) void kv_compact_paged_kernel(CompactPagedArgs p) {
+  __shared__ int s_src[ROWS], s_dst[ROWS];
+  const int b = blockIdx.y, layer = blockIdx.x / p.groups;
+  const int a = min(p.accept_len[b], min(p.path_cap, ROWS) - 1);
+  if (a < 0) return;   // not verified (uniform)
+  const int t = threadIdx.x;
+  if (t < ROWS) {
+    int src = -1, dst = -1;
+    if (t <= a) {
+      const int r0 = p.row_off[b], n = min(p.row_off[b + 1], p.rows) - r0;
+      const int node = p.path[static_cast<size_t>(b) * p.path_cap + t];
+      if (r0 >= 0 && node >= 0 && node < n && t < n && node != t) {
+        src = p.slot_map[r0 + node];
+        dst = p.slot_map[r0 + t];
+        if (src >= p.n_slots || dst < 0 || dst >= p.n_slots) src = -1;
+      }
+    }
+    s_src[t] = src;
+    s_dst[t] = dst;
+  }
+  __syncthreads();
+  const int chunks = p.d >> 3, per_tensor = p.Hkv * chunks;
+  const int col = (blockIdx.x % p.groups) * kCompactThreads + t;
+  if (col >= 2 * per_tensor) return;
+  uint16_t* const pool = (col >= per_tensor ? p.vp : p.kp) + layer * p.layer_stride;
+  const int g = (col % per_tensor) / chunks, ch = col % chunks;
+  auto at = [&](int slot) {
+    const size_t page = slot >> p.shift;
+    return reinterpret_cast<u32x4*>(
+        pool + (((page * p.Hkv + g) << p.shift) + (slot & ((1 << p.shift) - 1))) * p.d + ch * 8);
+  };
+  u32x4 val[ROWS];
+#pragma unroll
+  for (int j = 0; j < ROWS; ++j)
+    if (s_src[j] >= 0) val[j] = *at(s_src[j]);
+#pragma unroll
+  for (int j = 0; j < ROWS; ++j)
+    if (s_src[j] >= 0) *at(s_dst[j]) = val[j];
 }
 
 }  // namespace
@@ -248,4 +308,51 @@ extern "C" int32_t entmtp_kv_compact_batched_device(int32_t B, const int32_t* pa
   a.cap = cap;
   a.d = d;
   return launch_compact(a, B, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int32_t entmtp_kv_compact_paged(int32_t B, const int32_t* path, int32_t path_capacity,
+                                           const int32_t* accept_len, const int32_t* row_off,
+                                           const int32_t* slot_map, int32_t rows, entmtp_bf16* k_pool,
+                                           entmtp_bf16* v_pool, int32_t n_layers, int64_t layer_stride,
+                                           int32_t n_pages, int32_t Hkv, int32_t page_size, int32_t d,
+                                           void* stream) {
+  clear_error();
+  ENTMTP_CHECK_ARG(paged_batch(B), ENTMTP_EINVAL, "B = %d outside [1, %d]", B, ENTMTP_PAGED_B_MAX);
+  ENTMTP_CHECK_ARG(path && accept_len && row_off && slot_map && k_pool && v_pool, ENTMTP_EINVAL,
+                   "path, accept_len, row_off, slot_map and pools must be non-NULL");
+  ENTMTP_CHECK_ARG(path_capacity >= 1 && rows >= 1, ENTMTP_EINVAL, "path_capacity = %d, rows = %d must be >= 1",
+                   path_capacity, rows);
+  if (int32_t rc = check_pool(n_pages, page_size)) return rc;
+  ENTMTP_CHECK_ARG(n_layers >= 1 && Hkv >= 1, ENTMTP_EINVAL, "bad sizes (n_layers %d, Hkv %d)", n_layers, Hkv);
+  ENTMTP_CHECK_ARG(d >= 8 && d % 8 == 0 && d <= 256, ENTMTP_EINVAL, "d = %d must be a multiple of 8 in [8, 256]", d);
+  ENTMTP_CHECK_ARG(Hkv <= 65536, ENTMTP_ERANGE, "Hkv = %d too large", Hkv);
+  ENTMTP_CHECK_ARG(n_layers == 1 || layer_stride >= static_cast<int64_t>(n_pages) * Hkv * page_size * d,
+                   ENTMTP_EINVAL, "layer_stride %lld smaller than one layer", static_cast<long long>(layer_stride));
+  ENTMTP_CHECK_ARG(layer_stride % 8 == 0, ENTMTP_EINVAL, "layer_stride must keep 16-byte alignment");
+  ENTMTP_CHECK_ARG(aligned16(k_pool) && aligned16(v_pool), ENTMTP_EINVAL, "pools must be 16-byte aligned");
+  CompactPagedArgs a{};
+  a.kp = k_pool;
+  a.vp = v_pool;
+  a.path = path;
+  a.accept_len = accept_len;
+  a.row_off = row_off;
+  a.slot_map = slot_map;
+  a.layer_stride = static_cast<long long>(layer_stride);
+  a.path_cap = path_capacity;
+  a.rows = rows;
+  a.Hkv = Hkv;
+  a.d = d;
+  a.shift = page_shift(page_size);
+  a.n_slots = n_pages * page_size;
+  a.groups = (2 * Hkv * (d / 8) + kCompactThreads - 1) / kCompactThreads;
+  const int64_t blocks = static_cast<int64_t>(n_layers) * a.groups;
+  ENTMTP_CHECK_ARG(blocks <= INT32_MAX, ENTMTP_ERANGE, "%d layers of %d heads: too many", n_layers, Hkv);
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(blocks), B), dim3(kCompactThreads), 0,
+                       static_cast<hipStream_t>(stream), a);
+  };
+  // (72 registers a thread for paths of up to 16 rows, 136 for longer ones: more workgroups share a CU)
+  static_assert(ENTMTP_D_MAX + 1 <= 32, "the longest path");
+  path_capacity <= 16 ? go(kv_compact_paged_kernel<16>) : go(kv_compact_paged_kernel<32>);
+  return launch_status("kv_compact_paged launch");
 }

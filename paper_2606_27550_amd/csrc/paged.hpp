@@ -1,0 +1,89 @@
+// What the operators over a shared page pool have in common: the bank's trees
+// as kernel arguments, and where a row of a batch lies.
+//
+// A batch's choices (tree indices, prefix lengths, row offsets) are device
+// arrays that the host never reads, so every kernel checks the entries it
+// uses: a tree index against the bank, a row against the sequence's range and
+// the rows there are, a pool slot against the pool.
+#pragma once
+
+#include "common.hpp"
+
+namespace entmtp {
+
+constexpr int kPagedSeqs = ENTMTP_PAGED_B_MAX;
+constexpr int kPagedTrees = 32;   // bank trees a call can name (kernel arguments)
+
+struct PagedTree {
+  int T, D;
+  int off_mask, off_depth, off_path;   // bytes into the bank's arena
+};
+
+struct TreeTable {
+  const uint8_t* arena;
+  int n;
+  PagedTree t[kPagedTrees];
+};
+
+// The bank's trees as kernel arguments; an error status where the bank is not
+// on the current device or holds more trees than a call can name.
+inline int32_t tree_table(const entmtp_bank* bank, TreeTable* out) {
+  if (int32_t rc = check_device_bank(bank, 0)) return rc;
+  int dev = -1;
+  if (int32_t rc = hip_status(hipGetDevice(&dev), "hipGetDevice")) return rc;
+  ENTMTP_CHECK_ARG(dev == bank->device, ENTMTP_EINVAL, "the bank lies on device %d, the current one is %d",
+                   bank->device, dev);
+  ENTMTP_CHECK_ARG(static_cast<int>(bank->desc.size()) <= kPagedTrees, ENTMTP_ERANGE,
+                   "a device-planned batch names at most %d bank trees (bank has %zu)", kPagedTrees,
+                   bank->desc.size());
+  out->arena = bank->arena;
+  out->n = static_cast<int>(bank->desc.size());
+  for (int k = 0; k < out->n; ++k) {
+    const TopoDesc& td = bank->desc[k];
+    ENTMTP_CHECK_ARG(td.off_path <= INT32_MAX, ENTMTP_ERANGE, "bank arena offsets past 2 GiB");
+    out->t[k] = PagedTree{td.T, td.D, static_cast<int>(td.off_mask), static_cast<int>(td.off_depth),
+                          static_cast<int>(td.off_path)};
+  }
+  return ENTMTP_OK;
+}
+
+inline bool paged_batch(int B) { return B >= 1 && B <= kPagedSeqs; }
+
+// log2 of a page size (16, 32, 64, 128 or 256 slots), or -1.
+inline int page_shift(int page_size) {
+  for (int s = 4; s <= 8; ++s)
+    if (page_size == 1 << s) return s;
+  return -1;
+}
+
+// Checks of a pool that every entry point makes.
+inline int32_t check_pool(int32_t n_pages, int32_t page_size) {
+  ENTMTP_CHECK_ARG(page_shift(page_size) >= 0, ENTMTP_EINVAL,
+                   "page_size = %d must be 16, 32, 64, 128 or 256", page_size);
+  ENTMTP_CHECK_ARG(n_pages >= 1, ENTMTP_EINVAL, "n_pages = %d < 1", n_pages);
+  ENTMTP_CHECK_ARG(static_cast<int64_t>(n_pages) * page_size <= INT32_MAX, ENTMTP_ERANGE,
+                   "%d pages of %d slots: slots are 32-bit numbers", n_pages, page_size);
+  return ENTMTP_OK;
+}
+
+// The sequence whose rows [row_off[b], row_off[b + 1]) hold row r: the number
+// of sequences that end at or before it (B: none).  Called by whole
+// wavefronts with r uniform; the loads go out together.
+__device__ __forceinline__ int seq_of_row(const int* __restrict__ row_off, int B, int r) {
+  const int lane = threadIdx.x & 63;
+  int end[kPagedSeqs / 64];
+#pragma unroll
+  for (int k = 0; k < kPagedSeqs / 64; ++k) {
+    if (64 * k >= B) break;   // (uniform)
+    end[k] = row_off[min(64 * k + lane, B - 1) + 1];
+  }
+  int b = 0;
+#pragma unroll
+  for (int k = 0; k < kPagedSeqs / 64; ++k) {
+    if (64 * k >= B) break;
+    b += __popcll(__ballot(64 * k + lane < B && end[k] <= r));
+  }
+  return b;
+}
+
+}  // namespace entmtp
