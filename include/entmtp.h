@@ -553,6 +553,69 @@ int32_t entmtp_page_map(const entmtp_bank* bank, int32_t B, const int32_t* topo,
                         int32_t* slot_map, int32_t* status, void* stream);
 
 /*
+ * The attention's work list of a step: made once from entmtp_page_map's
+ * outputs (status other than ENTMTP_PAGE_OK: no work) and read by the calls of
+ * all layers with the same sizes and window (layers with another window take a
+ * list of their own).  It weighs how the batch's key blocks are split over the
+ * chip and checks the pages the attention will read: bad[b] (device int32[B],
+ * may be NULL) is 1 where one lies outside [0, n_pages), which leaves the
+ * sequence without work, else 0.  With a window, entries of pages that lie
+ * wholly before the root's are not read (they may be given back).
+ *   window  0: none; else node i sees positions above pos(i) - window
+ *   plan    device buffer of entmtp_tree_attn_paged_plan_bytes() bytes (0: bad
+ *           sizes), 64-byte aligned, for this bank, current device and sizes
+ * Requirements: Hq % Hkv == 0, Hq / Hkv <= 32, Hkv <= 256; sequences' rows do
+ * not overlap.
+ * Errors (host-checked): EINVAL, ERANGE, ENOSPC (plan), EHIP.
+ */
+size_t entmtp_tree_attn_paged_plan_bytes(const entmtp_bank* bank, int32_t B, int32_t rows_cap,
+                                         int32_t Hq, int32_t Hkv, int32_t max_pages,
+                                         int32_t page_size);
+int32_t entmtp_tree_attn_paged_plan(const entmtp_bank* bank, int32_t B, const int32_t* topo,
+                                    const int32_t* prefix_len, const int32_t* row_off,
+                                    const int32_t* status, const int32_t* block_table,
+                                    int32_t max_pages, int32_t page_size, int32_t n_pages,
+                                    int32_t rows_cap, int32_t Hq, int32_t Hkv, int32_t window,
+                                    int32_t* bad, void* plan, size_t plan_bytes, void* stream);
+
+/*
+ * One attention layer over the pool for the batch of a plan: as
+ * entmtp_tree_attn for every sequence (rotation, mask, fp32 softmax), its
+ * prefix read through the block table and its tree's keys and values written
+ * to the slots of slot_map (entries outside the pool: not written).  q, out
+ * [rows_cap][Hq][d], k_tree, v_tree [rows_cap][Hkv][d] bf16 hold the tree rows
+ * where row_off put them; rows of no sequence, or of one without work, are
+ * left alone in out.
+ *   softcap  0: none; else scores s = scale * (q . k) become
+ *            softcap * tanh(s / softcap)
+ *   slopes   NULL: none; else device fp32[Hq]: slopes[h] * (pos_q - pos_k) is
+ *            taken off the score (after the cap)
+ *   window   as the plan's: keys with pos_q - pos_k >= window are not seen
+ *   workspace  device scratch of entmtp_tree_attn_paged_workspace() bytes (0
+ *            for bad sizes, and where no prefix can be long enough to be
+ *            split: NULL is allowed then); calls that share one must be
+ *            ordered
+ * A plan made for other sizes, another window or another bank leaves every
+ * output alone.  Values of tree nodes that are not finite reach the rows that
+ * see them (all dims become NaN) and no others; keys and values before the
+ * root's window are not read.
+ * Requirements: d == ENTMTP_HEAD_DIM; otherwise as the plan.
+ * Errors (host-checked): EINVAL, ERANGE, ENOSPC, EHIP.
+ */
+size_t entmtp_tree_attn_paged_workspace(const entmtp_bank* bank, int32_t B, int32_t rows_cap,
+                                        int32_t Hq, int32_t Hkv, int32_t d, int32_t max_pages,
+                                        int32_t page_size);
+int32_t entmtp_tree_attn_paged(const entmtp_bank* bank, int32_t B, const void* plan,
+                               size_t plan_bytes, const entmtp_bf16* q, const entmtp_bf16* k_tree,
+                               const entmtp_bf16* v_tree, entmtp_bf16* k_pool,
+                               entmtp_bf16* v_pool, int32_t n_pages, int32_t page_size,
+                               const int32_t* block_table, int32_t max_pages,
+                               const int32_t* slot_map, int32_t rows_cap, int32_t Hq, int32_t Hkv,
+                               int32_t d, float scale, float rope_theta, float softcap,
+                               int32_t window, const float* slopes, entmtp_bf16* out,
+                               void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * entmtp_kv_compact over the pool: in every layer (layer l's pools start
  * layer_stride elements after layer l - 1's), head and j = 0 .. accept_len[b],
  *   pool[slot_map[row_off[b] + j]] <- pool[slot_map[row_off[b] + path[b][j]]]

@@ -131,8 +131,15 @@ def row_stats(z, inv_temp):
 
 def tree_attention_paged(q, kt, vt, k_pool, v_pool, table, L, parent, scale, theta, softcap=0.0,
                          window=0, slopes=None):
-    """One sequence: out [T, Hq, d] in 64 bits and the tree's rotated keys as
-    bf16 bits [T, Hkv, d].  q, kt, vt, pools: bf16 bits; table: its pages."""
+    """One sequence: out [T, Hq, d] in 64 bits, the tree's rotated keys as bf16
+    bits [T, Hkv, d], and how far roundings to bf16 can move out.  q, kt, vt,
+    pools: bf16 bits; table: its pages.
+
+    The last: a rounding to bf16 is off by at most u = 2^-8 of the value.  The
+    weights and a split's partial are rounded (u sum p |v| each), so is out (u
+    |out|); a rotated query's rounding moves a score by at most d_k = u scale
+    sum |q_c k_c| (a score cap bends by at most one), all of a row's by at most
+    D, and with it out by at most (e^(2 D) - 1) sum p |v - out|."""
     T, Hq, d = q.shape
     Hkv, page = k_pool.shape[1:3]
     depth = orc.depths(parent)
@@ -145,7 +152,8 @@ def tree_attention_paged(q, kt, vt, k_pool, v_pool, table, L, parent, scale, the
         qf = np.stack([orc.rope(qf[i], L + depth[i], theta) for i in range(T)])
         kf = orc.round_to_bf16(np.stack([orc.rope(kf[i], L + depth[i], theta) for i in range(T)]))
     pos = np.concatenate([np.arange(L), L + np.array(depth)])
-    out = np.zeros((T, Hq, d))
+    out, off = np.zeros((T, Hq, d)), np.zeros((T, Hq, d))
+    u = 2.0 ** -8
     for i in range(T):
         see = np.concatenate([np.ones(L, bool), np.isin(np.arange(T), orc.ancestors_or_self(parent, i))])
         dist = L + depth[i] - pos
@@ -153,11 +161,15 @@ def tree_attention_paged(q, kt, vt, k_pool, v_pool, table, L, parent, scale, the
             see &= dist < window
         for h in range(Hq):
             g = h // (Hq // Hkv)
-            z = np.concatenate([k_pre[g], kf[:, g]])[see] @ qf[i, h] * scale
+            k, v = np.concatenate([k_pre[g], kf[:, g]])[see], np.concatenate([v_pre[g], vf[:, g]])[see]
+            z = k @ qf[i, h] * scale
             if softcap:
                 z = softcap * np.tanh(z / softcap)
             if slopes is not None:
                 z = z - float(slopes[h]) * dist[see]
             p = np.exp(z - z.max())
-            out[i, h] = (p / p.sum()) @ np.concatenate([v_pre[g], vf[:, g]])[see]
-    return out, orc.f64_to_bf16_bits(kf) if theta > 0 else kt
+            p /= p.sum()
+            out[i, h] = p @ v
+            D = u * scale * float((np.abs(k) @ np.abs(qf[i, h])).max()) if theta > 0 else 0.0
+            off[i, h] = 2 * u * (p @ np.abs(v)) + u * np.abs(out[i, h]) + (math.exp(2 * D) - 1) * (p @ np.abs(v - out[i, h]))
+    return out, orc.f64_to_bf16_bits(kf) if theta > 0 else kt, off

@@ -101,6 +101,13 @@ _SIGNATURES = {
                                    _c_i32, _c_i32, _c_p]),
     "entmtp_page_map": (_c_i32, [_c_p, _c_i32, _c_p, _c_p, _c_p, _c_i32, _c_i32, _c_i32, _c_p, _c_i32,
                                  _c_p, _c_i32, _c_p, _c_p, _c_p, _c_p]),
+    "entmtp_tree_attn_paged_plan_bytes": (_c_sz, [_c_p] + [_c_i32] * 6),
+    "entmtp_tree_attn_paged_plan": (_c_i32, [_c_p, _c_i32] + [_c_p] * 5 + [_c_i32] * 7 + [_c_p, _c_p, _c_sz,
+                                                                                         _c_p]),
+    "entmtp_tree_attn_paged_workspace": (_c_sz, [_c_p] + [_c_i32] * 7),
+    "entmtp_tree_attn_paged": (_c_i32, [_c_p, _c_i32, _c_p, _c_sz] + [_c_p] * 5 +
+                               [_c_i32, _c_i32, _c_p, _c_i32, _c_p] + [_c_i32] * 4 +
+                               [_c_f32, _c_f32, _c_f32, _c_i32, _c_p, _c_p, _c_p, _c_sz, _c_p]),
     "entmtp_kv_compact_paged": (_c_i32, [_c_i32, _c_p, _c_i32, _c_p, _c_p, _c_p, _c_i32, _c_p, _c_p,
                                          _c_i32, _c_i64, _c_i32, _c_i32, _c_i32, _c_i32, _c_p]),
     "entmtp_logit_adjust_workspace": (_c_sz, [_c_i32, _c_i32]),
@@ -788,6 +795,79 @@ def page_map(bank: Bank, topo, prefix_len, block_table, page_size: int, n_pages:
                                _stream(stream)))
 
 
+def tree_attn_paged_plan_bytes(bank: Bank, B: int, rows_cap: int, Hq: int, Hkv: int, max_pages: int,
+                               page_size: int) -> int:
+    return int(lib.entmtp_tree_attn_paged_plan_bytes(bank.handle, B, rows_cap, Hq, Hkv, max_pages,
+                                                     page_size))
+
+
+def _scratch(t, name):
+    _need(isinstance(t, _torch.Tensor) and t.is_cuda and t.is_contiguous(),
+          f"{name} must be a contiguous GPU tensor")
+    return t.numel() * t.element_size()
+
+
+def tree_attn_paged_plan(bank: Bank, topo, prefix_len, row_off, status, block_table, page_size: int,
+                         n_pages: int, rows_cap: int, Hq: int, Hkv: int, plan, window: int = 0,
+                         bad=None, stream=None) -> None:
+    """The attention's work list of a step, for all layers with this window:
+    row_off and status from page_map, plan a buffer of
+    tree_attn_paged_plan_bytes; bad int32 [B] (or None): sequences with a
+    prefix page outside the pool."""
+    i32 = _torch.int32
+    B = _paged_batch(topo, row_off)
+    _dev(prefix_len, "prefix_len", i32, (B,))
+    _dev(status, "status", i32, (B,))
+    _dev(block_table, "block_table", i32)
+    _need(block_table.dim() == 2 and block_table.shape[0] == B, "block_table is [B, max_pages]")
+    if bad is not None:
+        _dev(bad, "bad", i32, (B,))
+    size = _scratch(plan, "plan")
+    _here(topo, prefix_len, row_off, status, block_table, bad, plan)
+    _check(lib.entmtp_tree_attn_paged_plan(bank.handle, B, _p(topo), _p(prefix_len), _p(row_off),
+                                           _p(status), _p(block_table), block_table.shape[1], page_size,
+                                           n_pages, rows_cap, Hq, Hkv, window, _p(bad), _p(plan), size,
+                                           _stream(stream)))
+
+
+def tree_attn_paged_workspace(bank: Bank, B: int, rows_cap: int, Hq: int, Hkv: int, d: int,
+                              max_pages: int, page_size: int) -> int:
+    return int(lib.entmtp_tree_attn_paged_workspace(bank.handle, B, rows_cap, Hq, Hkv, d, max_pages,
+                                                    page_size))
+
+
+def tree_attn_paged(bank: Bank, plan, q, k_tree, v_tree, k_pool, v_pool, block_table, slot_map,
+                    scale: float, rope_theta: float, out, workspace, softcap: float = 0.0,
+                    window: int = 0, slopes=None, stream=None) -> None:
+    """q, out [rows_cap, Hq, d], k_tree, v_tree [rows_cap, Hkv, d], pools
+    [n_pages, Hkv, page_size, d] (bf16), block_table int32 [B, max_pages],
+    slot_map int32 [rows_cap]; plan of the same sizes and window; slopes fp32
+    [Hq] or None."""
+    bf = _torch.bfloat16
+    _need(q.dim() == 3 and k_pool.dim() == 4 and block_table.dim() == 2,
+          "q is 3-D, pools are 4-D, block_table is 2-D")
+    rows, Hq, d = q.shape
+    n_pages, Hkv, page, _ = k_pool.shape
+    B, max_pages = block_table.shape
+    _dev(q, "q", bf)
+    _dev(k_tree, "k_tree", bf, (rows, Hkv, d))
+    _dev(v_tree, "v_tree", bf, (rows, Hkv, d))
+    _dev(k_pool, "k_pool", bf, (n_pages, Hkv, page, d))
+    _dev(v_pool, "v_pool", bf, (n_pages, Hkv, page, d))
+    _dev(out, "out", bf, (rows, Hq, d))
+    _dev(block_table, "block_table", _torch.int32)
+    _dev(slot_map, "slot_map", _torch.int32, (rows,))
+    if slopes is not None:
+        _dev(slopes, "slopes", _torch.float32, (Hq,))
+    size = _scratch(plan, "plan")
+    ws_size = 0 if workspace is None else _scratch(workspace, "workspace")
+    _here(plan, q, k_tree, v_tree, k_pool, v_pool, block_table, slot_map, out, workspace, slopes)
+    _check(lib.entmtp_tree_attn_paged(bank.handle, B, _p(plan), size, _p(q), _p(k_tree), _p(v_tree),
+                                      _p(k_pool), _p(v_pool), n_pages, page, _p(block_table), max_pages,
+                                      _p(slot_map), rows, Hq, Hkv, d, scale, rope_theta, softcap, window,
+                                      _p(slopes), _p(out), _p(workspace), ws_size, _stream(stream)))
+
+
 def kv_compact_paged(path, accept_len, row_off, slot_map, k_pool, v_pool, stream=None) -> None:
     """path [B, path_capacity] and accept_len [B]; row_off and slot_map of the
     step's page_map; pools [n_pages, Hkv, page_size, d] (one layer) or
@@ -847,8 +927,7 @@ def logit_adjust(bank: Bank, topo, row_off, draft_tokens, logits, params, out, e
         _dev(mask, "mask", i32)
         _need(mask.dim() == 2, "mask is [m, words]")
         _dev(mask_idx, "mask_idx", i32, (rows,))
-    if workspace is not None:
-        _need(workspace.is_cuda and workspace.is_contiguous(), "workspace must be a contiguous GPU tensor")
+    ws_size = 0 if workspace is None else _scratch(workspace, "workspace")
     _here(topo, row_off, draft_tokens, logits, params, out, entropy, top1p, argmax, workspace, history,
           bias, bias_idx, mask, mask_idx)
     _check(lib.entmtp_logit_adjust(bank.handle, B, _p(topo), _p(row_off), rows, _p(draft_tokens),
@@ -857,8 +936,7 @@ def logit_adjust(bank: Bank, topo, row_off, draft_tokens, logits, params, out, e
                                    0 if mask is None else mask.shape[0],
                                    0 if mask is None else mask.shape[1], _p(mask_idx), _p(out),
                                    _p(entropy), _p(top1p), _p(argmax), _p(workspace),
-                                   0 if workspace is None else workspace.numel() * workspace.element_size(),
-                                   _stream(stream)))
+                                   ws_size, _stream(stream)))
 
 
 def token_history_prompt(tokens, tok_off, history, stream=None) -> None:

@@ -159,8 +159,7 @@ extern "C" int32_t entmtp_page_map(const entmtp_bank* bank, int32_t B, const int
   ENTMTP_CHECK_ARG(free_pages == nullptr || free_cap >= 1, ENTMTP_EINVAL, "free_cap = %d < 1", free_cap);
   ENTMTP_CHECK_ARG(rows_cap >= 1, ENTMTP_EINVAL, "rows_cap = %d < 1", rows_cap);
   if (int32_t rc = check_pool(n_pages, page_size)) return rc;
-  ENTMTP_CHECK_ARG(max_pages >= 1 && static_cast<int64_t>(max_pages) * page_size <= INT32_MAX, ENTMTP_ERANGE,
-                   "max_pages = %d of %d slots: positions are 32-bit numbers", max_pages, page_size);
+  if (int32_t rc = check_pages(max_pages, page_size)) return rc;
   MapArgs a{};
   if (int32_t rc = tree_table(bank, &a.trees)) return rc;
   a.topo = topo;

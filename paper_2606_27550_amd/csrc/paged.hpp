@@ -66,6 +66,14 @@ inline int32_t check_pool(int32_t n_pages, int32_t page_size) {
   return ENTMTP_OK;
 }
 
+// Positions of a sequence of max_pages pages: 32-bit numbers, with room for a
+// tree and a tile past the last one.
+inline int32_t check_pages(int32_t max_pages, int32_t page_size) {
+  ENTMTP_CHECK_ARG(max_pages >= 1 && static_cast<int64_t>(max_pages) * page_size <= INT32_MAX - 1024, ENTMTP_ERANGE,
+                   "max_pages = %d of %d slots: positions are 32-bit numbers", max_pages, page_size);
+  return ENTMTP_OK;
+}
+
 // The sequence whose rows [row_off[b], row_off[b + 1]) hold row r: the number
 // of sequences that end at or before it (B: none).  Called by whole
 // wavefronts with r uniform; the loads go out together.

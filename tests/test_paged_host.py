@@ -129,3 +129,43 @@ def test_statuses_match_the_header():
         assert int(re.search(rf"#define ENTMTP_PAGE_{name}\s+(\d+)", text)[1]) == getattr(api, "PAGE_" + name)
     assert int(re.search(r"#define ENTMTP_PAGED_B_MAX (\d+)", text)[1]) == api.PAGED_B_MAX
     assert ctypes.sizeof(ctypes.c_void_p) == 8
+
+
+PLAN = dict(bank=None, B=2, topo=P, prefix_len=P, row_off=P, status=P, table=P, max_pages=8, page=16, n_pages=4,
+            rows_cap=9, Hq=8, Hkv=2, window=0, bad=None, plan=P, plan_bytes=1 << 30, stream=None)
+ATTN = dict(bank=None, B=2, plan=P, plan_bytes=1 << 30, q=P, kt=P, vt=P, kp=P, vp=P, n_pages=4, page=16, table=P,
+            max_pages=8, slots=P, rows_cap=9, Hq=8, Hkv=2, d=128, scale=0.1, theta=1e4, softcap=0.0, window=0,
+            slopes=None, out=P, ws=P, ws_bytes=1 << 30, stream=None)
+BATCH = [(dict(B=0), api.EINVAL), (dict(B=257), api.EINVAL), (dict(rows_cap=0), api.EINVAL), (dict(Hq=0), api.EINVAL),
+         (dict(Hkv=0), api.EINVAL), (dict(Hq=9), api.ERANGE), (dict(Hq=66, Hkv=2), api.ERANGE),
+         (dict(Hq=257, Hkv=257), api.ERANGE), (dict(page=8), api.EINVAL), (dict(n_pages=0), api.EINVAL),
+         (dict(n_pages=1 << 27), api.ERANGE), (dict(max_pages=0), api.ERANGE),
+         (dict(max_pages=(1 << 27) - 1), api.ERANGE), (dict(window=-1), api.EINVAL), (dict(plan=None), api.EINVAL),
+         (dict(plan=P + 16), api.EINVAL), (dict(table=None), api.EINVAL), (dict(), api.EINVAL)]
+
+
+@pytest.mark.parametrize("change,code", BATCH + [(dict([(k, None)]), api.EINVAL) for k in
+                                                 ("topo", "prefix_len", "row_off", "status")])
+def test_plan_refusals(bank, change, code):
+    refused(call("entmtp_tree_attn_paged_plan", PLAN, **{"bank": bank.handle, **change}), code)
+
+
+@pytest.mark.parametrize("change,code", BATCH + [(dict([(k, v)]), api.EINVAL) for v in (None, ODD) for k in
+                                                 ("q", "kt", "vt", "kp", "vp", "out")] + [
+    (dict(slots=None), api.EINVAL), (dict(ws=ODD), api.EINVAL), (dict(d=64), api.EINVAL), (dict(scale=0.0), api.EINVAL),
+    (dict(scale=float("nan")), api.EINVAL), (dict(scale=float("inf")), api.EINVAL), (dict(theta=-1.0), api.EINVAL),
+    (dict(theta=float("inf")), api.EINVAL), (dict(softcap=-1.0), api.EINVAL), (dict(softcap=float("nan")), api.EINVAL),
+    (dict(softcap=float("inf")), api.EINVAL), (dict(softcap=1e-42, scale=1.0), api.EINVAL)])
+def test_paged_attention_refusals(bank, change, code):
+    refused(call("entmtp_tree_attn_paged", ATTN, **{"bank": bank.handle, **change}), code)
+
+
+def test_paged_sizes(bank):
+    size = lambda **c: (api.tree_attn_paged_plan_bytes(bank, *{**dict(B=2, rows=9, Hq=8, Hkv=2, mp=8, page=16), **c}.values()),  # noqa: E731
+                        api.tree_attn_paged_workspace(bank, *{**dict(B=2, rows=9, Hq=8, Hkv=2, d=128, mp=8, page=16), **c}.values()))
+    plan, ws = size()
+    assert plan > 0 and ws == 0                       # 128 positions: never split
+    assert size(mp=64)[1] > 0
+    for bad in (dict(B=0), dict(B=257), dict(rows=0), dict(Hq=7), dict(Hkv=0), dict(mp=0), dict(page=17), dict(mp=1 << 27)):
+        assert size(**bad) == (0, 0)
+    assert api.tree_attn_paged_workspace(bank, 2, 9, 8, 2, 64, 64, 16) == 0
