@@ -22,9 +22,14 @@
 // entry of the slice, so an entry's count is one addition.  Every wavefront
 // writes its own statistics partial (no barrier in the row loop) and a second
 // kernel merges a row's partials, a wavefront per row.
-// HBM bound: 8 bytes an entry and row.
+// HBM bound, 8 bytes an entry and row, once the arithmetic fits beside it: 1024
+// rows of 128256 with everything asked for take 207 us, 5.1 TB/s (a large copy
+// reaches 5.2).  The plain form of the same took 255: divisions, reductions by
+// LDS permutes, the argmax's index kept entry by entry, stores through the
+// caches.  26 rows of 32000 take 9.8 us, both kernels' latency.
 #include <cfloat>
 #include <climits>
+#include <type_traits>
 
 #include "paged.hpp"
 #include "stats.hpp"
@@ -37,6 +42,10 @@ constexpr int kAdjWaves = kAdjThreads / 64;
 constexpr int kEntries = 16;                           // entries per thread and row
 constexpr int kSlice = kEntries * kAdjThreads;         // 4096
 constexpr int kRows = 4;                               // rows a workgroup takes at most
+constexpr int kUnits = kEntries / 4;                   // a thread's units of four entries
+
+
+typedef float f32x4v __attribute__((ext_vector_type(4)));
 
 struct AdjustArgs {
   TreeTable trees;
@@ -76,51 +85,91 @@ __device__ __forceinline__ RowOf row_of(const AdjustArgs& p, int r) {
   return q;
 }
 
-// VEC: V is a multiple of four (16-byte units); entry e of a thread is then
-// e % 4 of unit e / 4, else a unit of its own.
-template <bool VEC>
+// f over the wavefront's 64 lanes, in every lane: within rows of 16 by DPP, then
+// the rows and the halves (through LDS permutes a row's reductions are a chain
+// of 24 round trips).
+template <typename T, typename F>
+__device__ __forceinline__ T wave_all(T v, F f) {
+  auto dpp = [&](auto ctrl) {
+    return __builtin_bit_cast(T, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), decltype(ctrl)::value, 0xf, 0xf, true));
+  };
+  v = f(v, dpp(std::integral_constant<int, 0xB1>{}));    // lane ^ 1
+  v = f(v, dpp(std::integral_constant<int, 0x4E>{}));    // lane ^ 2
+  v = f(v, dpp(std::integral_constant<int, 0x141>{}));   // mirrored halves of a row
+  v = f(v, dpp(std::integral_constant<int, 0x140>{}));   // mirrored rows
+  uint32_t u = __builtin_bit_cast(uint32_t, v);
+  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  v = f(__builtin_bit_cast(T, static_cast<uint32_t>(a[0])), __builtin_bit_cast(T, static_cast<uint32_t>(a[1])));
+  u = __builtin_bit_cast(uint32_t, v);
+  const auto c = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return f(__builtin_bit_cast(T, static_cast<uint32_t>(c[0])), __builtin_bit_cast(T, static_cast<uint32_t>(c[1])));
+}
+__device__ __forceinline__ float wave_max(float v) {
+  return wave_all(v, [](float a, float b) { return fmaxf(a, b); });
+}
+__device__ __forceinline__ float wave_sum(float v) {
+  return wave_all(v, [](float a, float b) { return a + b; });
+}
+__device__ __forceinline__ int wave_min(int v) {
+  return wave_all(v, [](int a, int b) { return a < b ? a : b; });
+}
+
+// A thread's units of four entries are 16-byte aligned in the logits.  WHOLE: V
+// is a multiple of four, so units start at multiples of four in every row.
+// Else row r starts (r V) % 4 entries past a 16-byte boundary: a workgroup then
+// takes every fourth row, which start alike, and its slices start that many
+// entries early.  (Rows as they come, by 16-byte accesses at any address, took
+// 305 us for 1024 rows of 128255 where rows of 128256 took 214.)
+template <bool WHOLE>
 __global__ __launch_bounds__(kAdjThreads) void logit_adjust_kernel(AdjustArgs p) {
-  constexpr int E = VEC ? 4 : 1, U = kEntries / E;
   __shared__ uint32_t s_said[kRows][kSlice / 4];   // a byte per entry: drafted tokens on the row's path
   __shared__ int s_row[kRows][4];                  // RowOf
+  constexpr int kStep = WHOLE ? 1 : 4;             // from row to row
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int V = p.V;
-  const int r0 = static_cast<int>(blockIdx.x / p.slices) * p.group;
-  const int slice = blockIdx.x % p.slices;
-  const int v0 = slice * kSlice;
-  const int n = min(p.group, p.rows - r0);
-  auto entry = [&](int u) { return v0 + (u * kAdjThreads + tid) * E; };
-  auto load = [&](float (&x)[kEntries], const float* row) {
+  const int part = static_cast<int>(blockIdx.x / p.slices), slice = blockIdx.x % p.slices;
+  const int r0 = part / kStep * (kStep * p.group) + part % kStep;
+  const int n = min(p.group, (p.rows - r0 + kStep - 1) / kStep);
+  if (n <= 0) return;
+  const int v0 = slice * kSlice - (WHOLE ? 0 : static_cast<int>(static_cast<unsigned>(r0) * static_cast<unsigned>(V) & 3u));
+  auto row_at = [&](int i) { return r0 + kStep * i; };
+  auto entry = [&](int u) { return v0 + (u * kAdjThreads + tid) * 4; };
+  auto in_row = [&](int v) { return v < V && (WHOLE || v >= 0); };
+  // the thread's entries of a row, zeros outside it
+  auto load = [&](auto& x, const auto* row, auto aligned) {
+    typedef std::remove_reference_t<decltype(x[0])> T;
+    typedef T T4 __attribute__((ext_vector_type(4), aligned(decltype(aligned)::value)));
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
+    for (int u = 0; u < kUnits; ++u) {
       const int v = entry(u);
-      if constexpr (VEC) {
-        float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (v < V) t = *reinterpret_cast<const float4*>(row + v);
-        x[4 * u] = t.x;
-        x[4 * u + 1] = t.y;
-        x[4 * u + 2] = t.z;
-        x[4 * u + 3] = t.w;
-      } else {
-        x[u] = v < V ? row[v] : 0.f;
+      T4 t = {0, 0, 0, 0};
+      if (v <= V - 4 && (WHOLE || v >= 0)) {
+        t = *reinterpret_cast<const T4*>(row + v);
+      } else if constexpr (!WHOLE) {   // the row's first or last unit
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (in_row(v + e)) t[e] = row[v + e];
       }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[4 * u + e] = t[e];
     }
   };
+  constexpr std::integral_constant<int, 16> kAligned{};
+  constexpr std::integral_constant<int, WHOLE ? 16 : 4> kAny{};   // history and bias rows start elsewhere
   auto row_ptr = [&](const float* m, int r) { return m + static_cast<size_t>(r) * V; };
 
   float x[kEntries], nx[kEntries];
-  load(x, row_ptr(p.z, r0));
+  load(x, row_ptr(p.z, r0), kAligned);
   for (int i = tid; i < n * (kSlice / 4); i += kAdjThreads) s_said[0][i] = 0u;
-  if (wave < n) {   // a wavefront per row finds its sequence
-    const RowOf q = row_of(p, r0 + wave);
+  for (int i = wave; i < n; i += kAdjWaves) {   // a wavefront finds a row's sequence
+    const RowOf q = row_of(p, row_at(i));
     if (lane == 0) {
-      s_row[wave][0] = q.b;
-      s_row[wave][1] = q.node;
-      s_row[wave][2] = q.row0;
-      s_row[wave][3] = q.tree;
+      s_row[i][0] = q.b;
+      s_row[i][1] = q.node;
+      s_row[i][2] = q.row0;
+      s_row[i][3] = q.tree;
     }
   }
-  static_assert(kAdjWaves >= kRows, "a wavefront per row");
   __syncthreads();
   if (tid < 32 * n) {   // 32 threads per row: the path's nodes below the root
     const int i = tid >> 5, j = (tid & 31) + 1;
@@ -130,8 +179,8 @@ __global__ __launch_bounds__(kAdjThreads) void logit_adjust_kernel(AdjustArgs p)
       if (j <= t.D) {
         const int node = reinterpret_cast<const int*>(p.trees.arena + t.off_path)[s_row[i][1] * (t.D + 1) + j];
         if (node >= 0 && s_row[i][2] + node < p.rows) {   // (-1 past the node's depth)
-          const int rel = p.tok[s_row[i][2] + node] - v0;
-          if (rel >= 0 && rel < kSlice) atomicAdd(&s_said[i][rel >> 2], 1u << (8 * (rel & 3)));
+          const int tok = p.tok[s_row[i][2] + node], rel = tok - v0;
+          if (tok >= 0 && rel >= 0 && rel < kSlice) atomicAdd(&s_said[i][rel >> 2], 1u << (8 * (rel & 3)));
         }
       }
     }
@@ -143,122 +192,132 @@ __global__ __launch_bounds__(kAdjThreads) void logit_adjust_kernel(AdjustArgs p)
   float bias[kEntries];
   int b_held = -1;
   float4 par = make_float4(1.f, 0.f, 0.f, 1.f);
+  float rrep = 1.f;
   bool biased = false, counts = false;
-  for (int i = 0; i < n; ++i) {
-    const int r = r0 + i;
-    if (i + 1 < n) load(nx, row_ptr(p.z, r + 1));
+  auto work = [&](float (&x)[kEntries], int i) {
+    const int r = row_at(i);
     const int b = __builtin_amdgcn_readfirstlane(s_row[i][0]);
-    if (b < p.B) {
-      if (b != b_held) {
-        b_held = b;
-        par = p.params[b];
-        counts = par.x != 1.f || par.y != 0.f || par.z != 0.f;
-        const int bi = p.bias ? p.bias_idx[b] : -1;
-        biased = bi >= 0 && bi < p.n_bias;
-        const int* h = p.history + static_cast<size_t>(b) * V;
-        const float* bs = p.bias + static_cast<size_t>(biased ? bi : 0) * V;
+    if (b >= p.B) return;
+    if (b != b_held) {
+      b_held = b;
+      par = p.params[b];
+      rrep = 1.f / par.x;
+      counts = par.x != 1.f || par.y != 0.f || par.z != 0.f;
+      const int bi = p.bias ? p.bias_idx[b] : -1;
+      biased = bi >= 0 && bi < p.n_bias;
+      const int* h = p.history + static_cast<size_t>(b) * V;
+      const float* bs = p.bias + static_cast<size_t>(biased ? bi : 0) * V;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int v = entry(u);
-          if constexpr (VEC) {
-            int4 t = make_int4(0, 0, 0, 0);
-            float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (counts && p.history && v < V) t = *reinterpret_cast<const int4*>(h + v);
-            if (biased && v < V) f = *reinterpret_cast<const float4*>(bs + v);
-            hist[4 * u] = t.x;
-            hist[4 * u + 1] = t.y;
-            hist[4 * u + 2] = t.z;
-            hist[4 * u + 3] = t.w;
-            bias[4 * u] = f.x;
-            bias[4 * u + 1] = f.y;
-            bias[4 * u + 2] = f.z;
-            bias[4 * u + 3] = f.w;
-          } else {
-            hist[u] = counts && p.history && v < V ? h[v] : 0;
-            bias[u] = biased && v < V ? bs[v] : 0.f;
-          }
-        }
+      for (int e = 0; e < kEntries; ++e) {
+        hist[e] = 0;
+        bias[e] = 0.f;
       }
-      const int mi = p.mask ? p.mask_idx[r] : -1;
-      const bool masked = mi >= 0 && mi < p.n_masks;
-      const uint32_t* mw = p.mask + static_cast<size_t>(masked ? mi : 0) * p.words;
-      uint32_t allow[U];   // the unit's bits, lowest first
+      if (counts && p.history) load(hist, h, kAny);
+      if (biased) load(bias, bs, kAny);
+    }
+    const int mi = p.mask ? p.mask_idx[r] : -1;
+    const bool masked = mi >= 0 && mi < p.n_masks;
+    uint32_t allow[kUnits];   // the unit's bits, lowest first
+    if (masked) {
+      const uint32_t* mw = p.mask + static_cast<size_t>(mi) * p.words;
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int v = entry(u);
-        allow[u] = ~0u;
-        if (masked && v < V) allow[u] = mw[v >> 5] >> (v & 31);
-      }
-      {
-#pragma clang fp contract(off)
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int at = (u * kAdjThreads + tid) * E;
-          uint32_t said = s_said[i][at >> 2];
-          if constexpr (!VEC) said = (said >> (8 * (at & 3))) & 0xffu;
-#pragma unroll
-          for (int e = 0; e < E; ++e) {
-            float& z = x[E * u + e];
-            const int h = hist[E * u + e];
-            const int more = VEC ? (said >> (8 * e)) & 0xff : said;
-            if (counts && (h | more) != 0) {
-              z = z > 0.f ? z / par.x : z * par.x;
-              const int c = (h & INT_MAX) + more;
-              if (c > 0) z = (z - par.y * static_cast<float>(c)) - par.z;
-            }
-            if (biased) z = z + bias[E * u + e];
-            if (!((allow[u] >> e) & 1u) || entry(u) >= V) z = -INFINITY;
-          }
+      for (int u = 0; u < kUnits; ++u) {
+        const int v = entry(u), last = (V - 1) >> 5;
+        if constexpr (WHOLE) {
+          allow[u] = mw[min(v >> 5, last)] >> (v & 31);
+        } else {   // (a unit can straddle two words)
+          const uint64_t lo = mw[max(0, min(v >> 5, last))], hi = mw[max(0, min((v >> 5) + 1, last))];
+          allow[u] = static_cast<uint32_t>((hi << 32 | lo) >> (v & 31));
         }
-      }
-      if (p.out) {
-        float* o = p.out + static_cast<size_t>(r) * V;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int v = entry(u);
-          if (v < V) {
-            if constexpr (VEC)
-              *reinterpret_cast<float4*>(o + v) = make_float4(x[4 * u], x[4 * u + 1], x[4 * u + 2], x[4 * u + 3]);
-            else
-              o[v] = x[u];
-          }
-        }
-      }
-      if (p.part) {
-        float best = -INFINITY;
-        int idx = INT_MAX;
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-          for (int e = 0; e < E; ++e)   // (in index order within a thread)
-            if (x[E * u + e] > best) {
-              best = x[E * u + e];
-              idx = entry(u) + e;
-            }
-#pragma unroll
-        for (int off = 32; off >= 1; off >>= 1)
-          take_max(best, idx, __shfl_xor(best, off, 64), __shfl_xor(idx, off, 64));
-        // (a NaN is no maximum, but shows in Z)
-        const float m = best == -INFINITY ? 0.f : best;
-        float Z = 0.f, S = 0.f;
-#pragma unroll
-        for (int e = 0; e < kEntries; ++e) {
-          const float t = (x[e] - m) * par.w;
-          const float f = __expf(t);
-          Z += f;
-          if (f > 0.f) S = fmaf(t, f, S);   // keeps (-inf) * 0 out of the sum
-        }
-#pragma unroll
-        for (int off = 32; off >= 1; off >>= 1) {
-          Z += __shfl_xor(Z, off, 64);
-          S += __shfl_xor(S, off, 64);
-        }
-        if (lane == 0)
-          p.part[(static_cast<size_t>(r) * p.slices + slice) * kAdjWaves + wave] = StatPart{best, Z, S, idx};
       }
     }
+    {
+#pragma clang fp contract(off)
+      if (counts) {
 #pragma unroll
-    for (int e = 0; e < kEntries; ++e) x[e] = nx[e];
+        for (int u = 0; u < kUnits; ++u) {
+          const uint32_t said = s_said[i][u * kAdjThreads + tid];
+          uint32_t any = said;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) any |= static_cast<uint32_t>(hist[4 * u + e]);
+          if (any == 0u) continue;   // (most tokens never were)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int h = hist[4 * u + e], more = (said >> (8 * e)) & 0xff;
+            float z = x[4 * u + e];
+            // z / rep: the reciprocal's product and a Newton step of it, which
+            // round as the division does (no step where one of them is infinite)
+            const float q = z * rrep, step = fmaf(fmaf(-q, par.x, z), rrep, q);
+            z = z > 0.f ? (fabsf(step) < INFINITY ? step : q) : z * par.x;
+            const int c = (h & INT_MAX) + more;
+            if (c > 0) z = (z - par.y * static_cast<float>(c)) - par.z;
+            if ((h | more) != 0) x[4 * u + e] = z;
+          }
+        }
+      }
+      if (biased) {
+#pragma unroll
+        for (int e = 0; e < kEntries; ++e) x[e] = x[e] + bias[e];
+      }
+      if (masked) {
+#pragma unroll
+        for (int e = 0; e < kEntries; ++e)
+          if (!((allow[e / 4] >> (e % 4)) & 1u)) x[e] = -INFINITY;
+      }
+#pragma unroll
+      for (int e = 0; e < kEntries; ++e)
+        if (!in_row(entry(e / 4) + (WHOLE ? 0 : e % 4))) x[e] = -INFINITY;
+    }
+    if (p.out) {
+      float* o = p.out + static_cast<size_t>(r) * V;
+#pragma unroll
+      for (int u = 0; u < kUnits; ++u) {
+        const int v = entry(u);
+        if (v <= V - 4 && (WHOLE || v >= 0)) {
+          // (written past the caches: nothing of this kernel reads it again)
+          __builtin_nontemporal_store(f32x4v{x[4 * u], x[4 * u + 1], x[4 * u + 2], x[4 * u + 3]},
+                                      reinterpret_cast<f32x4v*>(o + v));
+        } else if constexpr (!WHOLE) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (in_row(v + e)) o[v + e] = x[4 * u + e];
+        }
+      }
+    }
+    if (p.part) {
+      float mine = x[0];
+#pragma unroll
+      for (int e = 1; e < kEntries; ++e) mine = fmaxf(mine, x[e]);   // (a NaN is no maximum, but shows in Z)
+      const float best = wave_max(mine);
+      int idx = INT_MAX;
+      if (mine == best && best > -INFINITY) {
+#pragma unroll
+        for (int e = kEntries - 1; e >= 0; --e)   // (a thread's entries rise with e)
+          if (x[e] == best) idx = entry(e / 4) + e % 4;
+      }
+      idx = wave_min(idx);
+      // (the difference of the raw logits first: exact or nearly, 0 for the
+      // largest; base 2 from there on)
+      const float m = best > -INFINITY ? best : 0.f, it2 = par.w * 1.44269504088896341f;
+      float Z = 0.f, S = 0.f;
+#pragma unroll
+      for (int e = 0; e < kEntries; ++e) {
+        const float t = (x[e] - m) * it2;
+        const float f = __builtin_amdgcn_exp2f(t);
+        Z += f;
+        S = fmaf(fmaxf(t, -256.f), f, S);   // (2^-256 is 0: keeps (-inf) * 0 out of the sum)
+      }
+      Z = wave_sum(Z);
+      S = wave_sum(S) * 0.693147180559945309f;
+      if (lane == 0)
+        p.part[(static_cast<size_t>(r) * p.slices + slice) * kAdjWaves + wave] = StatPart{best, Z, S, idx};
+    }
+  };
+  for (int i = 0; i < n; i += 2) {   // (two rows a round: their registers take turns)
+    if (i + 1 < n) load(nx, row_ptr(p.z, row_at(i + 1)), kAligned);
+    work(x, i);
+    if (i + 2 < n) load(x, row_ptr(p.z, row_at(i + 2)), kAligned);
+    if (i + 1 < n) work(nx, i + 1);
   }
 }
 
@@ -356,7 +415,8 @@ __global__ __launch_bounds__(64) void history_accept_kernel(const int* __restric
   if (t >= 0 && t < V) atomicAdd(history + static_cast<size_t>(b) * V + t, 1);
 }
 
-int adjust_slices(int V) { return (V + kSlice - 1) / kSlice; }
+// (a row may start up to three entries into its first slice)
+int adjust_slices(int V) { return (V + ((V & 3) ? 3 : 0) + kSlice - 1) / kSlice; }
 
 }  // namespace
 }  // namespace entmtp
@@ -381,7 +441,7 @@ extern "C" int32_t entmtp_logit_adjust(const entmtp_bank* bank, int32_t B, const
   ENTMTP_CHECK_ARG(topo && row_off && draft_tokens && logits && params, ENTMTP_EINVAL,
                    "topo, row_off, draft_tokens, logits and params must be non-NULL device arrays");
   ENTMTP_CHECK_ARG(rows >= 1 && V >= 1, ENTMTP_EINVAL, "rows = %d, V = %d must be >= 1", rows, V);
-  ENTMTP_CHECK_ARG(V <= INT32_MAX - kSlice, ENTMTP_ERANGE, "V = %d too large", V);
+  ENTMTP_CHECK_ARG(V <= INT32_MAX - 2 * kSlice, ENTMTP_ERANGE, "V = %d too large", V);
   ENTMTP_CHECK_ARG((bias == nullptr) == (bias_idx == nullptr) && (!bias || n_bias >= 1), ENTMTP_EINVAL,
                    "bias (n_bias = %d rows) and bias_idx go together", n_bias);
   ENTMTP_CHECK_ARG((mask == nullptr) == (mask_idx == nullptr) && (!mask || n_masks >= 1), ENTMTP_EINVAL,
@@ -421,8 +481,14 @@ extern "C" int32_t entmtp_logit_adjust(const entmtp_bank* bank, int32_t B, const
   a.n_masks = n_masks;
   a.words = mask_words;
   a.slices = adjust_slices(V);
-  a.group = static_cast<long long>(rows) * a.slices >= 8192 ? kRows : 1;
-  const long long blocks = static_cast<long long>((rows + a.group - 1) / a.group) * a.slices;
+  // Rows a workgroup takes: as many as leave two rounds of the workgroups that
+  // are resident (four a CU, by registers), so that few rows fill the chip and
+  // many share their start.  128 rows of 128256: one row each 38.6 us, two 35.0;
+  // 1024 rows: four 207, eight 215; 26 rows of 128256: one 14.7.
+  const long long fill = static_cast<long long>(rows) * a.slices / (8 * device_cus());
+  a.group = static_cast<int>(fill < 1 ? 1 : (fill > kRows ? kRows : fill));
+  const int step = (V & 3) ? 4 : 1;   // rows a workgroup's rows lie apart
+  const long long blocks = static_cast<long long>((rows + step * a.group - 1) / (step * a.group)) * step * a.slices;
   ENTMTP_CHECK_ARG(blocks <= INT32_MAX, ENTMTP_ERANGE, "%d rows of %d entries: too many", rows, V);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   auto go = [&](auto kernel) {

@@ -47,6 +47,19 @@ inline int32_t tree_table(const entmtp_bank* bank, TreeTable* out) {
   return ENTMTP_OK;
 }
 
+// Compute units of the current device.
+inline int device_cus() {
+  static int cus[64] = {0};
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 256;
+  if (cus[dev] == 0) {
+    int n = 0;
+    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0) n = 256;
+    cus[dev] = n;
+  }
+  return cus[dev];
+}
+
 inline bool paged_batch(int B) { return B >= 1 && B <= kPagedSeqs; }
 
 // log2 of a page size (16, 32, 64, 128 or 256 slots), or -1.

@@ -846,18 +846,6 @@ __global__ __launch_bounds__(64 * kMergeWaves) void paged_merge_kernel(PagedArgs
 
 size_t up256(size_t x) { return (x + 255) & ~size_t(255); }
 
-int paged_cus() {
-  static int cus[64] = {0};
-  int dev = 0;
-  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 256;
-  if (cus[dev] == 0) {
-    int n = 0;
-    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0) n = 256;
-    cus[dev] = n;
-  }
-  return cus[dev];
-}
-
 // What a batch of these sizes can need at most, wherever its rows lie apart
 // from each other.  A sequence has ceil(G T / 128) query groups, so the groups
 // number at most rows G / 128 + B, the streams (KV heads x groups) Hkv times
@@ -873,7 +861,7 @@ struct PagedShape {
 
 PagedShape paged_shape(const entmtp_bank* bank, int B, int rows_cap, int Hq, int Hkv, long long cap) {
   PagedShape sh;
-  const int G = Hq / Hkv, slots = paged_cus() * kWgPerCu;
+  const int G = Hq / Hkv, slots = device_cus() * kWgPerCu;
   int T_max = 0;
   for (const TopoDesc& td : bank->desc) T_max = std::max(T_max, td.T);
   const long long rows = std::min<long long>(rows_cap, static_cast<long long>(B) * T_max);
@@ -966,7 +954,7 @@ extern "C" int32_t entmtp_tree_attn_paged_plan(const entmtp_bank* bank, int32_t 
   a.max_pages = max_pages;
   a.rows_cap = rows_cap;
   a.window = window;
-  a.slots = paged_cus() * kWgPerCu;
+  a.slots = device_cus() * kWgPerCu;
   a.items_cap = sh.items;
   a.two = sh.two;
   hipLaunchKernelGGL(paged_plan_kernel, dim3(B), dim3(kPlanThreads), 0, static_cast<hipStream_t>(stream), a);
