@@ -755,9 +755,9 @@ def kv_compact(path, accept_len, prefix_len: int, k_cache, v_cache, stream=None)
 def _here(*tensors):
     """The tensors (None: skipped) lie on the current device: the stream the
     call launches on belongs to it."""
-    dev = _torch.cuda.current_device()
+    dev = _torch._C._cuda_getDevice()
     for t in tensors:
-        if t is not None and t.device.index != dev:
+        if t is not None and t.get_device() != dev:
             raise ValueError(f"a tensor lies on {t.device}, the current device is cuda:{dev}")
 
 

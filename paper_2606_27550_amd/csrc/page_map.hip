@@ -14,14 +14,15 @@
 // among them.  Row offsets are the running sum of the node counts.
 //
 // One workgroup: two scans over at most 256 sequences (a thread each), then a
-// thread per tree row.  It is bound by its memory round trips (entries, table,
-// free list, table again: about 1 us each) and made once for all layers.
+// thread per tree row.  It is bound by its memory round trips (entries, trees,
+// table, free list), so each of them asks for all it needs at once.
 #include "paged.hpp"
 
 namespace entmtp {
 namespace {
 
 constexpr int kMapThreads = 1024;
+constexpr int kEntries = ENTMTP_T_MAX / 16 + 1;   // pages of 16 slots that a tree's positions fall into
 static_assert(kPagedSeqs == 256, "four wavefronts hold a thread per sequence");
 
 struct MapArgs {
@@ -54,6 +55,7 @@ __device__ __forceinline__ int scan256(int v, int* part) {
 
 __global__ __launch_bounds__(kMapThreads) void page_map_kernel(MapArgs p) {
   __shared__ int s_off[kPagedSeqs + 1], s_len[kPagedSeqs], s_ok[kPagedSeqs];
+  __shared__ int s_page[kEntries][kPagedSeqs];   // pages of the trees' positions
   __shared__ int part_rows[4], part_take[4];
   __shared__ int s_taken;
   const int tid = threadIdx.x;
@@ -77,21 +79,23 @@ __global__ __launch_bounds__(kMapThreads) void page_map_kernel(MapArgs p) {
   if (named && (end > p.rows_cap || L < 0 ||
                 static_cast<long long>(L) + T > static_cast<long long>(p.max_pages) * P))
     status = ENTMTP_PAGE_RANGE;
-  // the entries the tree's positions fall into
+  // the entries the tree's positions fall into (all requested at once)
   int* const row = p.table + static_cast<size_t>(mine ? tid : 0) * p.max_pages;
-  const int p0 = L >> p.shift, p1 = (L + T - 1) >> p.shift;
+  const int p0 = L >> p.shift;
+  const int n = status == ENTMTP_PAGE_OK ? ((L + T - 1) >> p.shift) - p0 + 1 : 0;
+  int id[kEntries];
+#pragma unroll
+  for (int k = 0; k < kEntries; ++k) id[k] = k < n ? row[p0 + k] : 0;
   int lack = 0;
-  if (status == ENTMTP_PAGE_OK) {
-    bool bad = false;
-    for (int k = p0; k <= p1; ++k) {
-      const int id = row[k];
-      bad = bad || id >= p.n_pages || (id < 0 && k == p0 && (L & (P - 1)) != 0);   // it holds prefix slots
-      lack += id < 0;
-    }
-    if (bad) {
-      status = ENTMTP_PAGE_BAD;
-      lack = 0;
-    }
+  bool bad = n > 0 && id[0] < 0 && (L & (P - 1)) != 0;   // its page holds prefix slots
+#pragma unroll
+  for (int k = 0; k < kEntries; ++k) {
+    bad = bad || id[k] >= p.n_pages;
+    lack += id[k] < 0;
+  }
+  if (bad) {
+    status = ENTMTP_PAGE_BAD;
+    lack = 0;
   }
   const int upto = scan256(lack, part_take);
   if (lack > 0) {
@@ -100,16 +104,29 @@ __global__ __launch_bounds__(kMapThreads) void page_map_kernel(MapArgs p) {
     } else {
       atomicMax(&s_taken, upto);
       const int* top = p.free + (free_n - 1 - (upto - lack));
-      bool bad = false;
-      for (int k = 0; k < lack; ++k) bad = bad || top[-k] < 0 || top[-k] >= p.n_pages;
+      int take[kEntries];
+#pragma unroll
+      for (int k = 0; k < kEntries; ++k) take[k] = k < lack ? top[-k] : 0;
+#pragma unroll
+      for (int k = 0; k < kEntries; ++k) bad = bad || take[k] < 0 || take[k] >= p.n_pages;
       if (bad) {
         status = ENTMTP_PAGE_BAD;
       } else {
-        int k = 0;
-        for (int e = p0; e <= p1; ++e)
-          if (row[e] < 0) row[e] = top[-k++];
+#pragma unroll
+        for (int k = 0; k < kEntries; ++k)   // the j-th missing entry takes the j-th page
+          if (id[k] < 0) {
+            id[k] = take[0];
+            row[p0 + k] = take[0];
+#pragma unroll
+            for (int j = 0; j + 1 < kEntries; ++j) take[j] = take[j + 1];
+          }
       }
     }
+  }
+  if (mine) {
+#pragma unroll
+    for (int k = 0; k < kEntries; ++k)
+      if (k < n) s_page[k][tid] = id[k];
   }
   if (mine) {
     p.status[tid] = status;
@@ -122,21 +139,17 @@ __global__ __launch_bounds__(kMapThreads) void page_map_kernel(MapArgs p) {
     s_off[0] = 0;
     p.row_off[0] = 0;
   }
-  __syncthreads();   // (the table's new entries are seen, every thread has read *n_free)
+  __syncthreads();   // (and every thread has read *n_free)
   if (tid == 0 && p.free) *p.n_free = free_n - s_taken;
   const int rows = s_off[p.B];
+#pragma unroll 4   // (the searches' LDS round trips overlap)
   for (int r = tid; r < rows; r += kMapThreads) {
-    int lo = 0, hi = p.B;   // the last b with s_off[b] <= r
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (s_off[mid] <= r) lo = mid; else hi = mid;
-    }
-    int slot = -1;
-    if (s_ok[lo]) {
-      const int pos = s_len[lo] + (r - s_off[lo]);
-      slot = (p.table[static_cast<size_t>(lo) * p.max_pages + (pos >> p.shift)] << p.shift) + (pos & (P - 1));
-    }
-    p.slot_map[r] = slot;
+    int b = 0;   // the last sequence that starts at or before r
+#pragma unroll
+    for (int step = kPagedSeqs / 2; step >= 1; step >>= 1)
+      if (s_off[min(b + step, p.B)] <= r && b + step < p.B) b += step;
+    const int pos = s_len[b] + (r - s_off[b]);
+    p.slot_map[r] = s_ok[b] ? (s_page[(pos >> p.shift) - (s_len[b] >> p.shift)][b] << p.shift) + (pos & (P - 1)) : -1;
   }
 }
 

@@ -156,7 +156,7 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs p) {
   const int k = lane & 15;
   const int t = batch_target(k, work, nb_max, p.slots);
   int items = 0, split = 0;
-  for (int u = tid >> 4; u < kPagedSeqs; u += 16) {
+  for (int u = tid >> 4; u < p.B; u += 16) {
     const int n = paged_splits(s_nb[u], t);
     items += s_H[u] * n;
     split |= s_H[u] > 0 && n > 1;
@@ -301,13 +301,18 @@ __device__ __forceinline__ Const<T> as_const(const void* p) {
   return (Const<T>)reinterpret_cast<uintptr_t>(p);
 }
 
-__device__ __forceinline__ bool plan_is_ours(const PagedArgs& p) {
-  const Const<PlanHeader> h = as_const<PlanHeader>(p.plan);
+// A 64-byte record in one scalar load (field by field behind branches, a
+// header took a dozen round trips).
+typedef int i32x16 __attribute__((ext_vector_type(16)));
+__device__ __forceinline__ i32x16 record(const uint8_t* p) { return *as_const<i32x16>(p); }
+
+// Whether a plan's header h says that it was made for this call.
+__device__ __forceinline__ bool plan_is_ours(const PagedArgs& p, const PlanHeader& h) {
   const uintptr_t a = reinterpret_cast<uintptr_t>(p.arena);
-  return h->magic == kPlanMagic && h->B == p.B && h->Hq == p.Hq && h->Hkv == p.Hkv && h->shift == p.shift &&
-         h->n_pages == p.n_pages && h->max_pages == p.max_pages && h->rows_cap == p.rows_cap &&
-         h->window == p.window && h->arena_lo == static_cast<uint32_t>(a) &&
-         h->arena_hi == static_cast<uint32_t>(a >> 32);
+  return ((h.magic ^ kPlanMagic) | (h.B ^ p.B) | (h.Hq ^ p.Hq) | (h.Hkv ^ p.Hkv) | (h.shift ^ p.shift) |
+          (h.n_pages ^ p.n_pages) | (h.max_pages ^ p.max_pages) | (h.rows_cap ^ p.rows_cap) | (h.window ^ p.window) |
+          static_cast<int>(h.arena_lo ^ static_cast<uint32_t>(a)) |
+          static_cast<int>(h.arena_hi ^ static_cast<uint32_t>(a >> 32))) == 0;
 }
 
 // WIDE: the rotation's angles may pass the short sine's range (wide_angles).
@@ -325,18 +330,19 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
   uint8_t* const ring[4] = {slot0, slot1, slot2, slot3};
   static_assert(kRing == 4, "the ring's slots");
   const int x = static_cast<int>(blockIdx.x);
-  const Const<PlanItem> it = as_const<PlanItem>(p.plan + p.items_at) + x;
-  if (!plan_is_ours(p) || x >= as_const<PlanHeader>(p.plan)->items) return;
-  const int T = it->T, L = it->L, row0 = it->row0, D = it->D, b = it->b, g = it->g, qg = it->qg;
-  const int split = it->split, nsplit = it->nsplit, blk_lo = it->blk_lo, blk_hi = it->blk_hi;
-  if (T == 0) return;
+  const i32x16 head = record(p.plan), item = record(p.plan + p.items_at + static_cast<size_t>(x) * sizeof(PlanItem));
+  const PlanHeader h = __builtin_bit_cast(PlanHeader, head);
+  const PlanItem it = __builtin_bit_cast(PlanItem, item);
+  if (!plan_is_ours(p, h) | (x >= h.items) | (it.T == 0)) return;
+  const int T = it.T, L = it.L, row0 = it.row0, D = it.D, b = it.b, g = it.g, qg = it.qg;
+  const int split = it.split, nsplit = it.nsplit, blk_lo = it.blk_lo, blk_hi = it.blk_hi;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int li = lane & 31, lh = lane >> 5;
   const int nkeys = L + T, GT = p.G * T, P = 1 << p.shift;
   const int qt = qg * kTilesPerWg + wave;        // this wave's query tile
-  const bool live = qt < it->rows_pad / kQTile;   // (uniform per wave)
-  const uint32_t* const mask = reinterpret_cast<const uint32_t*>(p.arena + it->off_mask);
-  const int* const depth = reinterpret_cast<const int*>(p.arena + it->off_depth);
+  const bool live = qt < it.rows_pad / kQTile;   // (uniform per wave)
+  const uint32_t* const mask = reinterpret_cast<const uint32_t*>(p.arena + it.off_mask);
+  const int* const depth = reinterpret_cast<const int*>(p.arena + it.off_depth);
   const Const<int> pages = as_const<int>(p.table + static_cast<size_t>(b) * p.max_pages);
   const float c = MOD ? 1.f : p.scale_log2;   // (MOD: the scores are turned to base 2 as they are bent)
   const int nb = blk_hi - blk_lo;
@@ -396,22 +402,29 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
     int slot;
   };
   const int trow = tid >> 3, tcc = tid & 7;
+  auto tree_key = [&](int i) { return min((blk_lo + min(i, nb - 1)) * KB + trow, nkeys - 1); };
+  // the page of a prefix key, the slot of a tree key (the keeper's)
+  auto tree_find = [&](TreeRegs& t, int i) {
+    const int key = tree_key(i);
+    t.slot = -1;
+    if (key < L)
+      t.slot = p.table[static_cast<size_t>(b) * p.max_pages + (key >> p.shift)];
+    else if (keeper)
+      t.slot = p.slot_map[row0 + key - L];
+  };
   auto tree_load = [&](TreeRegs& t, int i) {
-    const int key = min((blk_lo + min(i, nb - 1)) * KB + trow, nkeys - 1);
+    const int key = tree_key(i);
     const uint16_t *kp, *vp;
     bool there = true;
-    t.slot = -1;
     if (key < L) {
-      const int page = p.table[static_cast<size_t>(b) * p.max_pages + (key >> p.shift)];
-      there = static_cast<unsigned>(page) < static_cast<unsigned>(p.n_pages) && key >= w_lo;
-      const size_t off = (((static_cast<size_t>(there ? page : 0) * p.Hkv + g) << p.shift) + (key & (P - 1))) * HD;
+      there = static_cast<unsigned>(t.slot) < static_cast<unsigned>(p.n_pages) && key >= w_lo;
+      const size_t off = (((static_cast<size_t>(there ? t.slot : 0) * p.Hkv + g) << p.shift) + (key & (P - 1))) * HD;
       kp = p.kp + off;
       vp = p.vp + off;
     } else {
       const size_t own = (static_cast<size_t>(row0 + key - L) * p.Hkv + g) * HD;
       kp = p.kt + own;
       vp = p.vt + own;
-      if (keeper) t.slot = p.slot_map[row0 + key - L];
     }
     kp += 8 * tcc;
     vp += 8 * tcc;
@@ -462,7 +475,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
   int page = page_of(0);
   const int page1 = page_of(1), page2 = page_of(2);
   TreeRegs tregs;
-  if (nb > np) tree_load(tregs, np);
+  if (nb > np) tree_find(tregs, np);
 
   // The small loads go first (this wave's Q fragments, its rows' depths and
   // masks, all unconditional: rows past the tree read row 0 and are never
@@ -487,6 +500,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
   float slope = 0.f;
   if constexpr (MOD)
     if (p.slopes) slope = p.slopes[qhead] * kLog2e;
+  if (nb > np) tree_load(tregs, np);
   gload(ring[0], 0, page);
   gload(ring[1], 1, page1);
   gload(ring[2], 2, page2);
@@ -697,6 +711,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
       const int buf = (i - np) & 1;
       uint8_t* const slot = buf ? slot1 : slot0;
       const int odd = tree_stage(slot, tregs, i, buf);
+      tree_find(tregs, i + 1);
       tree_load(tregs, i + 1);
       const bool any = __syncthreads_or(odd) != 0;
       if (live) {
@@ -722,8 +737,8 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
     const int r = row < GT ? row : 0;
     dst = p.out + (static_cast<size_t>(row0 + r % T) * p.Hq + g * p.G + r / T) * HD;
   } else {
-    const long long part = static_cast<long long>((static_cast<unsigned long long>(it->part_hi) << 32) | it->part_lo);
-    const size_t prow = part + (static_cast<size_t>(split) * p.Hkv + g) * it->rows_pad + row;
+    const long long part = static_cast<long long>((static_cast<unsigned long long>(it.part_hi) << 32) | it.part_lo);
+    const size_t prow = part + (static_cast<size_t>(split) * p.Hkv + g) * it.rows_pad + row;
     dst = p.part_o + prow * HD;
     if (lh == 0 && row < GT) {
       p.part_ml[prow * 2 + 0] = m_run;
@@ -758,33 +773,43 @@ constexpr int kMergeWaves = 4;
 constexpr int kMergeAhead = 8;
 
 __global__ __launch_bounds__(64 * kMergeWaves) void paged_merge_kernel(PagedArgs p) {
-  if (!plan_is_ours(p)) return;
   const int lane = threadIdx.x & 63;
   const int x = __builtin_amdgcn_readfirstlane(static_cast<int>(blockIdx.x) * kMergeWaves + (threadIdx.x >> 6));
   const int r = x / p.Hq, h = x % p.Hq;
-  if (r >= p.rows_cap) return;
-  // the sequence that holds row r
+  // every sequence's record, a lane each (with the header: one round trip)
+  const i32x16 head = record(p.plan);
   const PlanSeq* const seqs = reinterpret_cast<const PlanSeq*>(p.plan + sizeof(PlanHeader));
-  int2 at[kPagedSeqs / 64];
+  int4 at[kPagedSeqs / 64];
+  long long part[kPagedSeqs / 64];
 #pragma unroll
   for (int k = 0; k < kPagedSeqs / 64; ++k) {
     if (64 * k >= p.B) break;   // (uniform)
-    at[k] = *reinterpret_cast<const int2*>(seqs + min(64 * k + lane, p.B - 1));   // row0, T
+    const PlanSeq* const q = seqs + min(64 * k + lane, p.B - 1);
+    at[k] = *reinterpret_cast<const int4*>(q);   // row0, T, nsplit, rows_pad
+    part[k] = q->part_off;
   }
-  int b = -1;
+  if (!plan_is_ours(p, __builtin_bit_cast(PlanHeader, head)) | (r >= p.rows_cap)) return;
+  PlanSeq sq{};
 #pragma unroll
   for (int k = 0; k < kPagedSeqs / 64; ++k) {
     if (64 * k >= p.B) break;
     const unsigned long long m = __ballot(64 * k + lane < p.B && at[k].x <= r && r < at[k].x + at[k].y);
-    if (b < 0 && m) b = 64 * k + __builtin_ctzll(m);
+    if (m && sq.T == 0) {
+      const int l = __builtin_ctzll(m);
+      sq.row0 = __builtin_amdgcn_readlane(at[k].x, l);
+      sq.T = __builtin_amdgcn_readlane(at[k].y, l);
+      sq.nsplit = __builtin_amdgcn_readlane(at[k].z, l);
+      sq.rows_pad = __builtin_amdgcn_readlane(at[k].w, l);
+      const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(part[k]), l);
+      const uint32_t hi = __builtin_amdgcn_readlane(static_cast<int>(part[k] >> 32), l);
+      sq.part_off = static_cast<long long>(static_cast<unsigned long long>(hi) << 32 | lo);
+    }
   }
-  if (b < 0) return;
-  const Const<PlanSeq> sq = as_const<PlanSeq>(seqs) + b;
-  const int nsplit = sq->nsplit;
-  if (nsplit == 1) return;   // written by the attention
-  const int row = (h % p.G) * sq->T + (r - sq->row0);
-  const size_t base = sq->part_off + static_cast<size_t>(h / p.G) * sq->rows_pad + row;
-  const size_t stride = static_cast<size_t>(p.Hkv) * sq->rows_pad;   // from split to split
+  const int nsplit = sq.nsplit;
+  if (sq.T == 0 || nsplit == 1) return;   // no sequence's row, or written by the attention
+  const int row = (h % p.G) * sq.T + (r - sq.row0);
+  const size_t base = sq.part_off + static_cast<size_t>(h / p.G) * sq.rows_pad + row;
+  const size_t stride = static_cast<size_t>(p.Hkv) * sq.rows_pad;   // from split to split
   float m0 = -INFINITY, l0 = 0.f, m1 = -INFINITY, l1 = 0.f;
   if (lane < nsplit) {
     const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + (base + lane * stride) * 2);
