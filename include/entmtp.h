@@ -739,7 +739,8 @@ int32_t entmtp_ladder_next_batched(int32_t B, int32_t* rung, const float* s, int
  *   argmax, top1p  device [T]: the statistics of those logits at the same
  *            inv_temp (entmtp_logit_stats / entmtp_verify_logits_stats), so
  *            that p(v) = exp((z_v - z_argmax) * inv_temp) * top1p needs no
- *            pass over the vocabulary
+ *            pass over the vocabulary; argmax -1 and top1p 0 (a row that
+ *            entmtp_logit_adjust found empty) give no token any mass: bonus -1
  *   q        device fp32 [T][V]: the draft distribution node i's children
  *            were drawn from (rows sum to 1)
  *   u_accept, u_sample  device fp32 [T]: uniforms in [0, 1) (the method's

@@ -141,7 +141,9 @@ __global__ __launch_bounds__(kSpecThreads) void accept_stochastic_kernel(
         qc = qr[t];
       }
     } else if (tid == ENTMTP_T_MAX) {
-      s_zm = zr[s_amax[cur]];
+      // (a row that a mask left empty has no argmax: its logits are all -inf)
+      const int am = s_amax[cur];
+      s_zm = am >= 0 && am < V ? zr[am] : 0.f;
     }
     __syncthreads();
     int nchild = 0;
