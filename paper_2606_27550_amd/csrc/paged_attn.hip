@@ -344,7 +344,6 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
   const uint32_t* const mask = reinterpret_cast<const uint32_t*>(p.arena + it.off_mask);
   const int* const depth = reinterpret_cast<const int*>(p.arena + it.off_depth);
   const Const<int> pages = as_const<int>(p.table + static_cast<size_t>(b) * p.max_pages);
-  const float c = MOD ? 1.f : p.scale_log2;   // (MOD: the scores are turned to base 2 as they are bent)
   const int nb = blk_hi - blk_lo;
   const bool rope = p.theta > 0.0;
   // the first query group's workgroups keep the tree's keys (rotated) and
@@ -511,15 +510,24 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
   asm volatile("" : "+v"(freq));   // (the compiler would sink its load below the copies)
   float2* const tab32 = reinterpret_cast<float2*>(slot3);
   static_assert((ENTMTP_D_MAX + 1) * kRopePairs * sizeof(float2) <= kRingSlot, "the angles fit in a slot");
-  if (rope) rope_table<WIDE>(tid, D, L, freq, [&](int d, int pr, double2 cs) {
-    tab32[d * kRopePairs + (pr ^ (2 * (d & 31)))] = make_float2(static_cast<float>(cs.x), static_cast<float>(cs.y));
-  });
+  // (unless the scores are bent, times the scale in base 2: the products then
+  // give logits, and no rotation is a turn by nothing)
+  const float qs = MOD ? 1.f : p.scale_log2;
+  auto tab_put = [&](int d, int pr, double2 cs) {
+    tab32[d * kRopePairs + (pr ^ (2 * (d & 31)))] = make_float2(static_cast<float>(cs.x) * qs, static_cast<float>(cs.y) * qs);
+  };
+  if (rope) {
+    rope_table<WIDE>(tid, D, L, freq, tab_put);
+  } else if constexpr (!MOD) {
+    for (int d = tid / kRopePairs; d <= D; d += kAttnThreads / kRopePairs)
+      tab_put(d, tid % kRopePairs, make_double2(1.0, 0.0));
+  }
   s_depth[tid] = static_cast<uint8_t>(tdepth);
   static_assert(kAttnThreads >= ENTMTP_T_MAX, "one thread per node");
   wait_lds();
   stage_barrier();
   if (!qlive) mlo = mhi = u32x4{~0u, ~0u, ~0u, ~0u};   // padding rows see every key
-  if (rope) {
+  if (rope || !MOD) {
     const float2* tr = tab32 + qdepth * kRopePairs;
 #pragma unroll
     for (int s = 0; s < 4; ++s) rope_pairs_f32(qf[s], qf[s + 4], tr, 16 * s + 8 * lh, 2 * (qdepth & 31));
@@ -530,6 +538,13 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
 
   // l_run: the sum of this lane's half of the keys (the halves meet at the end)
   float m_run = -INFINITY, l_run = 0.f;
+  // Unless the scores are bent, a block's products start from minus the row's
+  // reference (zero before its first), so that they come out as the exponents
+  // themselves; lift: how far a block's largest may pass the reference.
+  f32x16 ref;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) ref[r] = 0.f;
+  float lift = -INFINITY;
   f32x16 o[4];
 #pragma unroll
   for (int ct = 0; ct < 4; ++ct)
@@ -546,8 +561,12 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
 
   // S^T = K Q^T of the block in a slot
   auto scores = [&](const uint8_t* slot, f32x16& sacc) {
+    if constexpr (MOD) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) sacc[r] = 0.f;
+      for (int r = 0; r < 16; ++r) sacc[r] = 0.f;
+    } else {
+      sacc = ref;
+    }
 #pragma unroll
     for (int s = 0; s < 8; ++s) {
       const u32x4 kf = *reinterpret_cast<const u32x4*>(slot + li * 256 + ((kx ^ (2 * s)) << 4));
@@ -565,8 +584,9 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
     return p.slopes ? fmaf(-slope, static_cast<float>(dist), y) : y;
   };
   // Block i's softmax (lazily raised max) and O^T += V^T P^T from its slot;
-  // prefix: every key of the block is in the prefix.
-  auto attend = [&](int i, const uint8_t* slot, f32x16& sacc, auto prefix, auto odd_of) {
+  // prefix: every key of the block is in the prefix; ahead: the next block's
+  // scores, which move with the reference they started from.
+  auto attend = [&](int i, const uint8_t* slot, f32x16& sacc, f32x16& ahead, auto prefix, auto odd_of) {
     float bmax = -INFINITY;
     const int kb = (blk_lo + i) * KB;
     if constexpr (decltype(prefix)::value) {
@@ -614,10 +634,10 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
       }
     }
     bmax = max_halves(bmax);
-    const float mb = bmax * c;
-    const bool need = mb > m_run + kLazyLog2;
+    // bent scores are held against m_run here, the others are relative to it
+    const bool need = MOD ? bmax > m_run + kLazyLog2 : bmax > lift;
     if (__any(need)) {
-      const float mn = need ? mb : m_run;
+      const float mn = !need ? m_run : (MOD || m_run == -INFINITY ? bmax : m_run + bmax);
       const float alpha = !need ? 1.f : (m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - mn));
       l_run *= alpha;
 #pragma unroll
@@ -625,13 +645,23 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[ct][r] *= alpha;
       m_run = mn;
+      if constexpr (!MOD) {
+        const float by = need ? bmax : 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          sacc[r] -= by;
+          ahead[r] -= by;
+          ref[r] -= by;
+        }
+        lift = need ? kLazyLog2 : lift;
+      }
     }
-    const float mneg = m_run == -INFINITY ? 0.f : -m_run;
+    const float mneg = !MOD || m_run == -INFINITY ? 0.f : -m_run;
     float pr[16];
     float rsum = 0.f;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      pr[r] = __builtin_amdgcn_exp2f(fmaf(sacc[r], c, mneg));
+      pr[r] = __builtin_amdgcn_exp2f(MOD ? sacc[r] + mneg : sacc[r]);
       rsum += pr[r];
     }
     l_run += rsum;
@@ -680,7 +710,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
       if (live) {
         f32x16& cur = k & 1 ? sb : sa;
         scores(ring[(k + 1) % kRing], k & 1 ? sa : sb);
-        attend(i0 + k, ring[k], cur, std::true_type{}, none);
+        attend(i0 + k, ring[k], cur, k & 1 ? sa : sb, std::true_type{}, none);
       }
     }
   }
@@ -694,7 +724,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
       if (i0 + k < np) {
         f32x16& cur = k & 1 ? sb : sa;
         if (k + 1 < kRing - 1) scores(ring[k + 1], k & 1 ? sa : sb);
-        attend(i0 + k, ring[k], cur, std::true_type{}, none);
+        attend(i0 + k, ring[k], cur, k & 1 ? sa : sb, std::true_type{}, none);
       }
   }
 
@@ -716,7 +746,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
       const bool any = __syncthreads_or(odd) != 0;
       if (live) {
         scores(slot, sa);
-        attend(i, slot, sa, std::false_type{}, [&](int n) {
+        attend(i, slot, sa, sb, std::false_type{}, [&](int n) {
           if (!any) return false;
           const uint2 f = *reinterpret_cast<const uint2*>(s_odd[buf][n]);
           return (f.x | f.y) != 0;
