@@ -138,7 +138,8 @@ def tree_attention_paged(q, kt, vt, k_pool, v_pool, table, L, parent, scale, the
     The last: a rounding to bf16 is off by at most u = 2^-8 of the value.  The
     weights and a split's partial are rounded (u sum p |v| each), so is out (u
     |out|); the rounding of a rotated or scaled query (scale in base 2 taken
-    into it: u of every element, whatever the scale) moves a score by at most d_k = u scale
+    into it: u of every element, whatever the scale), and the cap's own error
+    (softcap 2^-21), move a score by at most d_k = u scale
     sum |q_c k_c| (a score cap bends by at most one), all of a row's by at most
     D, and with it out by at most (e^(2 D) - 1) sum p |v - out|."""
     T, Hq, d = q.shape
@@ -171,6 +172,6 @@ def tree_attention_paged(q, kt, vt, k_pool, v_pool, table, L, parent, scale, the
             p = np.exp(z - z.max())
             p /= p.sum()
             out[i, h] = p @ v
-            D = u * scale * float((np.abs(k) @ np.abs(qf[i, h])).max())
+            D = u * scale * float((np.abs(k) @ np.abs(qf[i, h])).max()) + softcap * 2.0 ** -21
             off[i, h] = 2 * u * (p @ np.abs(v)) + u * np.abs(out[i, h]) + (math.exp(2 * D) - 1) * (p @ np.abs(v - out[i, h]))
     return out, orc.f64_to_bf16_bits(kf) if theta > 0 else kt, off

@@ -34,6 +34,7 @@ namespace {
 
 constexpr int kPagedSplits = 128;
 constexpr int kMaxKvHeads = 256;   // (work lists are counted in 32 bits)
+constexpr float kMaxCap = 1024.f;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kPlanThreads = kPagedSeqs;   // a thread per sequence
 constexpr int kPlanMagic = 0x50a6ed01;
@@ -64,7 +65,12 @@ struct PlanItem {
 };
 static_assert(sizeof(PlanItem) == 64, "plan layout");
 
-size_t plan_items_at(int B) { return (sizeof(PlanHeader) + sizeof(PlanSeq) * B + 63) / 64 * 64; }
+// A plan: header, sequences, the sequence of every tree row (a byte each; only
+// rows that hold one are written, the reader checks it against the sequence's
+// record), work items.
+size_t plan_rows_at(int B) { return sizeof(PlanHeader) + sizeof(PlanSeq) * B; }
+size_t plan_items_at(int B, int rows_cap) { return (plan_rows_at(B) + rows_cap + 63) / 64 * 64; }
+static_assert(kPagedSeqs <= 256, "a sequence is a byte");
 
 __host__ __device__ inline int paged_splits(int nb, int t) {
   if (nb <= kLoneBlocks) return 1;
@@ -91,7 +97,7 @@ struct PlanArgs {
   const int* table;
   int* bad;
   uint8_t* plan;
-  long long items_at, part_cap;
+  long long rows_at, items_at, part_cap;
   int B, G, Hq, Hkv, shift, n_pages, max_pages, rows_cap, window, slots, items_cap, two;
 };
 
@@ -245,6 +251,8 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs p) {
     it.part_hi = static_cast<uint32_t>(s_seq.part_off >> 32);
     list[i] = it;
   }
+  if (tid < sT) p.plan[p.rows_at + s_seq.row0 + tid] = static_cast<uint8_t>(b);
+  static_assert(kPlanThreads >= ENTMTP_T_MAX, "one thread per tree row");
   if (tid == 0) {
     PlanSeq q = s_seq;
     q.T = sT;
@@ -285,10 +293,10 @@ struct PagedArgs {
   uint16_t* part_o;      // [part rows][HD] bf16: the split's output, normalised by its sum
   float* part_ml;        // [part rows][2]
   uint16_t* out;         // [rows_cap][Hq][HD]
-  long long items_at;
-  int B, G, Hq, Hkv, shift, n_pages, max_pages, rows_cap, window, items_cap;
-  float scale_log2;
-  float cap_in, cap_log2;   // 2 log2(e) scale / cap, and cap log2(e); cap_log2 = 0: no cap
+  long long rows_at, items_at;
+  int B, G, Hq, Hkv, shift, n_pages, max_pages, rows_cap, window;
+  float q_scale;     // scale log2(e), or with a cap 2 log2(e) scale / cap
+  float cap_log2;    // cap log2(e), 0: no cap
   double theta;             // rotation base (0: no rotation)
   double freq[kRopePairs];
 };
@@ -326,6 +334,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
   __shared__ __attribute__((aligned(16))) uint8_t slot2[kRingSlot];
   __shared__ __attribute__((aligned(16))) uint8_t slot3[kRingSlot];
   __shared__ uint8_t s_depth[ENTMTP_T_MAX];
+  __shared__ int s_any[2][4];
   __shared__ __attribute__((aligned(8))) uint8_t s_odd[2][KB][8];   // tree values that are not finite, by key and chunk pair
   uint8_t* const ring[4] = {slot0, slot1, slot2, slot3};
   static_assert(kRing == 4, "the ring's slots");
@@ -510,15 +519,15 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
   asm volatile("" : "+v"(freq));   // (the compiler would sink its load below the copies)
   float2* const tab32 = reinterpret_cast<float2*>(slot3);
   static_assert((ENTMTP_D_MAX + 1) * kRopePairs * sizeof(float2) <= kRingSlot, "the angles fit in a slot");
-  // (unless the scores are bent, times the scale in base 2: the products then
-  // give logits, and no rotation is a turn by nothing)
-  const float qs = MOD ? 1.f : p.scale_log2;
+  // (times what the scores are scaled by, so that the products give logits in
+  // base 2, or the cap's argument; no rotation is a turn by nothing)
+  const float qs = p.q_scale;
   auto tab_put = [&](int d, int pr, double2 cs) {
     tab32[d * kRopePairs + (pr ^ (2 * (d & 31)))] = make_float2(static_cast<float>(cs.x) * qs, static_cast<float>(cs.y) * qs);
   };
   if (rope) {
     rope_table<WIDE>(tid, D, L, freq, tab_put);
-  } else if constexpr (!MOD) {
+  } else {
     for (int d = tid / kRopePairs; d <= D; d += kAttnThreads / kRopePairs)
       tab_put(d, tid % kRopePairs, make_double2(1.0, 0.0));
   }
@@ -527,7 +536,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
   wait_lds();
   stage_barrier();
   if (!qlive) mlo = mhi = u32x4{~0u, ~0u, ~0u, ~0u};   // padding rows see every key
-  if (rope || !MOD) {
+  {
     const float2* tr = tab32 + qdepth * kRopePairs;
 #pragma unroll
     for (int s = 0; s < 4; ++s) rope_pairs_f32(qf[s], qf[s + 4], tr, 16 * s + 8 * lh, 2 * (qdepth & 31));
@@ -573,16 +582,21 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
       sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kf), as_bf16x8(qf[s]), sacc, 0, 0, 0);
     }
   };
-  // MOD: a raw score at distance dist as its logit in base 2.  tanh(u) = 1 -
-  // 2 / (e^2u + 1): 0 and infinity of the exponential give -1 and 1.
-  auto bend = [&](float s, int dist) {
-    float y = s * p.scale_log2;
+  // MOD: the block's products as logits in base 2, key r at distance dist(r).
+  // tanh(u) = 1 - 2 / (e^2u + 1) with 2 u / ln 2 from the products: 0 and
+  // infinity of the exponential give -1 and 1.
+  auto bend = [&](f32x16& sacc, auto dist) {
     if (p.cap_log2 > 0.f) {
-      const float e = __builtin_amdgcn_exp2f(s * p.cap_in);
-      y = fmaf(-2.f * p.cap_log2, __builtin_amdgcn_rcpf(e + 1.f), p.cap_log2);
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        sacc[r] = fmaf(-2.f * p.cap_log2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(sacc[r]) + 1.f), p.cap_log2);
     }
-    return p.slopes ? fmaf(-slope, static_cast<float>(dist), y) : y;
+    if (p.slopes) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sacc[r] = fmaf(-slope, static_cast<float>(dist(r)), sacc[r]);
+    }
   };
+  auto key_of = [&](int r) { return 8 * (r >> 2) + 4 * lh + (r & 3); };   // accumulator r's key of the block
   // Block i's softmax (lazily raised max) and O^T += V^T P^T from its slot;
   // prefix: every key of the block is in the prefix; ahead: the next block's
   // scores, which move with the reference they started from.
@@ -591,12 +605,11 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
     const int kb = (blk_lo + i) * KB;
     if constexpr (decltype(prefix)::value) {
       if constexpr (MOD) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) sacc[r] = bend(sacc[r], qpos - (kb + 8 * (r >> 2) + 4 * lh + (r & 3)));
+        bend(sacc, [&](int r) { return qpos - (kb + key_of(r)); });
         if (kb < w_hi) {
 #pragma unroll
           for (int r = 0; r < 16; ++r)
-            if (kb + 8 * (r >> 2) + 4 * lh + (r & 3) < w_row) sacc[r] = -INFINITY;
+            if (kb + key_of(r) < w_row) sacc[r] = -INFINITY;
         }
       }
 #pragma unroll
@@ -618,16 +631,17 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
         const uint32_t lo = word(wi), hi = word(wi + 1);
         win = sh ? (lo >> sh) | (hi << (32 - sh)) : lo;
       }
+      // (a tree key's position is that of its depth)
+      auto pos_k = [&](int r) {
+        const int j = kb + key_of(r) - L;
+        return j < 0 ? kb + key_of(r) : L + s_depth[min(j, ENTMTP_T_MAX - 1)];
+      };
+      if constexpr (MOD) bend(sacc, [&](int r) { return qpos - pos_k(r); });
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const int n = 8 * (r >> 2) + 4 * lh + (r & 3);
+        const int n = key_of(r);
         bool vis = ((win >> n) & 1u) && (kb + n < nkeys);
-        if constexpr (MOD) {
-          const int j = kb + n - L;
-          const int kpos = j < 0 ? kb + n : L + s_depth[min(j, ENTMTP_T_MAX - 1)];
-          sacc[r] = bend(sacc[r], qpos - kpos);
-          vis = vis && kpos >= w_row;
-        }
+        if constexpr (MOD) vis = vis && pos_k(r) >= w_row;
         sacc[r] = vis ? sacc[r] : -INFINITY;
         bmax = fmaxf(bmax, sacc[r]);
         if (odd_of(n) && vis) l_run = NAN;
@@ -665,7 +679,8 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
       rsum += pr[r];
     }
     l_run += rsum;
-    bf16x8 pf[2];   // (weights up to 2^8 in bf16: a relative rounding of 2^-9, averaged over the keys)
+    bf16x8 pf[2];   // (weights up to 2^8 in bf16, as the matrix instructions want them: off by at most 2^-8 each, averaged over
+    // the keys)
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       u32x4 w;
@@ -740,11 +755,17 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
     for (int i = np; i < nb; ++i) {
       const int buf = (i - np) & 1;
       uint8_t* const slot = buf ? slot1 : slot0;
-      const int odd = tree_stage(slot, tregs, i, buf);
-      tree_find(tregs, i + 1);
-      tree_load(tregs, i + 1);
-      const bool any = __syncthreads_or(odd) != 0;
+      const bool odd = tree_stage(slot, tregs, i, buf);
+      if (lane == 0) s_any[buf][wave] = 0;
+      if (__any(odd) && lane == 0) s_any[buf][wave] = 1;
+      if (i + 1 < nb) {   // (in flight during this block's products: the barrier waits for the LDS alone)
+        tree_find(tregs, i + 1);
+        tree_load(tregs, i + 1);
+      }
+      wait_lds();
+      stage_barrier();
       if (live) {
+        const bool any = (s_any[buf][0] | s_any[buf][1] | s_any[buf][2] | s_any[buf][3]) != 0;
         scores(slot, sa);
         attend(i, slot, sa, sb, std::false_type{}, [&](int n) {
           if (!any) return false;
@@ -794,92 +815,77 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
 
 // ----------------------------------------------------------------- merge --
 
-// One wavefront per (tree row, query head): lane c reads the (max, sum) of
-// splits c and c + 64, the halves of the wavefront take the partial outputs of
-// even and odd splits, four dims a lane, the first kMergeAhead of each half
-// requested with the (max, sum) pairs (one memory round trip), later ones
-// kMergeAhead at a time.
-constexpr int kMergeWaves = 4;
-constexpr int kMergeAhead = 8;
+// A workgroup takes eight query heads of a tree row, a half-wavefront each: lane
+// c reads the (max, sum) of splits c, c + 32, .., every lane four dims of the
+// splits' partial outputs, the first kMergeAhead of them requested with the
+// (max, sum) pairs (one memory round trip), later ones kMergeAhead at a time.
+// The row's sequence is found by scalar loads: its number, then its record.
+constexpr int kMergeHeads = 8;
+constexpr int kMergeAhead = 16;
+constexpr int kMergeLanes = kPagedSplits / 32;   // (max, sum) pairs a lane
 
-__global__ __launch_bounds__(64 * kMergeWaves) void paged_merge_kernel(PagedArgs p) {
-  const int lane = threadIdx.x & 63;
-  const int x = __builtin_amdgcn_readfirstlane(static_cast<int>(blockIdx.x) * kMergeWaves + (threadIdx.x >> 6));
-  const int r = x / p.Hq, h = x % p.Hq;
-  // every sequence's record, a lane each (with the header: one round trip)
+__global__ __launch_bounds__(32 * kMergeHeads) void paged_merge_kernel(PagedArgs p) {
+  const int groups = (p.Hq + kMergeHeads - 1) / kMergeHeads;
+  const int r = static_cast<int>(blockIdx.x) / groups;   // (below rows_cap, by the grid)
+  const int h = (static_cast<int>(blockIdx.x) % groups) * kMergeHeads + (threadIdx.x >> 5);
   const i32x16 head = record(p.plan);
-  const PlanSeq* const seqs = reinterpret_cast<const PlanSeq*>(p.plan + sizeof(PlanHeader));
-  int4 at[kPagedSeqs / 64];
-  long long part[kPagedSeqs / 64];
-#pragma unroll
-  for (int k = 0; k < kPagedSeqs / 64; ++k) {
-    if (64 * k >= p.B) break;   // (uniform)
-    const PlanSeq* const q = seqs + min(64 * k + lane, p.B - 1);
-    at[k] = *reinterpret_cast<const int4*>(q);   // row0, T, nsplit, rows_pad
-    part[k] = q->part_off;
-  }
-  if (!plan_is_ours(p, __builtin_bit_cast(PlanHeader, head)) | (r >= p.rows_cap)) return;
-  PlanSeq sq{};
-#pragma unroll
-  for (int k = 0; k < kPagedSeqs / 64; ++k) {
-    if (64 * k >= p.B) break;
-    const unsigned long long m = __ballot(64 * k + lane < p.B && at[k].x <= r && r < at[k].x + at[k].y);
-    if (m && sq.T == 0) {
-      const int l = __builtin_ctzll(m);
-      sq.row0 = __builtin_amdgcn_readlane(at[k].x, l);
-      sq.T = __builtin_amdgcn_readlane(at[k].y, l);
-      sq.nsplit = __builtin_amdgcn_readlane(at[k].z, l);
-      sq.rows_pad = __builtin_amdgcn_readlane(at[k].w, l);
-      const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(part[k]), l);
-      const uint32_t hi = __builtin_amdgcn_readlane(static_cast<int>(part[k] >> 32), l);
-      sq.part_off = static_cast<long long>(static_cast<unsigned long long>(hi) << 32 | lo);
-    }
-  }
-  const int nsplit = sq.nsplit;
-  if (sq.T == 0 || nsplit == 1) return;   // no sequence's row, or written by the attention
+  const size_t byte = static_cast<size_t>(p.rows_at) + r;
+  const uint32_t word = *as_const<uint32_t>(p.plan + (byte & ~size_t(3)));
+  const int b = min(static_cast<int>(word >> (8 * (byte & 3)) & 0xffu), p.B - 1);
+  typedef int i32x8 __attribute__((ext_vector_type(8)));
+  const PlanSeq sq =
+      __builtin_bit_cast(PlanSeq, *as_const<i32x8>(p.plan + sizeof(PlanHeader) + static_cast<size_t>(b) * sizeof(PlanSeq)));
+  if (!plan_is_ours(p, __builtin_bit_cast(PlanHeader, head)) | (r < sq.row0) | (r >= sq.row0 + sq.T) | (sq.nsplit == 1))
+    return;   // (a row of no sequence, or written by the attention)
+  if (h >= p.Hq) return;
+  const int nsplit = sq.nsplit, lane = threadIdx.x & 31;
   const int row = (h % p.G) * sq.T + (r - sq.row0);
   const size_t base = sq.part_off + static_cast<size_t>(h / p.G) * sq.rows_pad + row;
   const size_t stride = static_cast<size_t>(p.Hkv) * sq.rows_pad;   // from split to split
-  float m0 = -INFINITY, l0 = 0.f, m1 = -INFINITY, l1 = 0.f;
-  if (lane < nsplit) {
-    const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + (base + lane * stride) * 2);
-    m0 = ml.x;
-    l0 = ml.y;
+  const uint16_t* const po = p.part_o + base * HD + 4 * lane;
+  float m[kMergeLanes], l[kMergeLanes];
+#pragma unroll
+  for (int k = 0; k < kMergeLanes; ++k) {
+    m[k] = -INFINITY;
+    l[k] = 0.f;
+    if (lane + 32 * k < nsplit) {
+      const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + (base + (lane + 32 * k) * stride) * 2);
+      m[k] = ml.x;
+      l[k] = ml.y;
+    }
   }
-  if (lane + 64 < nsplit) {
-    const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + (base + (lane + 64) * stride) * 2);
-    m1 = ml.x;
-    l1 = ml.y;
-  }
-  const int half = lane >> 5, d4 = 4 * (lane & 31);
-  const uint16_t* const po = p.part_o + base * HD + d4;
   uint2 ob[kMergeAhead];
   auto request = [&](int c0) {
 #pragma unroll
     for (int k = 0; k < kMergeAhead; ++k)
-      ob[k] = *reinterpret_cast<const uint2*>(po + min(c0 + 2 * k + half, nsplit - 1) * stride * HD);
+      if (c0 + k < nsplit) ob[k] = *reinterpret_cast<const uint2*>(po + (c0 + k) * stride * HD);   // (uniform)
   };
   request(0);
-  float M = fmaxf(m0, m1);
+  float M = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+  static_assert(kMergeLanes == 4, "four pairs a lane");
 #pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, 64));
+  for (int off = 16; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, 32));
   // (a split that sees no key of the row has max -inf and counts for nothing;
   // where M is -inf too the row has a NaN score, kept in a sum)
-  float w0 = m0 == -INFINITY ? l0 : l0 * __builtin_amdgcn_exp2f(m0 - M);
-  float w1 = m1 == -INFINITY ? l1 : l1 * __builtin_amdgcn_exp2f(m1 - M);
-  float lsum = w0 + w1;
+  float lsum = 0.f;
 #pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) lsum += __shfl_xor(lsum, off, 64);
-  w0 /= lsum;   // the split's share of the row
-  w1 /= lsum;
+  for (int k = 0; k < kMergeLanes; ++k) {
+    l[k] = m[k] == -INFINITY ? l[k] : l[k] * __builtin_amdgcn_exp2f(m[k] - M);
+    lsum += l[k];
+  }
+#pragma unroll
+  for (int off = 16; off >= 1; off >>= 1) lsum += __shfl_xor(lsum, off, 32);
+  const float inv = 1.f / lsum;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int c0 = 0; c0 < nsplit; c0 += 2 * kMergeAhead) {
+  for (int c0 = 0; c0 < nsplit; c0 += kMergeAhead) {
     if (c0 > 0) request(c0);
+    float w = l[0];   // the splits' weights, lane c % 32 holding split c's (c0 to c0 + 15 lie in one register)
+#pragma unroll
+    for (int k = 1; k < kMergeLanes; ++k) w = c0 >= 32 * k ? l[k] : w;
 #pragma unroll
     for (int k = 0; k < kMergeAhead; ++k) {
-      const int c = c0 + 2 * k + half;
-      const float wc = __shfl(c < 64 ? w0 : w1, c & 63, 64);
-      if (c < nsplit) {
+      const float wc = __shfl(w, (c0 + k) & 31, 32);
+      if (c0 + k < nsplit) {
         acc.x = fmaf(wc, __uint_as_float(ob[k].x << 16), acc.x);
         acc.y = fmaf(wc, __uint_as_float(ob[k].x & 0xffff0000u), acc.y);
         acc.z = fmaf(wc, __uint_as_float(ob[k].y << 16), acc.z);
@@ -887,14 +893,9 @@ __global__ __launch_bounds__(64 * kMergeWaves) void paged_merge_kernel(PagedArgs
       }
     }
   }
-  acc.x += __shfl_xor(acc.x, 32, 64);
-  acc.y += __shfl_xor(acc.y, 32, 64);
-  acc.z += __shfl_xor(acc.z, 32, 64);
-  acc.w += __shfl_xor(acc.w, 32, 64);
-  if (half) return;
-  const uint2 pk = {__builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{acc.x, acc.y}), bf16x2)),
-                    __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{acc.z, acc.w}), bf16x2))};
-  *reinterpret_cast<uint2*>(p.out + (static_cast<size_t>(r) * p.Hq + h) * HD + d4) = pk;
+  const uint2 pk = {__builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{acc.x * inv, acc.y * inv}), bf16x2)),
+                    __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{acc.z * inv, acc.w * inv}), bf16x2))};
+  *reinterpret_cast<uint2*>(p.out + (static_cast<size_t>(r) * p.Hq + h) * HD + 4 * lane) = pk;
 }
 
 // ------------------------------------------------------------------ host --
@@ -926,11 +927,11 @@ PagedShape paged_shape(const entmtp_bank* bank, int B, int rows_cap, int Hq, int
   sh.splits = bound > 1;
   const int nqg = query_groups(rows_padded(G, T_max) / kQTile);
   const long long all = static_cast<long long>(B) * ((static_cast<long long>(Hkv) * bound + 7) / 8 * 8) * nqg;
-  const long long most = (sh.two ? 2LL : 1LL) * slots + streams + 7 * groups;
+  const long long most = (sh.two ? 2LL : 1LL) * slots + streams + (Hkv % 8 ? 7 * groups : 0);
   sh.items = static_cast<int>(std::min(std::min(most, all), static_cast<long long>(INT32_MAX)));
   if (sh.splits)
     sh.part_rows = static_cast<long long>(sh.items) * std::min(kTilesPerWg * kQTile, rows_padded(G, T_max));
-  sh.plan_bytes = plan_items_at(B) + sizeof(PlanItem) * static_cast<size_t>(sh.items);
+  sh.plan_bytes = plan_items_at(B, rows_cap) + sizeof(PlanItem) * static_cast<size_t>(sh.items);
   sh.workspace = up256(static_cast<size_t>(sh.part_rows) * HD * sizeof(uint16_t)) +
                  up256(static_cast<size_t>(sh.part_rows) * 2 * sizeof(float));
   return sh;
@@ -998,7 +999,8 @@ extern "C" int32_t entmtp_tree_attn_paged_plan(const entmtp_bank* bank, int32_t 
   a.table = block_table;
   a.bad = bad;
   a.plan = static_cast<uint8_t*>(plan);
-  a.items_at = static_cast<long long>(plan_items_at(B));
+  a.rows_at = static_cast<long long>(plan_rows_at(B));
+  a.items_at = static_cast<long long>(plan_items_at(B, rows_cap));
   a.part_cap = sh.part_rows;
   a.B = B;
   a.G = Hq / Hkv;
@@ -1031,9 +1033,10 @@ extern "C" int32_t entmtp_tree_attn_paged(const entmtp_bank* bank, int32_t B, co
   ENTMTP_CHECK_ARG(d == HD, ENTMTP_EINVAL, "head dim %d unsupported (built for %d)", d, HD);
   ENTMTP_CHECK_ARG(scale > 0.f && scale < INFINITY, ENTMTP_EINVAL, "scale must be positive");
   ENTMTP_CHECK_ARG(rope_theta >= 0.f && rope_theta < INFINITY, ENTMTP_EINVAL, "rope_theta must be >= 0");
-  ENTMTP_CHECK_ARG(softcap >= 0.f && softcap < INFINITY && (softcap == 0.f || 4.f * (scale / softcap) < INFINITY),
-                   ENTMTP_EINVAL, "softcap = %g must be 0 or positive, scale / softcap finite",
-                   static_cast<double>(softcap));
+  // (1 - 2 / (e^2u + 1) is off by about 2^-22, the cap times that)
+  ENTMTP_CHECK_ARG(softcap >= 0.f && softcap <= kMaxCap && (softcap == 0.f || 4.f * (scale / softcap) < INFINITY),
+                   ENTMTP_EINVAL, "softcap = %g must be 0 or in (0, %g], scale / softcap finite",
+                   static_cast<double>(softcap), static_cast<double>(kMaxCap));
   ENTMTP_CHECK_ARG((reinterpret_cast<uintptr_t>(plan) & 63u) == 0, ENTMTP_EINVAL, "the plan must be 64-byte aligned");
   ENTMTP_CHECK_ARG(aligned16(q) && aligned16(k_tree) && aligned16(v_tree) && aligned16(k_pool) && aligned16(v_pool) &&
                        aligned16(out) && aligned16(workspace),
@@ -1061,7 +1064,8 @@ extern "C" int32_t entmtp_tree_attn_paged(const entmtp_bank* bank, int32_t B, co
   a.part_ml = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) +
                                        up256(static_cast<size_t>(sh.part_rows) * HD * sizeof(uint16_t)));
   a.out = out;
-  a.items_at = static_cast<long long>(plan_items_at(B));
+  a.rows_at = static_cast<long long>(plan_rows_at(B));
+  a.items_at = static_cast<long long>(plan_items_at(B, rows_cap));
   a.B = B;
   a.G = Hq / Hkv;
   a.Hq = Hq;
@@ -1071,9 +1075,7 @@ extern "C" int32_t entmtp_tree_attn_paged(const entmtp_bank* bank, int32_t B, co
   a.max_pages = max_pages;
   a.rows_cap = rows_cap;
   a.window = window;
-  a.items_cap = sh.items;
-  a.scale_log2 = scale * kLog2e;
-  a.cap_in = softcap > 0.f ? 2.f * kLog2e * (scale / softcap) : 0.f;
+  a.q_scale = softcap > 0.f ? 2.f * kLog2e * (scale / softcap) : scale * kLog2e;
   a.cap_log2 = softcap * kLog2e;
   a.theta = static_cast<double>(rope_theta);
   rope_freqs(rope_theta, a.freq);
@@ -1086,9 +1088,8 @@ extern "C" int32_t entmtp_tree_attn_paged(const entmtp_bank* bank, int32_t B, co
     wide ? go(paged_attn_kernel<true, false>) : go(paged_attn_kernel<false, false>);
   if (int32_t rc = launch_status("tree_attn_paged launch")) return rc;
   if (!sh.splits) return ENTMTP_OK;
-  const long long pairs = static_cast<long long>(rows_cap) * Hq;
-  ENTMTP_CHECK_ARG(pairs / kMergeWaves < INT32_MAX, ENTMTP_ERANGE, "%d rows of %d heads: too many", rows_cap, Hq);
-  hipLaunchKernelGGL(paged_merge_kernel, dim3(static_cast<uint32_t>((pairs + kMergeWaves - 1) / kMergeWaves)),
-                     dim3(64 * kMergeWaves), 0, s, a);
+  const long long blocks = static_cast<long long>(rows_cap) * ((Hq + kMergeHeads - 1) / kMergeHeads);
+  ENTMTP_CHECK_ARG(blocks <= INT32_MAX, ENTMTP_ERANGE, "%d rows of %d heads: too many", rows_cap, Hq);
+  hipLaunchKernelGGL(paged_merge_kernel, dim3(static_cast<uint32_t>(blocks)), dim3(32 * kMergeHeads), 0, s, a);
   return launch_status("tree_attn_paged merge launch");
 }

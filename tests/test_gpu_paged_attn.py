@@ -130,8 +130,8 @@ def test_against_64_bits(api, topo, lens, Hq, Hkv, page):
     check(c, d)
 
 
-OPTIONS = [dict(softcap=3.0), dict(window=1), dict(window=2), dict(window=5), dict(window=33), dict(window=64),
-           dict(window=500), dict(window=2 ** 31 - 1), dict(slopes=True), dict(softcap=30.0, window=40),
+OPTIONS = [dict(softcap=3.0), dict(softcap=1024.0), dict(softcap=0.01), dict(window=1), dict(window=2),
+           dict(window=5), dict(window=33), dict(window=64), dict(window=500), dict(window=2 ** 31 - 1), dict(slopes=True), dict(softcap=30.0, window=40),
            dict(softcap=2.0, window=100, slopes=True), dict(theta=0.0), dict(theta=0.0, softcap=5.0, window=7),
            dict(theta=0.5), dict(theta=0.5, window=90)]
 

@@ -155,7 +155,8 @@ def test_plan_refusals(bank, change, code):
     (dict(slots=None), api.EINVAL), (dict(ws=ODD), api.EINVAL), (dict(d=64), api.EINVAL), (dict(scale=0.0), api.EINVAL),
     (dict(scale=float("nan")), api.EINVAL), (dict(scale=float("inf")), api.EINVAL), (dict(theta=-1.0), api.EINVAL),
     (dict(theta=float("inf")), api.EINVAL), (dict(softcap=-1.0), api.EINVAL), (dict(softcap=float("nan")), api.EINVAL),
-    (dict(softcap=float("inf")), api.EINVAL), (dict(softcap=1e-42, scale=1.0), api.EINVAL)])
+    (dict(softcap=float("inf")), api.EINVAL), (dict(softcap=1e-42, scale=1.0), api.EINVAL),
+    (dict(softcap=1025.0), api.EINVAL)])
 def test_paged_attention_refusals(bank, change, code):
     refused(call("entmtp_tree_attn_paged", ATTN, **{"bank": bank.handle, **change}), code)
 
