@@ -596,9 +596,10 @@ int32_t entmtp_tree_attn_paged_plan(const entmtp_bank* bank, int32_t B, const in
  *            split: NULL is allowed then); calls that share one must be
  *            ordered
  * A plan made for other sizes, another window or another bank leaves every
- * output alone.  Values of tree nodes that are not finite reach the rows that
- * see them (all dims become NaN) and no others; keys and values before the
- * root's window are not read.
+ * output alone.  Keys and values that are not finite reach the rows that see
+ * them (from a tree node's value, or one that a window hides from part of the
+ * tree, all dims become NaN) and no others; keys and values before the root's
+ * window are not read.
  * Requirements: d == ENTMTP_HEAD_DIM; otherwise as the plan.
  * Errors (host-checked): EINVAL, ERANGE, ENOSPC, EHIP.
  */

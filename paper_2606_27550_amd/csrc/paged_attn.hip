@@ -323,6 +323,13 @@ __device__ __forceinline__ bool plan_is_ours(const PagedArgs& p, const PlanHeade
           static_cast<int>(h.arena_hi ^ static_cast<uint32_t>(a >> 32))) == 0;
 }
 
+// A pair of bf16 values with those that are not finite as zeros (odd is set).
+__device__ __forceinline__ uint32_t finite_pair(uint32_t w, bool& odd) {
+  const bool lo = (w & 0x7f80u) == 0x7f80u, hi = (w & 0x7f800000u) == 0x7f800000u;
+  odd = odd || lo || hi;
+  return w & ((lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u));
+}
+
 // WIDE: the rotation's angles may pass the short sine's range (wide_angles).
 // MOD: a score cap, distance bias or window.
 template <bool WIDE, bool MOD>
@@ -460,15 +467,10 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
         *reinterpret_cast<u32x4*>(vd + HD / 2) = t.v1;
       }
     }
-    auto finite = [&](uint32_t w) {
-      const bool lo = (w & 0x7f80u) == 0x7f80u, hi = (w & 0x7f800000u) == 0x7f800000u;
-      odd = odd || lo || hi;
-      return w & ((lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u));
-    };
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      t.v0[e] = finite(t.v0[e]);
-      t.v1[e] = finite(t.v1[e]);
+      t.v0[e] = finite_pair(t.v0[e], odd);
+      t.v1[e] = finite_pair(t.v1[e], odd);
     }
     s_odd[buf][trow][tcc] = odd;
     uint8_t* const row = slot + trow * 256;
@@ -597,6 +599,10 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
     }
   };
   auto key_of = [&](int r) { return 8 * (r >> 2) + 4 * lh + (r & 3); };   // accumulator r's key of the block
+  auto odd_key = [&](int buf, int n) {
+    const uint2 f = *reinterpret_cast<const uint2*>(s_odd[buf][n]);
+    return (f.x | f.y) != 0;
+  };
   // Block i's softmax (lazily raised max) and O^T += V^T P^T from its slot;
   // prefix: every key of the block is in the prefix; ahead: the next block's
   // scores, which move with the reference they started from.
@@ -608,8 +614,12 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
         bend(sacc, [&](int r) { return qpos - (kb + key_of(r)); });
         if (kb < w_hi) {
 #pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (kb + key_of(r) < w_row) sacc[r] = -INFINITY;
+          for (int r = 0; r < 16; ++r) {
+            const int n = key_of(r);
+            const bool vis = kb + n >= w_row;
+            sacc[r] = vis ? sacc[r] : -INFINITY;
+            if (vis && odd_key(i & 1, n)) l_run = NAN;
+          }
         }
       }
 #pragma unroll
@@ -679,8 +689,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
       rsum += pr[r];
     }
     l_run += rsum;
-    bf16x8 pf[2];   // (weights up to 2^8 in bf16, as the matrix instructions want them: off by at most 2^-8 each, averaged over
-    // the keys)
+    bf16x8 pf[2];   // (weights up to 2^8 in bf16, as the products take them: each off by at most 2^-8)
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       u32x4 w;
@@ -712,6 +721,31 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
   // so the count in flight is always the same.
   f32x16 sa, sb;
   wait_vmcnt<(kRing - 2) * kRingLoads>();
+  if constexpr (MOD) {
+    // At the window's edge some rows of a tile see a prefix key and others do
+    // not.  Values there that are not finite are taken as zeros (a zero weight
+    // would make them NaNs) and noted, and the rows that see them become NaN.
+    // A tree's positions differ by less than a block, so the edge lies in the
+    // split's first two blocks; each wave's rows are those that it copied.
+    static_assert(ENTMTP_D_MAX < KB, "the edge lies in two blocks");
+    if (blk_lo * KB < w_hi) {
+      wait_vmcnt<(kRing - 3) * kRingLoads>();
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        bool odd = false;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          u32x4* const at = reinterpret_cast<u32x4*>(ring[k] + kRingK + trow * 256 + (((tcc + 8 * c) ^ v_swz(trow)) << 4));
+          u32x4 v = *at;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = finite_pair(v[e], odd);
+          *at = v;
+        }
+        s_odd[k][trow][tcc] = odd;
+      }
+      wait_lds();
+    }
+  }
   stage_barrier();
   if (live) scores(ring[0], sa);
   int i0 = 0;
@@ -767,11 +801,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
       if (live) {
         const bool any = (s_any[buf][0] | s_any[buf][1] | s_any[buf][2] | s_any[buf][3]) != 0;
         scores(slot, sa);
-        attend(i, slot, sa, sb, std::false_type{}, [&](int n) {
-          if (!any) return false;
-          const uint2 f = *reinterpret_cast<const uint2*>(s_odd[buf][n]);
-          return (f.x | f.y) != 0;
-        });
+        attend(i, slot, sa, sb, std::false_type{}, [&](int n) { return any && odd_key(buf, n); });
       }
     }
   }
@@ -1079,6 +1109,8 @@ extern "C" int32_t entmtp_tree_attn_paged(const entmtp_bank* bank, int32_t B, co
   a.cap_log2 = softcap * kLog2e;
   a.theta = static_cast<double>(rope_theta);
   rope_freqs(rope_theta, a.freq);
+  const long long blocks = static_cast<long long>(rows_cap) * ((Hq + kMergeHeads - 1) / kMergeHeads);
+  ENTMTP_CHECK_ARG(blocks <= INT32_MAX, ENTMTP_ERANGE, "%d rows of %d heads: too many", rows_cap, Hq);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(sh.items), dim3(kAttnThreads), 0, s, a); };
   const bool mod = softcap > 0.f || window > 0 || slopes != nullptr, wide = wide_angles(a.theta);
@@ -1088,8 +1120,6 @@ extern "C" int32_t entmtp_tree_attn_paged(const entmtp_bank* bank, int32_t B, co
     wide ? go(paged_attn_kernel<true, false>) : go(paged_attn_kernel<false, false>);
   if (int32_t rc = launch_status("tree_attn_paged launch")) return rc;
   if (!sh.splits) return ENTMTP_OK;
-  const long long blocks = static_cast<long long>(rows_cap) * ((Hq + kMergeHeads - 1) / kMergeHeads);
-  ENTMTP_CHECK_ARG(blocks <= INT32_MAX, ENTMTP_ERANGE, "%d rows of %d heads: too many", rows_cap, Hq);
   hipLaunchKernelGGL(paged_merge_kernel, dim3(static_cast<uint32_t>(blocks)), dim3(32 * kMergeHeads), 0, s, a);
   return launch_status("tree_attn_paged merge launch");
 }

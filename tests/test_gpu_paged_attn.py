@@ -131,9 +131,9 @@ def test_against_64_bits(api, topo, lens, Hq, Hkv, page):
 
 
 OPTIONS = [dict(softcap=3.0), dict(softcap=1024.0), dict(softcap=0.01), dict(window=1), dict(window=2),
-           dict(window=5), dict(window=33), dict(window=64), dict(window=500), dict(window=2 ** 31 - 1), dict(slopes=True), dict(softcap=30.0, window=40),
-           dict(softcap=2.0, window=100, slopes=True), dict(theta=0.0), dict(theta=0.0, softcap=5.0, window=7),
-           dict(theta=0.5), dict(theta=0.5, window=90)]
+           dict(window=5), dict(window=33), dict(window=64), dict(window=500), dict(window=2 ** 31 - 1),
+           dict(slopes=True), dict(softcap=30.0, window=40), dict(softcap=2.0, window=100, slopes=True),
+           dict(theta=0.0), dict(theta=0.0, softcap=5.0, window=7), dict(theta=0.5), dict(theta=0.5, window=90)]
 
 
 @pytest.mark.parametrize("opt", OPTIONS)
@@ -305,6 +305,27 @@ def test_what_is_not_finite_reaches_the_rows_that_see_it(api, bad, which):
     s = c["slots"][node]
     assert (unbits(d["vp" if which == "vt" else "kp"])[s // 16, :, s % 16, 9] != c["vp" if which == "vt" else "kp"][
         s // 16, :, s % 16, 9]).any()
+
+
+@pytest.mark.parametrize("bad", [0x7FC0, 0x7F80, 0xFF80])
+@pytest.mark.parametrize("which", ["vp", "kp"])
+def test_what_is_not_finite_at_the_windows_edge(api, bad, which):
+    """A prefix key or value within the root's window and before its descendants': only rows that see it show it."""
+    t, L, window = 4, 700, 300
+    depth = orc.depths(TREES[t])
+    for pos in (L + 1 - window, L + 2 - window, L + int(max(depth)) - window):
+        c = make(22, [t, 1], [L, 20], 8, 2, 16)
+        sees = np.array([L + d - pos < window for d in depth])
+        assert sees.any() and not sees.all()
+        clean = launch(api, c, window=window)
+        c[which] = c[which].copy()
+        c[which][c["table"][0, pos // 16], :, pos % 16, 9] = bad
+        d = launch(api, c, window=window)
+        got, ref = d["out"].float().cpu().numpy(), clean["out"].float().cpu().numpy()
+        np.testing.assert_array_equal(got[:64][~sees], ref[:64][~sees])
+        np.testing.assert_array_equal(got[64:], ref[64:])
+        if which == "vp" or bad == 0x7FC0:
+            assert np.isnan(got[:64][sees]).all()
 
 
 def test_streams_graphs_and_two_at_once(api):
