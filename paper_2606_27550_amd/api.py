@@ -752,21 +752,58 @@ def kv_compact(path, accept_len, prefix_len: int, k_cache, v_cache, stream=None)
 
 # ------------------------------------------------- serving from a page pool --
 
-def _here(*tensors):
-    """The tensors (None: skipped) lie on the current device: the stream the
-    call launches on belongs to it."""
-    dev = _torch._C._cuda_getDevice()
-    for t in tensors:
-        if t is not None and t.get_device() != dev:
-            raise ValueError(f"a tensor lies on {t.device}, the current device is cuda:{dev}")
+# These calls are as short as their launches at small batches, so what they
+# check of a tensor is one expression, which yields its pointer.
+
+def _device(t, name):
+    """The current device, where all tensors of a call have to lie (its stream
+    belongs to it); t: the first of them, so that there is a device."""
+    _need(isinstance(t, _torch.Tensor) and t.is_cuda, f"{name} must be a torch tensor on the GPU")
+    return _torch._C._cuda_getDevice()
 
 
-def _paged_batch(topo, row_off=None):
-    _dev(topo, "topo", _torch.int32)
-    B = topo.numel()
-    _need(topo.dim() == 1 and 1 <= B <= PAGED_B_MAX, f"topo is [B] with 1 <= B <= {PAGED_B_MAX}")
-    if row_off is not None:
-        _dev(row_off, "row_off", _torch.int32, (B + 1,))
+def _at(t, name, dtype, shape, dev):
+    """Pointer of a contiguous tensor of this type and shape on device dev."""
+    try:
+        if t.dtype is dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _dev(t, name, dtype, shape)
+    raise ValueError(f"{name} lies on {t.device}, the current device is cuda:{dev}")
+
+
+def _dims(t, name, *n):
+    """Shape of a tensor of n dimensions."""
+    shape = getattr(t, "shape", ())
+    _need(len(shape) in n, f"{name} must be a tensor of {' or '.join(map(str, n))} dimensions")
+    return shape
+
+
+def _flat(t, name, dtype, dev):
+    """Pointer and size of a contiguous tensor of any shape that is not empty."""
+    shape = getattr(t, "shape", ())
+    ptr = _at(t, name, dtype, shape, dev)
+    n = t.numel()
+    _need(n >= 1, f"{name} needs at least 1 element")
+    return ptr, n
+
+
+def _scratch(t, name, dev):
+    """Pointer and bytes of a contiguous tensor of any type on device dev."""
+    if isinstance(t, _torch.Tensor) and t.get_device() == dev and t.is_contiguous():
+        return t.data_ptr(), t.nbytes
+    raise ValueError(f"{name} must be a contiguous tensor on the current device, cuda:{dev}")
+
+
+def _stream_on(stream, dev):
+    """Handle of a stream (None: torch's current one on dev)."""
+    return _raw_stream(dev) if stream is None and _raw_stream is not None else _stream(stream)
+
+
+def _paged_batch(topo):
+    B, = _dims(topo, "topo", 1)
+    _need(1 <= B <= PAGED_B_MAX, f"topo is [B] with 1 <= B <= {PAGED_B_MAX}")
     return B
 
 
@@ -777,34 +814,25 @@ def page_map(bank: Bank, topo, prefix_len, block_table, page_size: int, n_pages:
     need are taken from free_pages[:n_free], from its end), row_off int32
     [B + 1] and slot_map int32 [rows_cap] out."""
     i32 = _torch.int32
-    B = _paged_batch(topo, row_off)
-    _dev(prefix_len, "prefix_len", i32, (B,))
-    _dev(status, "status", i32, (B,))
-    _dev(block_table, "block_table", i32)
-    _need(block_table.dim() == 2 and block_table.shape[0] == B, "block_table is [B, max_pages]")
-    _dev(slot_map, "slot_map", i32, min_numel=1)
+    B = _paged_batch(topo)
+    _, max_pages = _dims(block_table, "block_table", 2)
+    dev = _device(topo, "topo")
     _need((free_pages is None) == (n_free is None), "free_pages and n_free go together")
-    if free_pages is not None:
-        _dev(free_pages, "free_pages", i32, min_numel=1)
-        _dev(n_free, "n_free", i32, (1,))
-    _here(topo, prefix_len, block_table, row_off, slot_map, status, free_pages, n_free)
-    _check(lib.entmtp_page_map(bank.handle, B, _p(topo), _p(prefix_len), _p(block_table),
-                               block_table.shape[1], page_size, n_pages, _p(free_pages),
-                               0 if free_pages is None else free_pages.numel(), _p(n_free),
-                               slot_map.numel(), _p(row_off), _p(slot_map), _p(status),
-                               _stream(stream)))
+    free, free_cap = (None, 0) if free_pages is None else _flat(free_pages, "free_pages", i32, dev)
+    slots, rows_cap = _flat(slot_map, "slot_map", i32, dev)
+    _check(lib.entmtp_page_map(bank.handle, B, _at(topo, "topo", i32, (B,), dev),
+                               _at(prefix_len, "prefix_len", i32, (B,), dev),
+                               _at(block_table, "block_table", i32, (B, max_pages), dev), max_pages,
+                               page_size, n_pages, free, free_cap,
+                               None if n_free is None else _at(n_free, "n_free", i32, (1,), dev),
+                               rows_cap, _at(row_off, "row_off", i32, (B + 1,), dev), slots,
+                               _at(status, "status", i32, (B,), dev), _stream_on(stream, dev)))
 
 
 def tree_attn_paged_plan_bytes(bank: Bank, B: int, rows_cap: int, Hq: int, Hkv: int, max_pages: int,
                                page_size: int) -> int:
     return int(lib.entmtp_tree_attn_paged_plan_bytes(bank.handle, B, rows_cap, Hq, Hkv, max_pages,
                                                      page_size))
-
-
-def _scratch(t, name):
-    _need(isinstance(t, _torch.Tensor) and t.is_cuda and t.is_contiguous(),
-          f"{name} must be a contiguous GPU tensor")
-    return t.numel() * t.element_size()
 
 
 def tree_attn_paged_plan(bank: Bank, topo, prefix_len, row_off, status, block_table, page_size: int,
@@ -815,19 +843,18 @@ def tree_attn_paged_plan(bank: Bank, topo, prefix_len, row_off, status, block_ta
     tree_attn_paged_plan_bytes; bad int32 [B] (or None): sequences with a
     prefix page outside the pool."""
     i32 = _torch.int32
-    B = _paged_batch(topo, row_off)
-    _dev(prefix_len, "prefix_len", i32, (B,))
-    _dev(status, "status", i32, (B,))
-    _dev(block_table, "block_table", i32)
-    _need(block_table.dim() == 2 and block_table.shape[0] == B, "block_table is [B, max_pages]")
-    if bad is not None:
-        _dev(bad, "bad", i32, (B,))
-    size = _scratch(plan, "plan")
-    _here(topo, prefix_len, row_off, status, block_table, bad, plan)
-    _check(lib.entmtp_tree_attn_paged_plan(bank.handle, B, _p(topo), _p(prefix_len), _p(row_off),
-                                           _p(status), _p(block_table), block_table.shape[1], page_size,
-                                           n_pages, rows_cap, Hq, Hkv, window, _p(bad), _p(plan), size,
-                                           _stream(stream)))
+    B = _paged_batch(topo)
+    _, max_pages = _dims(block_table, "block_table", 2)
+    dev = _device(topo, "topo")
+    plan_p, size = _scratch(plan, "plan", dev)
+    _check(lib.entmtp_tree_attn_paged_plan(bank.handle, B, _at(topo, "topo", i32, (B,), dev),
+                                           _at(prefix_len, "prefix_len", i32, (B,), dev),
+                                           _at(row_off, "row_off", i32, (B + 1,), dev),
+                                           _at(status, "status", i32, (B,), dev),
+                                           _at(block_table, "block_table", i32, (B, max_pages), dev),
+                                           max_pages, page_size, n_pages, rows_cap, Hq, Hkv, window,
+                                           None if bad is None else _at(bad, "bad", i32, (B,), dev),
+                                           plan_p, size, _stream_on(stream, dev)))
 
 
 def tree_attn_paged_workspace(bank: Bank, B: int, rows_cap: int, Hq: int, Hkv: int, d: int,
@@ -843,52 +870,44 @@ def tree_attn_paged(bank: Bank, plan, q, k_tree, v_tree, k_pool, v_pool, block_t
     [n_pages, Hkv, page_size, d] (bf16), block_table int32 [B, max_pages],
     slot_map int32 [rows_cap]; plan of the same sizes and window; slopes fp32
     [Hq] or None."""
-    bf = _torch.bfloat16
-    _need(q.dim() == 3 and k_pool.dim() == 4 and block_table.dim() == 2,
-          "q is 3-D, pools are 4-D, block_table is 2-D")
-    rows, Hq, d = q.shape
-    n_pages, Hkv, page, _ = k_pool.shape
-    B, max_pages = block_table.shape
-    _dev(q, "q", bf)
-    _dev(k_tree, "k_tree", bf, (rows, Hkv, d))
-    _dev(v_tree, "v_tree", bf, (rows, Hkv, d))
-    _dev(k_pool, "k_pool", bf, (n_pages, Hkv, page, d))
-    _dev(v_pool, "v_pool", bf, (n_pages, Hkv, page, d))
-    _dev(out, "out", bf, (rows, Hq, d))
-    _dev(block_table, "block_table", _torch.int32)
-    _dev(slot_map, "slot_map", _torch.int32, (rows,))
-    if slopes is not None:
-        _dev(slopes, "slopes", _torch.float32, (Hq,))
-    size = _scratch(plan, "plan")
-    ws_size = 0 if workspace is None else _scratch(workspace, "workspace")
-    _here(plan, q, k_tree, v_tree, k_pool, v_pool, block_table, slot_map, out, workspace, slopes)
-    _check(lib.entmtp_tree_attn_paged(bank.handle, B, _p(plan), size, _p(q), _p(k_tree), _p(v_tree),
-                                      _p(k_pool), _p(v_pool), n_pages, page, _p(block_table), max_pages,
-                                      _p(slot_map), rows, Hq, Hkv, d, scale, rope_theta, softcap, window,
-                                      _p(slopes), _p(out), _p(workspace), ws_size, _stream(stream)))
+    bf, i32 = _torch.bfloat16, _torch.int32
+    rows, Hq, d = _dims(q, "q", 3)
+    n_pages, Hkv, page, _ = _dims(k_pool, "k_pool", 4)
+    B, max_pages = _dims(block_table, "block_table", 2)
+    dev = _device(q, "q")
+    wide, narrow, pool = (rows, Hq, d), (rows, Hkv, d), (n_pages, Hkv, page, d)
+    plan_p, size = _scratch(plan, "plan", dev)
+    ws, ws_size = (None, 0) if workspace is None else _scratch(workspace, "workspace", dev)
+    _check(lib.entmtp_tree_attn_paged(bank.handle, B, plan_p, size, _at(q, "q", bf, wide, dev),
+                                      _at(k_tree, "k_tree", bf, narrow, dev),
+                                      _at(v_tree, "v_tree", bf, narrow, dev),
+                                      _at(k_pool, "k_pool", bf, pool, dev),
+                                      _at(v_pool, "v_pool", bf, pool, dev), n_pages, page,
+                                      _at(block_table, "block_table", i32, (B, max_pages), dev), max_pages,
+                                      _at(slot_map, "slot_map", i32, (rows,), dev), rows, Hq, Hkv, d,
+                                      scale, rope_theta, softcap, window,
+                                      None if slopes is None else _at(slopes, "slopes", _torch.float32, (Hq,), dev),
+                                      _at(out, "out", bf, wide, dev), ws, ws_size, _stream_on(stream, dev)))
 
 
 def kv_compact_paged(path, accept_len, row_off, slot_map, k_pool, v_pool, stream=None) -> None:
     """path [B, path_capacity] and accept_len [B]; row_off and slot_map of the
     step's page_map; pools [n_pages, Hkv, page_size, d] (one layer) or
     [n_layers, n_pages, Hkv, page_size, d] (bf16)."""
-    i32 = _torch.int32
-    _dev(path, "path", i32)
-    _need(path.dim() == 2 and 1 <= path.shape[0] <= PAGED_B_MAX, "path is [B, path_capacity]")
-    B = path.shape[0]
-    _dev(accept_len, "accept_len", i32, (B,))
-    _dev(row_off, "row_off", i32, (B + 1,))
-    _dev(slot_map, "slot_map", i32, min_numel=1)
-    _need(k_pool.dim() in (4, 5), "pools are 4-D or 5-D")
-    _dev(k_pool, "k_pool", _torch.bfloat16)
-    _dev(v_pool, "v_pool", _torch.bfloat16, k_pool.shape)
-    _here(path, accept_len, row_off, slot_map, k_pool, v_pool)
-    n_layers = 1 if k_pool.dim() == 4 else k_pool.shape[0]
-    n_pages, Hkv, page, d = k_pool.shape[-4:]
-    _check(lib.entmtp_kv_compact_paged(B, _p(path), path.shape[1], _p(accept_len), _p(row_off),
-                                       _p(slot_map), slot_map.numel(), _p(k_pool), _p(v_pool),
-                                       n_layers, n_pages * Hkv * page * d, n_pages, Hkv, page, d,
-                                       _stream(stream)))
+    i32, bf = _torch.int32, _torch.bfloat16
+    B, path_cap = _dims(path, "path", 2)
+    _need(1 <= B <= PAGED_B_MAX, f"path is [B, path_capacity] with 1 <= B <= {PAGED_B_MAX}")
+    shape = _dims(k_pool, "pools", 4, 5)
+    n_pages, Hkv, page, d = shape[-4:]
+    dev = _device(path, "path")
+    slots, rows = _flat(slot_map, "slot_map", i32, dev)
+    _check(lib.entmtp_kv_compact_paged(B, _at(path, "path", i32, (B, path_cap), dev), path_cap,
+                                       _at(accept_len, "accept_len", i32, (B,), dev),
+                                       _at(row_off, "row_off", i32, (B + 1,), dev), slots, rows,
+                                       _at(k_pool, "k_pool", bf, shape, dev),
+                                       _at(v_pool, "v_pool", bf, shape, dev),
+                                       1 if len(shape) == 4 else shape[0], n_pages * Hkv * page * d,
+                                       n_pages, Hkv, page, d, _stream_on(stream, dev)))
 
 
 def logit_adjust_workspace(rows: int, V: int) -> int:
@@ -904,71 +923,59 @@ def logit_adjust(bank: Bank, topo, row_off, draft_tokens, logits, params, out, e
     bias_idx int32 [B], mask int32 [m, words] (bits) with mask_idx int32
     [rows]."""
     i32, f32 = _torch.int32, _torch.float32
-    B = _paged_batch(topo, row_off)
-    _need(logits.dim() == 2, "logits are [rows, V]")
-    rows, V = logits.shape
-    _dev(logits, "logits", f32)
-    _dev(draft_tokens, "draft_tokens", i32, (rows,))
-    _dev(params, "params", f32, (B, 4))
-    if out is not None:
-        _dev(out, "out", f32, (rows, V))
-    for name, t, dt in (("entropy", entropy, f32), ("top1p", top1p, f32), ("argmax", argmax, i32)):
-        if t is not None:
-            _dev(t, name, dt, (rows,))
-    if history is not None:
-        _dev(history, "history", i32, (B, V))
+    B = _paged_batch(topo)
+    rows, V = _dims(logits, "logits", 2)
+    dev = _device(logits, "logits")
     _need((bias is None) == (bias_idx is None), "bias and bias_idx go together")
-    if bias is not None:
-        _dev(bias, "bias", f32)
-        _need(bias.dim() == 2 and bias.shape[1] == V, "bias is [n, V]")
-        _dev(bias_idx, "bias_idx", i32, (B,))
     _need((mask is None) == (mask_idx is None), "mask and mask_idx go together")
-    if mask is not None:
-        _dev(mask, "mask", i32)
-        _need(mask.dim() == 2, "mask is [m, words]")
-        _dev(mask_idx, "mask_idx", i32, (rows,))
-    ws_size = 0 if workspace is None else _scratch(workspace, "workspace")
-    _here(topo, row_off, draft_tokens, logits, params, out, entropy, top1p, argmax, workspace, history,
-          bias, bias_idx, mask, mask_idx)
-    _check(lib.entmtp_logit_adjust(bank.handle, B, _p(topo), _p(row_off), rows, _p(draft_tokens),
-                                   _p(logits), V, _p(params), _p(history), _p(bias),
-                                   0 if bias is None else bias.shape[0], _p(bias_idx), _p(mask),
-                                   0 if mask is None else mask.shape[0],
-                                   0 if mask is None else mask.shape[1], _p(mask_idx), _p(out),
-                                   _p(entropy), _p(top1p), _p(argmax), _p(workspace),
-                                   ws_size, _stream(stream)))
+    n_bias = 0 if bias is None else _dims(bias, "bias", 2)[0]
+    n_masks, words = (0, 0) if mask is None else _dims(mask, "mask", 2)
+    ws, ws_size = (None, 0) if workspace is None else _scratch(workspace, "workspace", dev)
+    _check(lib.entmtp_logit_adjust(
+        bank.handle, B, _at(topo, "topo", i32, (B,), dev), _at(row_off, "row_off", i32, (B + 1,), dev),
+        rows, _at(draft_tokens, "draft_tokens", i32, (rows,), dev),
+        _at(logits, "logits", f32, (rows, V), dev), V, _at(params, "params", f32, (B, 4), dev),
+        None if history is None else _at(history, "history", i32, (B, V), dev),
+        None if bias is None else _at(bias, "bias", f32, (n_bias, V), dev), n_bias,
+        None if bias is None else _at(bias_idx, "bias_idx", i32, (B,), dev),
+        None if mask is None else _at(mask, "mask", i32, (n_masks, words), dev), n_masks, words,
+        None if mask is None else _at(mask_idx, "mask_idx", i32, (rows,), dev),
+        None if out is None else _at(out, "out", f32, (rows, V), dev),
+        None if entropy is None else _at(entropy, "entropy", f32, (rows,), dev),
+        None if top1p is None else _at(top1p, "top1p", f32, (rows,), dev),
+        None if argmax is None else _at(argmax, "argmax", i32, (rows,), dev),
+        ws, ws_size, _stream_on(stream, dev)))
 
 
 def token_history_prompt(tokens, tok_off, history, stream=None) -> None:
     """history int32 [B, V]: marks the prompts' tokens, sequence b's at
     tokens[tok_off[b]:tok_off[b + 1]] (int32)."""
-    _dev(history, "history", _torch.int32)
-    _need(history.dim() == 2 and 1 <= history.shape[0] <= PAGED_B_MAX, "history is [B, V]")
-    B, V = history.shape
-    _dev(tokens, "tokens", _torch.int32)
-    _dev(tok_off, "tok_off", _torch.int32, (B + 1,))
-    _here(tokens, tok_off, history)
-    _check(lib.entmtp_token_history_prompt(_p(tokens), tokens.numel(), _p(tok_off), B, V, _p(history),
-                                           _stream(stream)))
+    i32 = _torch.int32
+    B, V = _dims(history, "history", 2)
+    _need(1 <= B <= PAGED_B_MAX, f"history is [B, V] with 1 <= B <= {PAGED_B_MAX}")
+    n, = _dims(tokens, "tokens", 1)
+    dev = _device(history, "history")
+    _check(lib.entmtp_token_history_prompt(_at(tokens, "tokens", i32, (n,), dev), n,
+                                           _at(tok_off, "tok_off", i32, (B + 1,), dev), B, V,
+                                           _at(history, "history", i32, (B, V), dev),
+                                           _stream_on(stream, dev)))
 
 
 def token_history_accept(row_off, draft_tokens, path, accept_len, bonus, history, stream=None) -> None:
     """history int32 [B, V]: counts the accepted drafts (path [B,
     path_capacity], accept_len [B]) and the bonus tokens [B] of a step."""
     i32 = _torch.int32
-    _dev(history, "history", i32)
-    _need(history.dim() == 2 and 1 <= history.shape[0] <= PAGED_B_MAX, "history is [B, V]")
-    B, V = history.shape
-    _dev(row_off, "row_off", i32, (B + 1,))
-    _dev(draft_tokens, "draft_tokens", i32, min_numel=1)
-    _dev(path, "path", i32)
-    _need(path.dim() == 2 and path.shape[0] == B, "path is [B, path_capacity]")
-    _dev(accept_len, "accept_len", i32, (B,))
-    _dev(bonus, "bonus", i32, (B,))
-    _here(row_off, draft_tokens, path, accept_len, bonus, history)
-    _check(lib.entmtp_token_history_accept(B, _p(row_off), _p(draft_tokens), draft_tokens.numel(),
-                                           _p(path), path.shape[1], _p(accept_len), _p(bonus), V,
-                                           _p(history), _stream(stream)))
+    B, V = _dims(history, "history", 2)
+    _need(1 <= B <= PAGED_B_MAX, f"history is [B, V] with 1 <= B <= {PAGED_B_MAX}")
+    _, path_cap = _dims(path, "path", 2)
+    dev = _device(history, "history")
+    tok, rows = _flat(draft_tokens, "draft_tokens", i32, dev)
+    _check(lib.entmtp_token_history_accept(B, _at(row_off, "row_off", i32, (B + 1,), dev), tok, rows,
+                                           _at(path, "path", i32, (B, path_cap), dev), path_cap,
+                                           _at(accept_len, "accept_len", i32, (B,), dev),
+                                           _at(bonus, "bonus", i32, (B,), dev), V,
+                                           _at(history, "history", i32, (B, V), dev),
+                                           _stream_on(stream, dev)))
 
 
 def ladder_next(rung: int, n_rungs: int, s: float, tau_on: float, tau_off: float) -> int:
