@@ -86,6 +86,16 @@ __host__ __device__ inline int first_pos(int L, int window) {
   return window > 0 && L >= window ? L + 1 - window : 0;
 }
 
+// What the last split's part of the tree costs beyond its blocks, in prefix
+// blocks: a table of fp64 angles and, for each of the ntree blocks with tree
+// keys, their rotation and staging through registers (2.7 us against 0.9 at 128
+// nodes).  One 128-node tree at 8192: 34.7 us, 39.7 with one block more per tree
+// block, 39.2 with two fewer; four mixed trees up to 16384 79.3, 84 with two fewer.
+__host__ __device__ inline int paged_tree_extra(int nb, int ntree, int ns) {
+  const int extra = 2 + 3 * ntree, share = nb / ns;
+  return extra < share ? extra : share;   // (the last split keeps a block)
+}
+
 // ------------------------------------------------------------------ plan --
 
 struct PlanArgs {
@@ -225,7 +235,7 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs p) {
   const PagedTree& tree = p.trees.t[s_tree];
   const int sns = s_seq.nsplit, sblk = s_nb0;
   const int snb = (sL + s_seq.T + KB - 1) / KB - sblk, sqg = query_groups(s_seq.rows_pad / kQTile);
-  const int extra = sT > 0 ? tree_extra(snb, sL - sblk * KB, sns) : 0;
+  const int extra = sT > 0 ? paged_tree_extra(snb, snb - (sL / KB - sblk), sns) : 0;
   PlanItem* const list = reinterpret_cast<PlanItem*>(p.plan + p.items_at) + s_item0;
   // the query groups of one (head, split) at a distance of eight: workgroups
   // go to the XCDs in turn, so they share an L2
