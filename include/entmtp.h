@@ -498,10 +498,11 @@ int32_t entmtp_kv_compact_batched_device(int32_t B, const int32_t* path, int32_t
 /*
  * The pool of one layer is k_pool / v_pool [n_pages][Hkv][page_size][d] bf16
  * (page_size 16, 32, 64, 128 or 256, n_pages * page_size < 2^31).  Row b of
- * block_table [B][max_pages] (device int32) names the pages of sequence b in
- * order: position p lies in slot table[b][p / page_size] * page_size +
- * p % page_size of the pool; entries below zero hold no page.  A batch has up
- * to ENTMTP_PAGED_B_MAX sequences, the bank up to 32 trees.  The order of one
+ * block_table [B][max_pages] (device int32, max_pages * page_size < 2^31 -
+ * 1024) names the pages of sequence b in order: position p lies in slot
+ * table[b][p / page_size] * page_size + p % page_size of the pool; entries
+ * below zero hold no page.  A batch has up to ENTMTP_PAGED_B_MAX sequences,
+ * the bank up to 32 trees.  The order of one
  * step is
  *   entmtp_page_map              rows, slots and pages of the step's trees
  *   entmtp_tree_attn_paged_plan  the attention's work list, for all layers

@@ -237,6 +237,9 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs p) {
   const int snb = (sL + s_seq.T + KB - 1) / KB - sblk, sqg = query_groups(s_seq.rows_pad / kQTile);
   const int extra = sT > 0 ? paged_tree_extra(snb, snb - (sL / KB - sblk), sns) : 0;
   PlanItem* const list = reinterpret_cast<PlanItem*>(p.plan + p.items_at) + s_item0;
+  // where split c begins: c (snb + extra) / sns, without the product's 33 bits
+  const int share = (snb + extra) / sns, rest = (snb + extra) % sns;
+  auto begin = [&](int c) { return c * share + c * rest / sns; };
   // the query groups of one (head, split) at a distance of eight: workgroups
   // go to the XCDs in turn, so they share an L2
   for (int i = tid; i < s_len; i += kPlanThreads) {
@@ -254,8 +257,8 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs p) {
     it.qg = qg;
     it.split = c;
     it.nsplit = sns;
-    it.blk_lo = sblk + split_begin(c, sns, snb, extra);
-    it.blk_hi = sblk + split_begin(c + 1, sns, snb, extra);
+    it.blk_lo = sblk + begin(c);
+    it.blk_hi = sblk + (c + 1 < sns ? begin(c + 1) : snb);
     it.rows_pad = s_seq.rows_pad;
     it.part_lo = static_cast<uint32_t>(s_seq.part_off);
     it.part_hi = static_cast<uint32_t>(s_seq.part_off >> 32);

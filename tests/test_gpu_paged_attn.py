@@ -368,6 +368,31 @@ def test_streams_graphs_and_two_at_once(api):
     check(two, b, window=300)
 
 
+def test_two_graphs_of_one_workspace(api):
+    """Two captured batches share a workspace and replay in turn, an eager call of a third between them."""
+    cs = [make(24, [4, 2], [900, 300], 8, 2, 16), make(25, [5, 0, 1], [400, 2000, 0], 8, 4, 32), make(26, [6], [3000], 4, 2, 64)]
+    ds = [launch(api, c, run=False) for c in cs]
+    ws = torch.empty(max(d["ws"].numel() for d in ds), dtype=torch.uint8, device="cuda")
+    graphs = []
+    for d in ds:
+        d["ws"] = ws
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            d["plan_call"]()
+            d["attend"]()
+    for order in ((0, 1, 1, 0), (1, 0, 0, 1)):
+        for d in ds:
+            d["out"].fill_(7)
+        for k in order:
+            graphs[k].replay()
+            ds[2]["plan_call"]()
+            ds[2]["attend"]()
+        torch.cuda.synchronize()
+        for c, d in zip(cs, ds):
+            check(c, d)
+
+
 def test_results_do_not_depend_on_the_run(api):
     c = make(18, [4, 2, 0, 5], [900, 30, 5000, 111], 8, 2, 16)
     ref = unbits(launch(api, c)["out"])
@@ -401,6 +426,38 @@ def test_offsets_past_32_bits(api):
     api.kv_compact_paged(path, a, d["off"], slots, big["kp"], big["vp"])
     for k in big:
         np.testing.assert_array_equal(unbits(big[k][-c["n_pages"]:]), want[k])
+
+
+def test_positions_near_31_bits(api):
+    """With a window and no rotation a sequence far along gives what it gives early on; so do its slots."""
+    c = make(23, [2], [700], 8, 2, 256)
+    T, window = len(TREES[2]), 300
+    near = launch(api, c, theta=0.0, window=window)
+    pages = (2 ** 31 - 1 - 1024) // 256      # the most there may be
+    shift = pages - 4                        # (the tree lies in pages 2 .. 3 of the table)
+    table = torch.full((1, pages), -1, dtype=torch.int32, device="cuda")
+    table[0, shift:shift + 3] = i32(c["table"][0, :3])
+    d = launch(api, c, run=False)
+    L, bank = i32([700 + 256 * shift]), d["bank"]
+    off, slots, status = (torch.zeros(n, dtype=torch.int32, device="cuda") for n in (2, T, 1))
+    say("tree_attn_paged at position", int(L))
+    api.page_map(bank, d["topo"], L, table, 256, c["n_pages"], off, slots, status)
+    assert host(status)[0] == po.OK
+    np.testing.assert_array_equal(host(slots), c["slots"])
+    shape = (T, 8, 2)
+    plan = torch.empty(api.tree_attn_paged_plan_bytes(bank, 1, *shape, pages, 256), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(api.tree_attn_paged_workspace(bank, 1, *shape, D, pages, 256), dtype=torch.uint8, device="cuda")
+    api.tree_attn_paged_plan(bank, d["topo"], L, off, status, table, 256, c["n_pages"], *shape, plan, window=window,
+                             bad=d["bad"])
+    api.tree_attn_paged(bank, plan, d["q"], d["kt"], d["vt"], d["kp"], d["vp"], table, slots, SCALE, 0.0, d["out"], ws,
+                        window=window)
+    assert host(d["bad"])[0] == 0
+    for k in ("out", "kp", "vp"):
+        np.testing.assert_array_equal(unbits(d[k]), unbits(near[k]))
+    # every position there can be, in one page: the work list's ranges (the attention is not run)
+    table.zero_()
+    api.tree_attn_paged_plan(bank, d["topo"], L, off, status, table, 256, 1, *shape, plan, bad=d["bad"])
+    assert host(d["bad"])[0] == 0
 
 
 def test_refusals(api):
