@@ -354,7 +354,6 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
   __shared__ __attribute__((aligned(16))) uint8_t slot2[kRingSlot];
   __shared__ __attribute__((aligned(16))) uint8_t slot3[kRingSlot];
   __shared__ uint8_t s_depth[ENTMTP_T_MAX];
-  __shared__ int s_any[2][4];
   __shared__ __attribute__((aligned(8))) uint8_t s_odd[2][KB][8];   // tree values that are not finite, by key and chunk pair
   uint8_t* const ring[4] = {slot0, slot1, slot2, slot3};
   static_assert(kRing == 4, "the ring's slots");
@@ -428,6 +427,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
   struct TreeRegs {
     u32x4 k0, k1, v0, v1;
     int slot;
+    bool there;
   };
   const int trow = tid >> 3, tcc = tid & 7;
   auto tree_key = [&](int i) { return min((blk_lo + min(i, nb - 1)) * KB + trow, nkeys - 1); };
@@ -443,10 +443,10 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
   auto tree_load = [&](TreeRegs& t, int i) {
     const int key = tree_key(i);
     const uint16_t *kp, *vp;
-    bool there = true;
+    t.there = true;
     if (key < L) {
-      there = static_cast<unsigned>(t.slot) < static_cast<unsigned>(p.n_pages) && key >= w_lo;
-      const size_t off = (((static_cast<size_t>(there ? t.slot : 0) * p.Hkv + g) << p.shift) + (key & (P - 1))) * HD;
+      t.there = static_cast<unsigned>(t.slot) < static_cast<unsigned>(p.n_pages) && key >= w_lo;
+      const size_t off = (((static_cast<size_t>(t.there ? t.slot : 0) * p.Hkv + g) << p.shift) + (key & (P - 1))) * HD;
       kp = p.kp + off;
       vp = p.vp + off;
     } else {
@@ -460,14 +460,13 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
     t.k1 = *reinterpret_cast<const u32x4*>(kp + HD / 2);
     t.v0 = *reinterpret_cast<const u32x4*>(vp);
     t.v1 = *reinterpret_cast<const u32x4*>(vp + HD / 2);
-    if (!there) t.k0 = t.k1 = t.v0 = t.v1 = u32x4{0u, 0u, 0u, 0u};
   };
-  // Returns whether a value was not finite: it is staged as zero (a zero
-  // weight would make it a NaN in every row) and noted, and the rows that see
-  // its key become NaN.
+  // A value that is not finite is staged as zero (a zero weight would make it a
+  // NaN in every row) and noted, and the rows that see its key become NaN.
   auto tree_stage = [&](uint8_t* slot, TreeRegs& t, int i, int buf) {
     const int key = (blk_lo + i) * KB + trow;
     bool odd = false;
+    if (!t.there) t.k0 = t.k1 = t.v0 = t.v1 = u32x4{0u, 0u, 0u, 0u};   // (here: the loads' first use)
     if (key >= L && key < nkeys) {
       if (rope) rope_pairs(t.k0, t.k1, tab64(s_depth[key - L]) + 8 * tcc, tcc & 7);
       if (t.slot >= 0 && t.slot < p.n_pages << p.shift) {
@@ -491,7 +490,6 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
     *reinterpret_cast<u32x4*>(row + (((tcc + 8) ^ k_swz(trow)) << 4)) = t.k1;
     *reinterpret_cast<u32x4*>(row + kRingK + ((tcc ^ v_swz(trow)) << 4)) = t.v0;
     *reinterpret_cast<u32x4*>(row + kRingK + (((tcc + 8) ^ v_swz(trow)) << 4)) = t.v1;
-    return odd;
   };
 
   double freq = p.freq[tid % kRopePairs];
@@ -612,33 +610,40 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
     }
   };
   auto key_of = [&](int r) { return 8 * (r >> 2) + 4 * lh + (r & 3); };   // accumulator r's key of the block
-  auto odd_key = [&](int buf, int n) {
-    const uint2 f = *reinterpret_cast<const uint2*>(s_odd[buf][n]);
-    return (f.x | f.y) != 0;
+  // the keys noted in buffer buf, a bit each
+  auto odd_keys = [&](int buf) {
+    const uint2 f = *reinterpret_cast<const uint2*>(s_odd[buf][li]);
+    return static_cast<uint32_t>(__ballot((f.x | f.y) != 0u));
+  };
+  // Keeps the scores of the keys in vis (a bit each), -inf elsewhere; a row
+  // that sees a key in odd becomes NaN.
+  auto keep = [&](f32x16& sacc, float& l, uint32_t vis, uint32_t odd) {
+    if ((vis & odd) != 0u) l = NAN;
+    vis >>= 4 * lh;   // bit 8 (r / 4) + r % 4 is accumulator r's key
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int m = static_cast<int>(vis << (31 - (8 * (r >> 2) + (r & 3)))) >> 31;
+      sacc[r] = __builtin_bit_cast(float, (m & __builtin_bit_cast(int, static_cast<float>(sacc[r]))) | (~m & INT32_C(-0x800000)));
+    }
   };
   // Block i's softmax (lazily raised max) and O^T += V^T P^T from its slot;
   // prefix: every key of the block is in the prefix; ahead: the next block's
   // scores, which move with the reference they started from.
-  auto attend = [&](int i, const uint8_t* slot, f32x16& sacc, f32x16& ahead, auto prefix, auto odd_of) {
+  auto attend = [&](int i, const uint8_t* slot, f32x16& sacc, f32x16& ahead, auto prefix) {
     float bmax = -INFINITY;
     const int kb = (blk_lo + i) * KB;
     if constexpr (decltype(prefix)::value) {
       if constexpr (MOD) {
         bend(sacc, [&](int r) { return qpos - (kb + key_of(r)); });
         if (kb < w_hi) {
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int n = key_of(r);
-            const bool vis = kb + n >= w_row;
-            sacc[r] = vis ? sacc[r] : -INFINITY;
-            if (vis && odd_key(i & 1, n)) l_run = NAN;
-          }
+          const int out = min(max(w_row - kb, 0), KB);   // keys before the row's window
+          keep(sacc, l_run, static_cast<uint32_t>(0xFFFFFFFFull << out), odd_keys(i & 1));
         }
       }
 #pragma unroll
       for (int r = 0; r < 16; ++r) bmax = fmaxf(bmax, sacc[r]);
     } else {
-      uint32_t win = 0xFFFFFFFFu;
+      uint32_t vis;
       const int rel = kb - L;
       auto word = [&](int w) {   // (w is uniform)
         uint32_t m = 0u;
@@ -648,27 +653,28 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
       };
       if (rel < 0) {
         const int npre = -rel;
-        win = (0xFFFFFFFFu >> (32 - npre)) | (mlo[0] << npre);
+        vis = (0xFFFFFFFFu >> (32 - npre)) | (mlo[0] << npre);
       } else {
         const int wi = rel >> 5, sh = rel & 31;
         const uint32_t lo = word(wi), hi = word(wi + 1);
-        win = sh ? (lo >> sh) | (hi << (32 - sh)) : lo;
+        vis = sh ? (lo >> sh) | (hi << (32 - sh)) : lo;
       }
-      // (a tree key's position is that of its depth)
-      auto pos_k = [&](int r) {
-        const int j = kb + key_of(r) - L;
-        return j < 0 ? kb + key_of(r) : L + s_depth[min(j, ENTMTP_T_MAX - 1)];
-      };
-      if constexpr (MOD) bend(sacc, [&](int r) { return qpos - pos_k(r); });
+      if (nkeys - kb < KB) vis &= (1u << (nkeys - kb)) - 1u;
+      if constexpr (MOD) {
+        // (a tree key's position is that of its depth)
+        auto pos_k = [&](int n) {
+          const int j = kb + n - L;
+          return j < 0 ? kb + n : L + s_depth[min(j, ENTMTP_T_MAX - 1)];
+        };
+        bend(sacc, [&](int r) { return qpos - pos_k(key_of(r)); });
+        if (min(kb, L) < w_hi) {   // (else the window holds the block)
+          for (int n = 0; n < KB; ++n)
+            if (pos_k(n) < w_row) vis &= ~(1u << n);
+        }
+      }
+      keep(sacc, l_run, vis, odd_keys((i - np) & 1));
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int n = key_of(r);
-        bool vis = ((win >> n) & 1u) && (kb + n < nkeys);
-        if constexpr (MOD) vis = vis && pos_k(r) >= w_row;
-        sacc[r] = vis ? sacc[r] : -INFINITY;
-        bmax = fmaxf(bmax, sacc[r]);
-        if (odd_of(n) && vis) l_run = NAN;
-      }
+      for (int r = 0; r < 16; ++r) bmax = fmaxf(bmax, sacc[r]);
     }
     bmax = max_halves(bmax);
     // bent scores are held against m_run here, the others are relative to it
@@ -724,7 +730,6 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
       }
     }
   };
-  auto none = [](int) { return false; };
 
   // The prefix's blocks.  Step i takes the scores of block i + 1 ahead of
   // block i's softmax, so that a wave has products to issue beside its
@@ -772,7 +777,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
       if (live) {
         f32x16& cur = k & 1 ? sb : sa;
         scores(ring[(k + 1) % kRing], k & 1 ? sa : sb);
-        attend(i0 + k, ring[k], cur, k & 1 ? sa : sb, std::true_type{}, none);
+        attend(i0 + k, ring[k], cur, k & 1 ? sa : sb, std::true_type{});
       }
     }
   }
@@ -786,7 +791,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
       if (i0 + k < np) {
         f32x16& cur = k & 1 ? sb : sa;
         if (k + 1 < kRing - 1) scores(ring[k + 1], k & 1 ? sa : sb);
-        attend(i0 + k, ring[k], cur, k & 1 ? sa : sb, std::true_type{}, none);
+        attend(i0 + k, ring[k], cur, k & 1 ? sa : sb, std::true_type{});
       }
   }
 
@@ -802,9 +807,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
     for (int i = np; i < nb; ++i) {
       const int buf = (i - np) & 1;
       uint8_t* const slot = buf ? slot1 : slot0;
-      const bool odd = tree_stage(slot, tregs, i, buf);
-      if (lane == 0) s_any[buf][wave] = 0;
-      if (__any(odd) && lane == 0) s_any[buf][wave] = 1;
+      tree_stage(slot, tregs, i, buf);
       if (i + 1 < nb) {   // (in flight during this block's products: the barrier waits for the LDS alone)
         tree_find(tregs, i + 1);
         tree_load(tregs, i + 1);
@@ -812,9 +815,8 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
       wait_lds();
       stage_barrier();
       if (live) {
-        const bool any = (s_any[buf][0] | s_any[buf][1] | s_any[buf][2] | s_any[buf][3]) != 0;
         scores(slot, sa);
-        attend(i, slot, sa, sb, std::false_type{}, [&](int n) { return any && odd_key(buf, n); });
+        attend(i, slot, sa, sb, std::false_type{});
       }
     }
   }
