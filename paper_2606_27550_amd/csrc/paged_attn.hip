@@ -20,9 +20,20 @@
 //    number comes by a scalar load one block ahead and costs no wait.  Pages
 //    outside the pool read as zeros (an empty buffer), never out of bounds.
 //  - Long prefixes split up to 128 ways (few heads and one sequence still fill
-//    the chip), and a wavefront merges a row's partials.
+//    the chip), and half a wavefront merges a row's partials.
+//  - The queries carry the scale, and a block's products start from minus the
+//    row's reference, so they leave the matrix pipe as exponents of two.
 //  - The score cap, distance bias and window live in an instance of their own;
 //    a window also cuts the key blocks that the plan hands out.
+// Few rows are HBM bound: 32 single tokens at 8192 (32:8 heads) take 188 us,
+// 5.7 TB/s; 26 nodes at 131000 115 us, 4.7.  Large trees are bound by the issue
+// of both pipes: a wave spends 16 products of 32 cycles and about 60 vector
+// instructions and 16 exponentials on a block, 500 cycles each, and two waves a
+// SIMD (512 registers between them, most of them the outputs and queries) hide
+// a third of it: eight 128-node trees at 8192 take 162 us, 0.85 PFLOP/s (a large
+// product reaches 1.31); 208 with a score cap, whose tanh adds two
+// transcendentals a score.  What is smaller is a chain of round trips: one token
+// at 63 takes 7.7 us.
 #include <algorithm>
 #include <type_traits>
 
@@ -128,6 +139,9 @@ __device__ __forceinline__ T scan_threads(T v, T* part) {
   return v;
 }
 
+// Bound by its chain of loads, scans and barriers: one sequence takes 6 us, 256
+// take 10 (each workgroup weighs the whole batch, which is cheaper than a second
+// launch or a wait between workgroups).
 __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs p) {
   static_assert(kPlanThreads == 256 && kTargets == 16, "four wavefronts; 16 threads to a candidate");
   __shared__ int s_nb[kPagedSeqs], s_H[kPagedSeqs];
@@ -865,6 +879,9 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
 // splits' partial outputs, the first kMergeAhead of them requested with the
 // (max, sum) pairs (one memory round trip), later ones kMergeAhead at a time.
 // The row's sequence is found by scalar loads: its number, then its record.
+// Four round trips and little data: 26 rows of 32 heads in 64 splits take 10 us
+// with the launch, 512 rows in four splits 9.  (8 partials ahead cost another
+// round trip at 64 splits; 32 leave fewer wavefronts a CU where rows are many.)
 constexpr int kMergeHeads = 8;
 constexpr int kMergeAhead = 16;
 constexpr int kMergeLanes = kPagedSplits / 32;   // (max, sum) pairs a lane
