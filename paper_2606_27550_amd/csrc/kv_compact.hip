@@ -160,11 +160,11 @@ __global__ __launch_bounds__(kCompactThreads) void kv_compact_paged_kernel(Compa
     return reinterpret_cast<u32x4*>(mine + ((page * p.Hkv << p.shift) + (slot & ((1 << p.shift) - 1))) * p.d);
   };
   u32x4 val[ROWS];
+  // (four rows at a time without a branch between their loads: a row that does
+  // not move reads slot 0)
 #pragma unroll
-  for (int k = 0; k < ROWS; ++k) {
-    const int s = __builtin_amdgcn_readlane(src, k);
-    if (s >= 0 && live) val[k] = *at(s);
-  }
+  for (int k = 0; k < ROWS; ++k)
+    if ((k / 4 == 0 || k / 4 * 4 <= a) && live) val[k] = *at(max(__builtin_amdgcn_readlane(src, k), 0));
 #pragma unroll
   for (int k = 0; k < ROWS; ++k)
     if (__builtin_amdgcn_readlane(src, k) >= 0 && live) *at(__builtin_amdgcn_readlane(dst, k)) = val[k];

@@ -874,22 +874,26 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
 
 // ----------------------------------------------------------------- merge --
 
-// A workgroup takes eight query heads of a tree row, a half-wavefront each: lane
-// c reads the (max, sum) of splits c, c + 32, .., every lane four dims of the
-// splits' partial outputs, the first kMergeAhead of them requested with the
-// (max, sum) pairs (one memory round trip), later ones kMergeAhead at a time.
-// The row's sequence is found by scalar loads: its number, then its record.
-// Four round trips and little data: 26 rows of 32 heads in 64 splits take 10 us
-// with the launch, 512 rows in four splits 9.  (8 partials ahead cost another
-// round trip at 64 splits; 32 leave fewer wavefronts a CU where rows are many.)
-constexpr int kMergeHeads = 8;
+// LANES threads (half a wavefront or a whole one) take a query head of a tree
+// row: lane c reads the (max, sum) of splits c, c + LANES, .., and each 32 lanes
+// hold the head's dims, four a lane, of kMergeAhead splits at a time -- a whole
+// wavefront's halves of 16 splits each, summed up at the end.  The first partial
+// outputs are requested with the (max, sum) pairs.  The row's sequence is found
+// by scalar loads: its number, then its record.
+// Round trips and little data: 512 rows of 32 heads in four splits take 9 us with
+// the launch.
+constexpr int kMergeThreads = 256;
 constexpr int kMergeAhead = 16;
-constexpr int kMergeLanes = kPagedSplits / 32;   // (max, sum) pairs a lane
 
-__global__ __launch_bounds__(32 * kMergeHeads) void paged_merge_kernel(PagedArgs p) {
-  const int groups = (p.Hq + kMergeHeads - 1) / kMergeHeads;
+template <int LANES>
+__global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedArgs p) {
+  constexpr int kHeads = kMergeThreads / LANES;
+  constexpr int kPairs = kPagedSplits / LANES;   // (max, sum) pairs a lane
+  constexpr int kRound = LANES / 32 * kMergeAhead;
+  static_assert(LANES % kRound == 0, "a round's weights lie in one register");
+  const int groups = (p.Hq + kHeads - 1) / kHeads;
   const int r = static_cast<int>(blockIdx.x) / groups;   // (below rows_cap, by the grid)
-  const int h = (static_cast<int>(blockIdx.x) % groups) * kMergeHeads + (threadIdx.x >> 5);
+  const int h = static_cast<int>(blockIdx.x) % groups * kHeads + threadIdx.x / LANES;
   const i32x16 head = record(p.plan);
   const size_t byte = static_cast<size_t>(p.rows_at) + r;
   const uint32_t word = *as_const<uint32_t>(p.plan + (byte & ~size_t(3)));
@@ -900,60 +904,73 @@ __global__ __launch_bounds__(32 * kMergeHeads) void paged_merge_kernel(PagedArgs
   if (!plan_is_ours(p, __builtin_bit_cast(PlanHeader, head)) | (r < sq.row0) | (r >= sq.row0 + sq.T) | (sq.nsplit == 1))
     return;   // (a row of no sequence, or written by the attention)
   if (h >= p.Hq) return;
-  const int nsplit = sq.nsplit, lane = threadIdx.x & 31;
+  const int nsplit = sq.nsplit, lane = threadIdx.x % LANES;
+  const int first = lane / 32 * kMergeAhead;   // this half's splits of a round
   const int row = (h % p.G) * sq.T + (r - sq.row0);
   const size_t base = sq.part_off + static_cast<size_t>(h / p.G) * sq.rows_pad + row;
   const size_t stride = static_cast<size_t>(p.Hkv) * sq.rows_pad;   // from split to split
-  const uint16_t* const po = p.part_o + base * HD + 4 * lane;
-  float m[kMergeLanes], l[kMergeLanes];
+  const uint16_t* const po = p.part_o + base * HD + 4 * (lane & 31);
+  float m[kPairs], l[kPairs];
 #pragma unroll
-  for (int k = 0; k < kMergeLanes; ++k) {
+  for (int k = 0; k < kPairs; ++k) {
     m[k] = -INFINITY;
     l[k] = 0.f;
-    if (lane + 32 * k < nsplit) {
-      const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + (base + (lane + 32 * k) * stride) * 2);
+    if (lane + LANES * k < nsplit) {
+      const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + (base + (lane + LANES * k) * stride) * 2);
       m[k] = ml.x;
       l[k] = ml.y;
     }
   }
+  // (kBatch at a time without a branch between them: a split past the last is
+  // that one again, at no weight)
+  constexpr int kBatch = LANES == 64 ? kMergeAhead : 4;
   uint2 ob[kMergeAhead];
-  auto request = [&](int c0) {
+  auto request = [&](int c) {
 #pragma unroll
     for (int k = 0; k < kMergeAhead; ++k)
-      if (c0 + k < nsplit) ob[k] = *reinterpret_cast<const uint2*>(po + (c0 + k) * stride * HD);   // (uniform)
+      if (k / kBatch == 0 || c + k / kBatch * kBatch < nsplit)
+        ob[k] = *reinterpret_cast<const uint2*>(po + min(c + first + k, nsplit - 1) * stride * HD);
   };
   request(0);
-  float M = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
-  static_assert(kMergeLanes == 4, "four pairs a lane");
+  float M = m[0];
 #pragma unroll
-  for (int off = 16; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, 32));
+  for (int k = 1; k < kPairs; ++k) M = fmaxf(M, m[k]);
+#pragma unroll
+  for (int off = LANES / 2; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, LANES));
   // (a split that sees no key of the row has max -inf and counts for nothing;
   // where M is -inf too the row has a NaN score, kept in a sum)
   float lsum = 0.f;
 #pragma unroll
-  for (int k = 0; k < kMergeLanes; ++k) {
+  for (int k = 0; k < kPairs; ++k) {
     l[k] = m[k] == -INFINITY ? l[k] : l[k] * __builtin_amdgcn_exp2f(m[k] - M);
     lsum += l[k];
   }
 #pragma unroll
-  for (int off = 16; off >= 1; off >>= 1) lsum += __shfl_xor(lsum, off, 32);
+  for (int off = LANES / 2; off >= 1; off >>= 1) lsum += __shfl_xor(lsum, off, LANES);
   const float inv = 1.f / lsum;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int c0 = 0; c0 < nsplit; c0 += kMergeAhead) {
-    if (c0 > 0) request(c0);
-    float w = l[0];   // the splits' weights, lane c % 32 holding split c's (c0 to c0 + 15 lie in one register)
+  for (int c = 0; c < nsplit; c += kRound) {
+    if (c > 0) request(c);
+    float w = l[0];   // the splits' weights, lane s % LANES holding split s's
 #pragma unroll
-    for (int k = 1; k < kMergeLanes; ++k) w = c0 >= 32 * k ? l[k] : w;
+    for (int k = 1; k < kPairs; ++k) w = c >= LANES * k ? l[k] : w;   // (0 past the last split)
 #pragma unroll
     for (int k = 0; k < kMergeAhead; ++k) {
-      const float wc = __shfl(w, (c0 + k) & 31, 32);
-      if (c0 + k < nsplit) {
+      const float wc = __shfl(w, (c + first + k) % LANES, LANES);
+      if (k / kBatch == 0 || c + k / kBatch * kBatch < nsplit) {
         acc.x = fmaf(wc, __uint_as_float(ob[k].x << 16), acc.x);
         acc.y = fmaf(wc, __uint_as_float(ob[k].x & 0xffff0000u), acc.y);
         acc.z = fmaf(wc, __uint_as_float(ob[k].y << 16), acc.z);
         acc.w = fmaf(wc, __uint_as_float(ob[k].y & 0xffff0000u), acc.w);
       }
     }
+  }
+  if constexpr (LANES == 64) {
+    acc.x += __shfl_xor(acc.x, 32, 64);
+    acc.y += __shfl_xor(acc.y, 32, 64);
+    acc.z += __shfl_xor(acc.z, 32, 64);
+    acc.w += __shfl_xor(acc.w, 32, 64);
+    if (lane >= 32) return;
   }
   const uint2 pk = {__builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{acc.x * inv, acc.y * inv}), bf16x2)),
                     __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{acc.z * inv, acc.w * inv}), bf16x2))};
@@ -1141,7 +1158,13 @@ extern "C" int32_t entmtp_tree_attn_paged(const entmtp_bank* bank, int32_t B, co
   a.cap_log2 = softcap * kLog2e;
   a.theta = static_cast<double>(rope_theta);
   rope_freqs(rope_theta, a.freq);
-  const long long blocks = static_cast<long long>(rows_cap) * ((Hq + kMergeHeads - 1) / kMergeHeads);
+  // a wavefront a head where they are few, so that long prefixes' many splits
+  // take half the round trips: 26 rows of 32 heads at 8192 20.9 us (attention and
+  // merge) against 23.9 by half wavefronts, 8 rows of 8 heads at 32000 18.9
+  // against 26.4; 4096 heads are level, 32768 take 10 us more by whole ones
+  const bool few = static_cast<long long>(rows_cap) * Hq <= 4LL * device_cus();
+  const int heads = kMergeThreads / (few ? 64 : 32);
+  const long long blocks = static_cast<long long>(rows_cap) * ((Hq + heads - 1) / heads);
   ENTMTP_CHECK_ARG(blocks <= INT32_MAX, ENTMTP_ERANGE, "%d rows of %d heads: too many", rows_cap, Hq);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(sh.items), dim3(kAttnThreads), 0, s, a); };
@@ -1152,6 +1175,9 @@ extern "C" int32_t entmtp_tree_attn_paged(const entmtp_bank* bank, int32_t B, co
     wide ? go(paged_attn_kernel<true, false>) : go(paged_attn_kernel<false, false>);
   if (int32_t rc = launch_status("tree_attn_paged launch")) return rc;
   if (!sh.splits) return ENTMTP_OK;
-  hipLaunchKernelGGL(paged_merge_kernel, dim3(static_cast<uint32_t>(blocks)), dim3(32 * kMergeHeads), 0, s, a);
+  auto merge = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(blocks)), dim3(kMergeThreads), 0, s, a);
+  };
+  few ? merge(paged_merge_kernel<64>) : merge(paged_merge_kernel<32>);
   return launch_status("tree_attn_paged merge launch");
 }
