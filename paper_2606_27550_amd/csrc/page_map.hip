@@ -42,11 +42,7 @@ struct MapArgs {
 // Inclusive sum over threads 0 .. 255 (four whole wavefronts call it).
 __device__ __forceinline__ int scan256(int v, int* part) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const int o = __shfl_up(v, off, 64);
-    if (lane >= off) v += o;
-  }
+  v = scan_wave(v, add);
   if (wave < 4 && lane == 63) part[wave] = v;
   __syncthreads();
   for (int w = 0; w < 3; ++w)

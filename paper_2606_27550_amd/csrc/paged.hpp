@@ -87,6 +87,21 @@ inline int32_t check_pages(int32_t max_pages, int32_t page_size) {
   return ENTMTP_OK;
 }
 
+// Inclusive sum (or, of values not below zero, maximum) over a wavefront's
+// lanes, by DPP: within rows of 16, then from row to row.
+template <typename F>
+__device__ __forceinline__ int scan_wave(int v, F f) {
+  v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false));   // row_shr:1
+  v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false));
+  v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false));
+  v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false));
+  v = f(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false));   // lane 15 to the next row
+  return f(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false));   // lane 31 to the upper half
+}
+__device__ __forceinline__ int add(int a, int b) { return a + b; }
+__device__ __forceinline__ int larger(int a, int b) { return max(a, b); }
+__device__ __forceinline__ int last_lane(int v) { return __builtin_amdgcn_readlane(v, 63); }
+
 // The sequence whose rows [row_off[b], row_off[b + 1]) hold row r: the number
 // of sequences that end at or before it (B: none).  Called by whole
 // wavefronts with r uniform; the loads go out together.

@@ -122,21 +122,15 @@ struct PlanArgs {
   int B, G, Hq, Hkv, shift, n_pages, max_pages, rows_cap, window, slots, items_cap, two;
 };
 
-// Inclusive sum over the workgroup's 256 threads; part: four entries of LDS of
-// this call's own.
-template <typename T>
-__device__ __forceinline__ T scan_threads(T v, T* part) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const T o = __shfl_up(v, off, 64);
-    if (lane >= off) v += o;
-  }
-  if (lane == 63) part[wave] = v;
-  __syncthreads();
-  for (int w = 0; w < 3; ++w)
-    if (w < wave) v += part[w];
-  return v;
+// ceil(nb / t) as paged_splits clips it: the quotient by t's reciprocal is off
+// by less than one up to 200, and past the clip beyond.
+__device__ __forceinline__ int paged_splits_by(int nb, int t, float rt) {
+  if (nb <= kLoneBlocks) return 1;
+  const int bound = min(nb / kMinBlocksPerSplit, kPagedSplits), n = nb + t - 1;
+  int q = static_cast<int>(static_cast<float>(n) * rt);
+  const int r = n - q * t;
+  q += r < 0 ? -1 : (r >= t ? 1 : 0);
+  return q < 1 ? 1 : min(q, bound);
 }
 
 // Bound by its chain of loads, scans and barriers: one sequence takes 6 us, 256
@@ -144,9 +138,9 @@ __device__ __forceinline__ T scan_threads(T v, T* part) {
 // launch or a wait between workgroups).
 __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs p) {
   static_assert(kPlanThreads == 256 && kTargets == 16, "four wavefronts; 16 threads to a candidate");
-  __shared__ int s_nb[kPagedSeqs], s_H[kPagedSeqs];
-  __shared__ long long part_work[4], part_rows[4];
-  __shared__ int part_items[4], part_max[4];
+  __shared__ int2 s_size[kPagedSeqs];   // blocks, streams
+  __shared__ long long part_work[4];
+  __shared__ int part_max[4], part_items[4], part_rows[4];
   __shared__ int s_items[4][kTargets], s_split[4][kTargets];
   __shared__ PlanSeq s_seq;
   __shared__ int s_tree, s_L, s_len, s_item0, s_nb0, s_end[4];
@@ -172,24 +166,29 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs p) {
   const int rows_pad = rows_padded(p.G, T);
   const int nqg = query_groups(rows_pad / kQTile);
   const int H = p.Hkv * nqg;
-  s_nb[tid] = nb;
-  s_H[tid] = H;
+  s_size[tid] = make_int2(nb, H);
   // the split target: thread (sequence group, candidate) weighs its share
-  scan_threads(static_cast<long long>(H) * nb, part_work);
-  int nb_max = nb;
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) nb_max = max(nb_max, __shfl_xor(nb_max, off, 64));
-  if (lane == 0) part_max[wave] = nb_max;
+  const long long mine = static_cast<long long>(H) * nb;   // (below 2^40: summed up in two pieces of 20 bits)
+  const int lo = last_lane(scan_wave(static_cast<int>(mine & 0xfffff), add));
+  const int hi = last_lane(scan_wave(static_cast<int>(mine >> 20), add));
+  int nb_max = last_lane(scan_wave(nb, larger));
+  if (lane == 0) {
+    part_work[wave] = (static_cast<long long>(hi) << 20) + lo;
+    part_max[wave] = nb_max;
+  }
   __syncthreads();
   const long long work = part_work[0] + part_work[1] + part_work[2] + part_work[3];
   nb_max = max(max(part_max[0], part_max[1]), max(part_max[2], part_max[3]));
   const int k = lane & 15;
   const int t = batch_target(k, work, nb_max, p.slots);
+  const float rt = 1.f / static_cast<float>(t);
   int items = 0, split = 0;
+#pragma unroll 4   // (their LDS reads overlap)
   for (int u = tid >> 4; u < p.B; u += 16) {
-    const int n = paged_splits(s_nb[u], t);
-    items += s_H[u] * n;
-    split |= s_H[u] > 0 && n > 1;
+    const int2 q = s_size[u];
+    const int n = paged_splits_by(q.x, t, rt);
+    items += q.y * n;
+    split |= q.y > 0 && n > 1;
   }
 #pragma unroll
   for (int off = 16; off <= 32; off <<= 1) {
@@ -216,13 +215,21 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs p) {
   // of sequences that overlap, which no page map makes, can pass the bounds:
   // the last sequences then have no work.)
   const int len = T ? (p.Hkv * ns + 7) / 8 * 8 * nqg : 0;
-  const long long prows = ns > 1 ? static_cast<long long>(ns) * p.Hkv * rows_pad : 0;
-  const int item_end = scan_threads(len, part_items);
-  const long long part_end = scan_threads(prows, part_rows);
-  const bool fits = item_end <= p.items_cap && part_end <= p.part_cap;
-  int last = fits ? item_end : 0;
+  const int ptiles = ns > 1 ? ns * p.Hkv * (rows_pad / kQTile) : 0;   // (four an item at most: no wrap where the items fit)
+  int item_end = scan_wave(len, add), tile_end = scan_wave(ptiles, add);
+  if (lane == 63) {
+    part_items[wave] = item_end;
+    part_rows[wave] = tile_end;
+  }
+  __syncthreads();
 #pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) last = max(last, __shfl_xor(last, off, 64));
+  for (int w = 0; w < 3; ++w) {
+    item_end += w < wave ? part_items[w] : 0;
+    tile_end += w < wave ? part_rows[w] : 0;
+  }
+  const long long part_end = static_cast<long long>(tile_end) * kQTile, prows = static_cast<long long>(ptiles) * kQTile;
+  const bool fits = item_end <= p.items_cap && part_end <= p.part_cap;
+  const int last = last_lane(scan_wave(fits ? item_end : 0, larger));
   if (lane == 0) s_end[wave] = last;
   const int b = blockIdx.x;
   if (tid == b) {
