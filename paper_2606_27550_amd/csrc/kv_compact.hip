@@ -117,8 +117,8 @@ int32_t launch_compact(const CompactArgs& a, int B, hipStream_t s) {
 // all its loads are in flight at once; the moves' slots are held by a
 // wavefront's lanes and read as scalars.  Bound by four dependent round trips
 // (lengths and path, slots, rows, stores) with few bytes behind them: one
-// layer of one sequence takes 3.8 us, 32 layers of 32 sequences 10.1 (20 MB:
-// 4 us at a large copy's rate).
+// layer of one sequence takes 3.4 us, 32 layers of 32 sequences 9.5 (20 MB:
+// 4 us at a large copy's rate; 11.1 with columns of 8 bytes, half the registers).
 // ROWS: path entries held (registers), at least the path capacity's.
 struct CompactPagedArgs {
   uint16_t* kp;   // [n_layers] pools [n_pages][Hkv][P][d], layer_stride apart

@@ -15,8 +15,8 @@
 //
 // One workgroup: two scans over at most 256 sequences (a thread each), then a
 // thread per tree row.  It is bound by its memory round trips (entries, trees,
-// table, free list), so each of them asks for all it needs at once: 4.2 us for
-// one sequence, 9.3 for 256 of up to 128 nodes.
+// table, free list), so each of them asks for all it needs at once: 3.8 us for
+// one sequence, 9.0 for 256 of up to 128 nodes.
 #include "paged.hpp"
 
 namespace entmtp {

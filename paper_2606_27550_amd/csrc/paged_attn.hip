@@ -26,7 +26,7 @@
 //  - The score cap, distance bias and window live in an instance of their own;
 //    a window also cuts the key blocks that the plan hands out.
 // Few rows are HBM bound: 32 single tokens at 8192 (32:8 heads) take 188 us,
-// 5.7 TB/s; 26 nodes at 131000 115 us, 4.7.  Large trees are bound by the issue
+// 5.7 TB/s; 26 nodes at 131000 110 us, 4.9.  Large trees are bound by the issue
 // of both pipes: a wave spends 16 products of 32 cycles and about 60 vector
 // instructions and 16 exponentials on a block, 500 cycles each, and two waves a
 // SIMD (512 registers between them, most of them the outputs and queries) hide
@@ -133,8 +133,8 @@ __device__ __forceinline__ int paged_splits_by(int nb, int t, float rt) {
   return q < 1 ? 1 : min(q, bound);
 }
 
-// Bound by its chain of loads, scans and barriers: one sequence takes 6 us, 256
-// take 10 (each workgroup weighs the whole batch, which is cheaper than a second
+// Bound by its chain of loads, scans and barriers: one sequence takes 5.2 us, 256
+// take 9.2 (each workgroup weighs the whole batch, which is cheaper than a second
 // launch or a wait between workgroups).
 __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs p) {
   static_assert(kPlanThreads == 256 && kTargets == 16, "four wavefronts; 16 threads to a candidate");
@@ -887,7 +887,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
 // wavefront's halves of 16 splits each, summed up at the end.  The first partial
 // outputs are requested with the (max, sum) pairs.  The row's sequence is found
 // by scalar loads: its number, then its record.
-// Round trips and little data: 512 rows of 32 heads in four splits take 9 us with
+// Round trips and little data: 512 rows of 32 heads in four splits take 8 us with
 // the launch.
 constexpr int kMergeThreads = 256;
 constexpr int kMergeAhead = 16;
