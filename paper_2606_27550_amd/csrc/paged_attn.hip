@@ -965,10 +965,11 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedArgs p)
     for (int k = 0; k < kMergeAhead; ++k) {
       const float wc = __shfl(w, (c + first + k) % LANES, LANES);
       if (k / kBatch == 0 || c + k / kBatch * kBatch < nsplit) {
-        acc.x = fmaf(wc, __uint_as_float(ob[k].x << 16), acc.x);
-        acc.y = fmaf(wc, __uint_as_float(ob[k].x & 0xffff0000u), acc.y);
-        acc.z = fmaf(wc, __uint_as_float(ob[k].y << 16), acc.z);
-        acc.w = fmaf(wc, __uint_as_float(ob[k].y & 0xffff0000u), acc.w);
+        const uint2 v = c + first + k < nsplit ? ob[k] : uint2{0u, 0u};   // (the last one again may hold infinities)
+        acc.x = fmaf(wc, __uint_as_float(v.x << 16), acc.x);
+        acc.y = fmaf(wc, __uint_as_float(v.x & 0xffff0000u), acc.y);
+        acc.z = fmaf(wc, __uint_as_float(v.y << 16), acc.z);
+        acc.w = fmaf(wc, __uint_as_float(v.y & 0xffff0000u), acc.w);
       }
     }
   }
@@ -1166,8 +1167,8 @@ extern "C" int32_t entmtp_tree_attn_paged(const entmtp_bank* bank, int32_t B, co
   a.theta = static_cast<double>(rope_theta);
   rope_freqs(rope_theta, a.freq);
   // a wavefront a head where they are few, so that long prefixes' many splits
-  // take half the round trips: 26 rows of 32 heads at 8192 20.9 us (attention and
-  // merge) against 23.9 by half wavefronts, 8 rows of 8 heads at 32000 18.9
+  // take half the round trips: 26 rows of 32 heads at 8192 21.4 us (attention and
+  // merge) against 23.9 by half wavefronts, 8 rows of 8 heads at 32000 18.3
   // against 26.4; 4096 heads are level, 32768 take 10 us more by whole ones
   const bool few = static_cast<long long>(rows_cap) * Hq <= 4LL * device_cus();
   const int heads = kMergeThreads / (few ? 64 : 32);

@@ -328,6 +328,21 @@ def test_what_is_not_finite_at_the_windows_edge(api, bad, which):
             assert np.isnan(got[:64][sees]).all()
 
 
+@pytest.mark.parametrize("t,Hq,Hkv,L", [(2, 32, 8, 5000), (4, 32, 8, 1500), (0, 8, 8, 3333)])
+def test_an_infinite_value_of_the_prefix_is_one_in_its_column(api, t, Hq, Hkv, L):
+    """Also from the last of a prefix's splits, and however many heads a merge takes."""
+    c = make(27, [t], [L], Hq, Hkv, 16)
+    clean = launch(api, c)["out"].float().cpu().numpy()
+    for pos in (3, L - 40):
+        e = dict(c, vp=c["vp"].copy())
+        e["vp"][c["table"][0, pos // 16], 0, pos % 16, 9] = 0x7F80
+        got = launch(api, e)["out"].float().cpu().numpy()
+        G = Hq // Hkv
+        assert np.isposinf(got[:, :G, 9]).all()
+        got[:, :G, 9] = clean[:, :G, 9]
+        np.testing.assert_array_equal(got, clean)
+
+
 def test_streams_graphs_and_two_at_once(api):
     """A captured plan and attention follow the lengths they find; two batches on two streams, each with its workspace."""
     c = make(15, [2, 0, 1, 4], [0, 0, 0, 0], 8, 2, 16)
