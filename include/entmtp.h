@@ -505,13 +505,22 @@ int32_t entmtp_kv_compact_batched_device(int32_t B, const int32_t* path, int32_t
  * the bank up to 32 trees.  The order of one
  * step is
  *   entmtp_page_map              rows, slots and pages of the step's trees
- *   entmtp_tree_attn_paged_plan  the attention's work list, for all layers
+ *   entmtp_tree_attn_paged_plan  the attention's work list, for all layers;
+ *                                run = entmtp_tree_attn_paged_topo(plan, B)
  *   entmtp_tree_attn_paged       layer by layer
  *   entmtp_verify_logits, entmtp_logit_adjust, entmtp_accept_batched_device
- *                                (topo + 16 k, row_off + 16 k for sequences
- *                                16 k .. 16 k + 15 of a larger batch)
+ *                                with run in topo's place (run + 16 k, row_off
+ *                                + 16 k for sequences 16 k .. 16 k + 15 of a
+ *                                larger batch)
  *   entmtp_kv_compact_paged, entmtp_token_history_accept
- * with prefix_len[b] += accept_len[b] + 1 before the next one.
+ * with prefix_len[b] += accept_len[b] + 1 before the next one.  run[b] is
+ * topo[b], or -1 for a sequence that the page map or the plan could not serve
+ * (no free page, a page missing, no room).  Such a sequence keeps its place in
+ * row_off, but what lies in its rows was not computed: with run its logits are
+ * left alone, its accept_len and bonus come out -1, and its length, history,
+ * pool slots and pages stay as they are, so that it can be run again, from the
+ * same last token, in a later step (topo itself is never changed).  (The LM
+ * head computes all rows.)
  * The current device is the one the bank and the tensors lie on.
  */
 
@@ -562,6 +571,14 @@ int32_t entmtp_page_map(const entmtp_bank* bank, int32_t B, const int32_t* topo,
  * may be NULL) is 1 where one lies outside [0, n_pages), which leaves the
  * sequence without work, else 0.  With a window, entries of pages that lie
  * wholly before the root's are not read (they may be given back).
+ * entmtp_tree_attn_paged_topo: where the plan's call writes the trees of the
+ * sequences that have work, a device int32[B] inside plan: topo[b], or -1 where
+ * there is none (topo[b] outside the bank, a status, a bad page, no room).  The
+ * step's later calls take it in topo's place; so does the next plan of a step
+ * that makes several (for layers with other windows), and the later calls then
+ * the last one's, which has work for the sequences that every plan serves (a
+ * plan is not made from its own: EINVAL).
+ * NULL where plan is NULL or B out of range.
  *   window  0: none; else node i sees positions above pos(i) - window
  *   plan    device buffer of entmtp_tree_attn_paged_plan_bytes() bytes (0: bad
  *           sizes), 64-byte aligned, for this bank, current device and sizes
@@ -572,6 +589,7 @@ int32_t entmtp_page_map(const entmtp_bank* bank, int32_t B, const int32_t* topo,
 size_t entmtp_tree_attn_paged_plan_bytes(const entmtp_bank* bank, int32_t B, int32_t rows_cap,
                                          int32_t Hq, int32_t Hkv, int32_t max_pages,
                                          int32_t page_size);
+const int32_t* entmtp_tree_attn_paged_topo(const void* plan, int32_t B);
 int32_t entmtp_tree_attn_paged_plan(const entmtp_bank* bank, int32_t B, const int32_t* topo,
                                     const int32_t* prefix_len, const int32_t* row_off,
                                     const int32_t* status, const int32_t* block_table,

@@ -104,6 +104,7 @@ _SIGNATURES = {
     "entmtp_tree_attn_paged_plan_bytes": (_c_sz, [_c_p] + [_c_i32] * 6),
     "entmtp_tree_attn_paged_plan": (_c_i32, [_c_p, _c_i32] + [_c_p] * 5 + [_c_i32] * 7 + [_c_p, _c_p, _c_sz,
                                                                                          _c_p]),
+    "entmtp_tree_attn_paged_topo": (_c_p, [_c_p, _c_i32]),
     "entmtp_tree_attn_paged_workspace": (_c_sz, [_c_p] + [_c_i32] * 7),
     "entmtp_tree_attn_paged": (_c_i32, [_c_p, _c_i32, _c_p, _c_sz] + [_c_p] * 5 +
                                [_c_i32, _c_i32, _c_p, _c_i32, _c_p] + [_c_i32] * 4 +
@@ -841,7 +842,8 @@ def tree_attn_paged_plan(bank: Bank, topo, prefix_len, row_off, status, block_ta
     """The attention's work list of a step, for all layers with this window:
     row_off and status from page_map, plan a buffer of
     tree_attn_paged_plan_bytes; bad int32 [B] (or None): sequences with a
-    prefix page outside the pool."""
+    prefix page outside the pool.  What follows the attention in the step takes
+    tree_attn_paged_topo(plan, B) in topo's place."""
     i32 = _torch.int32
     B = _paged_batch(topo)
     _, max_pages = _dims(block_table, "block_table", 2)
@@ -855,6 +857,20 @@ def tree_attn_paged_plan(bank: Bank, topo, prefix_len, row_off, status, block_ta
                                            max_pages, page_size, n_pages, rows_cap, Hq, Hkv, window,
                                            None if bad is None else _at(bad, "bad", i32, (B,), dev),
                                            plan_p, size, _stream_on(stream, dev)))
+
+
+def tree_attn_paged_topo(plan, B: int):
+    """The int32 [B] inside a plan that tree_attn_paged_plan writes (a view, made
+    once): the trees of the sequences that have work, -1 for the others.
+    logit_adjust and accept_batched_device (and the next plan, if a step makes
+    several) take it in topo's place, so that a sequence that could not be
+    mapped is not accepted from rows that were never computed."""
+    _need(isinstance(plan, _torch.Tensor) and plan.is_contiguous(), "plan must be a contiguous tensor")
+    _need(1 <= B <= PAGED_B_MAX, f"1 <= B <= {PAGED_B_MAX}")
+    at = lib.entmtp_tree_attn_paged_topo(plan.data_ptr(), B)
+    off = (at or 0) - plan.data_ptr()
+    _need(at and off + 4 * B <= plan.nbytes, f"the plan is too small for a batch of {B}")
+    return plan.reshape(-1).view(_torch.uint8)[off:off + 4 * B].view(_torch.int32)
 
 
 def tree_attn_paged_workspace(bank: Bank, B: int, rows_cap: int, Hq: int, Hkv: int, d: int,

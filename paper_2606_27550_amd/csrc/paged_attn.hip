@@ -76,10 +76,11 @@ struct PlanItem {
 };
 static_assert(sizeof(PlanItem) == 64, "plan layout");
 
-// A plan: header, sequences, the sequence of every tree row (a byte each; only
-// rows that hold one are written, the reader checks it against the sequence's
-// record), work items.
-size_t plan_rows_at(int B) { return sizeof(PlanHeader) + sizeof(PlanSeq) * B; }
+// A plan: header, sequences, the tree of every sequence that has work (-1: none),
+// the sequence of every tree row (a byte each; only rows that hold one are
+// written, the reader checks it against the sequence's record), work items.
+size_t plan_topo_at(int B) { return sizeof(PlanHeader) + sizeof(PlanSeq) * B; }
+size_t plan_rows_at(int B) { return plan_topo_at(B) + sizeof(int) * B; }
 size_t plan_items_at(int B, int rows_cap) { return (plan_rows_at(B) + rows_cap + 63) / 64 * 64; }
 static_assert(kPagedSeqs <= 256, "a sequence is a byte");
 
@@ -118,7 +119,7 @@ struct PlanArgs {
   const int* table;
   int* bad;
   uint8_t* plan;
-  long long rows_at, items_at, part_cap;
+  long long topo_at, rows_at, items_at, part_cap;
   int B, G, Hq, Hkv, shift, n_pages, max_pages, rows_cap, window, slots, items_cap, two;
 };
 
@@ -291,6 +292,7 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs p) {
     PlanSeq q = s_seq;
     q.T = sT;
     reinterpret_cast<PlanSeq*>(p.plan + sizeof(PlanHeader))[b] = q;
+    reinterpret_cast<int*>(p.plan + p.topo_at)[b] = sT > 0 ? s_tree : -1;
     if (p.bad) p.bad[b] = bad != 0;
     if (b == 0) {
       PlanHeader h{};
@@ -1062,6 +1064,11 @@ extern "C" size_t entmtp_tree_attn_paged_workspace(const entmtp_bank* bank, int3
   return paged_shape(bank, B, rows_cap, Hq, Hkv, static_cast<long long>(max_pages) * page_size).workspace;
 }
 
+extern "C" const int32_t* entmtp_tree_attn_paged_topo(const void* plan, int32_t B) {
+  if (!plan || !paged_batch(B)) return nullptr;
+  return reinterpret_cast<const int32_t*>(static_cast<const uint8_t*>(plan) + plan_topo_at(B));
+}
+
 extern "C" int32_t entmtp_tree_attn_paged_plan(const entmtp_bank* bank, int32_t B, const int32_t* topo,
                                                const int32_t* prefix_len, const int32_t* row_off,
                                                const int32_t* status, const int32_t* block_table, int32_t max_pages,
@@ -1079,6 +1086,8 @@ extern "C" int32_t entmtp_tree_attn_paged_plan(const entmtp_bank* bank, int32_t 
   ENTMTP_CHECK_ARG(sh.items < INT32_MAX / 64, ENTMTP_ERANGE, "%d rows of %d heads: too many", rows_cap, Hq);
   ENTMTP_CHECK_ARG(plan_bytes >= sh.plan_bytes, ENTMTP_ENOSPC, "the plan has %zu bytes, needs %zu", plan_bytes,
                    sh.plan_bytes);
+  ENTMTP_CHECK_ARG(reinterpret_cast<uintptr_t>(topo) - reinterpret_cast<uintptr_t>(plan) >= sh.plan_bytes, ENTMTP_EINVAL,
+                   "topo must not lie in the plan that is made from it");
   a.topo = topo;
   a.len = prefix_len;
   a.row_off = row_off;
@@ -1086,6 +1095,7 @@ extern "C" int32_t entmtp_tree_attn_paged_plan(const entmtp_bank* bank, int32_t 
   a.table = block_table;
   a.bad = bad;
   a.plan = static_cast<uint8_t*>(plan);
+  a.topo_at = static_cast<long long>(plan_topo_at(B));
   a.rows_at = static_cast<long long>(plan_rows_at(B));
   a.items_at = static_cast<long long>(plan_items_at(B, rows_cap));
   a.part_cap = sh.part_rows;
