@@ -5,6 +5,7 @@
 // indices (paper §2.3) -- precomputed once so that the scheduler of §4 can
 // switch trees by index ("Cost": a pointer swap with no GPU work).  Planning
 // is pure host code; the finished image goes to the device in one copy.
+#include <atomic>
 #include <cstdarg>
 #include <cstring>
 
@@ -134,7 +135,9 @@ extern "C" int32_t entmtp_bank_build(const int32_t* parents, const int32_t* size
     base += T;
   }
 
+  static std::atomic<uint64_t> banks{0};
   auto* bank = new entmtp_bank();
+  bank->number = ++banks;
   bank->desc.resize(n_trees);
   base = 0;
   for (int32_t t = 0; t < n_trees; ++t) {

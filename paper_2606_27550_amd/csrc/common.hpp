@@ -49,6 +49,7 @@ struct entmtp_bank {
   std::vector<uint8_t> image;  // host copy of the arena contents
   uint8_t* arena = nullptr;    // device arena (nullptr for a host-only bank)
   int device = -1;
+  uint64_t number = 0;         // of all banks of the process (an arena's address can come again)
 };
 
 namespace entmtp {

@@ -21,6 +21,7 @@ struct PagedTree {
 
 struct TreeTable {
   const uint8_t* arena;
+  uint64_t bank;   // its number
   int n;
   PagedTree t[kPagedTrees];
 };
@@ -37,6 +38,7 @@ inline int32_t tree_table(const entmtp_bank* bank, TreeTable* out) {
                    "a device-planned batch names at most %d bank trees (bank has %zu)", kPagedTrees,
                    bank->desc.size());
   out->arena = bank->arena;
+  out->bank = bank->number;
   out->n = static_cast<int>(bank->desc.size());
   for (int k = 0; k < out->n; ++k) {
     const TopoDesc& td = bank->desc[k];

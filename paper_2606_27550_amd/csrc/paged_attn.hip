@@ -54,7 +54,7 @@ constexpr int kPlanMagic = 0x50a6ed01;
 // with a plan of something else) and the length of its work list.
 struct PlanHeader {
   int magic, B, Hq, Hkv, shift, n_pages, max_pages, rows_cap, window, items;
-  uint32_t arena_lo, arena_hi;
+  uint32_t bank_lo, bank_hi;
   int pad[4];
 };
 static_assert(sizeof(PlanHeader) == 64, "plan layout");
@@ -306,8 +306,8 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs p) {
       h.rows_cap = p.rows_cap;
       h.window = p.window;
       h.items = max(max(s_end[0], s_end[1]), max(s_end[2], s_end[3]));
-      h.arena_lo = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p.trees.arena));
-      h.arena_hi = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p.trees.arena) >> 32);
+      h.bank_lo = static_cast<uint32_t>(p.trees.bank);
+      h.bank_hi = static_cast<uint32_t>(p.trees.bank >> 32);
       *reinterpret_cast<PlanHeader*>(p.plan) = h;
     }
   }
@@ -330,6 +330,7 @@ struct PagedArgs {
   float* part_ml;        // [part rows][2]
   uint16_t* out;         // [rows_cap][Hq][HD]
   long long rows_at, items_at;
+  uint64_t bank;         // the bank's number
   int B, G, Hq, Hkv, shift, n_pages, max_pages, rows_cap, window;
   float q_scale;     // scale log2(e), or with a cap 2 log2(e) scale / cap
   float cap_log2;    // cap log2(e), 0: no cap
@@ -352,11 +353,10 @@ __device__ __forceinline__ i32x16 record(const uint8_t* p) { return *as_const<i3
 
 // Whether a plan's header h says that it was made for this call.
 __device__ __forceinline__ bool plan_is_ours(const PagedArgs& p, const PlanHeader& h) {
-  const uintptr_t a = reinterpret_cast<uintptr_t>(p.arena);
   return ((h.magic ^ kPlanMagic) | (h.B ^ p.B) | (h.Hq ^ p.Hq) | (h.Hkv ^ p.Hkv) | (h.shift ^ p.shift) |
           (h.n_pages ^ p.n_pages) | (h.max_pages ^ p.max_pages) | (h.rows_cap ^ p.rows_cap) | (h.window ^ p.window) |
-          static_cast<int>(h.arena_lo ^ static_cast<uint32_t>(a)) |
-          static_cast<int>(h.arena_hi ^ static_cast<uint32_t>(a >> 32))) == 0;
+          static_cast<int>(h.bank_lo ^ static_cast<uint32_t>(p.bank)) |
+          static_cast<int>(h.bank_hi ^ static_cast<uint32_t>(p.bank >> 32))) == 0;
 }
 
 // A pair of bf16 values with those that are not finite as zeros (odd is set).
@@ -1149,6 +1149,7 @@ extern "C" int32_t entmtp_tree_attn_paged(const entmtp_bank* bank, int32_t B, co
   PagedArgs a{};
   a.plan = static_cast<const uint8_t*>(plan);
   a.arena = trees.arena;
+  a.bank = trees.bank;
   a.table = block_table;
   a.slot_map = slot_map;
   a.slopes = slopes;
