@@ -21,8 +21,10 @@
 //    outside the pool read as zeros (an empty buffer), never out of bounds.
 //  - Long prefixes split up to 128 ways (few heads and one sequence still fill
 //    the chip), and half a wavefront merges a row's partials.
-//  - The queries carry the scale, and a block's products start from minus the
-//    row's reference, so they leave the matrix pipe as exponents of two.
+//  - Rotated queries carry the scale (it shares their one rounding to bf16), and
+//    a block's products start from minus the row's reference, so they leave the
+//    matrix pipe as exponents of two.  Queries that are not rotated are exact in
+//    bf16 and stay as they are; their scores are scaled in fp32.
 //  - The score cap, distance bias and window live in an instance of their own;
 //    a window also cuts the key blocks that the plan hands out.
 // Few rows are HBM bound: 32 single tokens at 8192 (32:8 heads) take 188 us,
@@ -332,10 +334,9 @@ struct PagedArgs {
   long long rows_at, items_at;
   uint64_t bank;         // the bank's number
   int B, G, Hq, Hkv, shift, n_pages, max_pages, rows_cap, window;
-  float q_scale;     // scale log2(e), or with a cap 2 log2(e) scale / cap
+  float q_scale;     // scale log2(e), or with a cap 2 log2(e) scale / cap: of the rotated query, or the products
   float cap_log2;    // cap log2(e), 0: no cap
-  double theta;             // rotation base (0: no rotation)
-  double freq[kRopePairs];
+  double freq[kRopePairs];   // of the rotation's pairs
 };
 
 // Memory that earlier kernels wrote and this one only reads, by scalar loads.
@@ -366,9 +367,11 @@ __device__ __forceinline__ uint32_t finite_pair(uint32_t w, bool& odd) {
   return w & ((lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u));
 }
 
-// WIDE: the rotation's angles may pass the short sine's range (wide_angles).
-// MOD: a score cap, distance bias or window.
-template <bool WIDE, bool MOD>
+// TURN: no rotation, one whose angles keep to the short sine's range, or one
+// whose angles may pass it (wide_angles).  MOD: a score cap, distance bias or
+// window.
+enum Turn { kStill, kNear, kWide };
+template <Turn TURN, bool MOD>
 __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p) {
   // one LDS object per slot, so that the compiler can tell the slot being
   // read from the slots the copies in flight write to
@@ -396,7 +399,11 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
   const int* const depth = reinterpret_cast<const int*>(p.arena + it.off_depth);
   const Const<int> pages = as_const<int>(p.table + static_cast<size_t>(b) * p.max_pages);
   const int nb = blk_hi - blk_lo;
-  const bool rope = p.theta > 0.0;
+  constexpr bool rope = TURN != kStill, WIDE = TURN == kWide;
+  // what the products are: exponents of two over the row's reference (REF), bare
+  // dot products still to be scaled (!rope), or, with a cap's or bias's turn to
+  // come, scaled ones
+  constexpr bool REF = rope && !MOD;
   // the first query group's workgroups keep the tree's keys (rotated) and
   // values in their slots of the pool for the steps after this one
   const bool keeper = qg == 0;
@@ -491,7 +498,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
     bool odd = false;
     if (!t.there) t.k0 = t.k1 = t.v0 = t.v1 = u32x4{0u, 0u, 0u, 0u};   // (here: the loads' first use)
     if (key >= L && key < nkeys) {
-      if (rope) rope_pairs(t.k0, t.k1, tab64(s_depth[key - L]) + 8 * tcc, tcc & 7);
+      if constexpr (rope) rope_pairs(t.k0, t.k1, tab64(s_depth[key - L]) + 8 * tcc, tcc & 7);
       if (t.slot >= 0 && t.slot < p.n_pages << p.shift) {
         const size_t off = (((static_cast<size_t>(t.slot >> p.shift) * p.Hkv + g) << p.shift) + (t.slot & (P - 1))) * HD;
         uint16_t* kd = p.kp + off + 8 * tcc;
@@ -515,7 +522,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
     *reinterpret_cast<u32x4*>(row + kRingK + (((tcc + 8) ^ v_swz(trow)) << 4)) = t.v1;
   };
 
-  double freq = p.freq[tid % kRopePairs];
+  double freq = rope ? p.freq[tid % kRopePairs] : 0.0;
   int page = page_of(0);
   const int page1 = page_of(1), page2 = page_of(2);
   TreeRegs tregs;
@@ -556,23 +563,18 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
   float2* const tab32 = reinterpret_cast<float2*>(slot3);
   static_assert((ENTMTP_D_MAX + 1) * kRopePairs * sizeof(float2) <= kRingSlot, "the angles fit in a slot");
   // (times what the scores are scaled by, so that the products give logits in
-  // base 2, or the cap's argument; no rotation is a turn by nothing)
+  // base 2, or the cap's argument)
   const float qs = p.q_scale;
   auto tab_put = [&](int d, int pr, double2 cs) {
     tab32[d * kRopePairs + (pr ^ (2 * (d & 31)))] = make_float2(static_cast<float>(cs.x) * qs, static_cast<float>(cs.y) * qs);
   };
-  if (rope) {
-    rope_table<WIDE>(tid, D, L, freq, tab_put);
-  } else {
-    for (int d = tid / kRopePairs; d <= D; d += kAttnThreads / kRopePairs)
-      tab_put(d, tid % kRopePairs, make_double2(1.0, 0.0));
-  }
+  if constexpr (rope) rope_table<WIDE>(tid, D, L, freq, tab_put);
   s_depth[tid] = static_cast<uint8_t>(tdepth);
   static_assert(kAttnThreads >= ENTMTP_T_MAX, "one thread per node");
   wait_lds();
   stage_barrier();
   if (!qlive) mlo = mhi = u32x4{~0u, ~0u, ~0u, ~0u};   // padding rows see every key
-  {
+  if constexpr (rope) {
     const float2* tr = tab32 + qdepth * kRopePairs;
 #pragma unroll
     for (int s = 0; s < 4; ++s) rope_pairs_f32(qf[s], qf[s + 4], tr, 16 * s + 8 * lh, 2 * (qdepth & 31));
@@ -583,7 +585,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
 
   // l_run: the sum of this lane's half of the keys (the halves meet at the end)
   float m_run = -INFINITY, l_run = 0.f;
-  // Unless the scores are bent, a block's products start from minus the row's
+  // REF: a block's products start from minus the row's
   // reference (zero before its first), so that they come out as the exponents
   // themselves; lift: how far a block's largest may pass the reference.
   f32x16 ref;
@@ -606,11 +608,11 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
 
   // S^T = K Q^T of the block in a slot
   auto scores = [&](const uint8_t* slot, f32x16& sacc) {
-    if constexpr (MOD) {
+    if constexpr (REF) {
+      sacc = ref;
+    } else {
 #pragma unroll
       for (int r = 0; r < 16; ++r) sacc[r] = 0.f;
-    } else {
-      sacc = ref;
     }
 #pragma unroll
     for (int s = 0; s < 8; ++s) {
@@ -622,6 +624,10 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
   // tanh(u) = 1 - 2 / (e^2u + 1) with 2 u / ln 2 from the products: 0 and
   // infinity of the exponential give -1 and 1.
   auto bend = [&](f32x16& sacc, auto dist) {
+    if constexpr (!rope) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sacc[r] *= qs;
+    }
     if (p.cap_log2 > 0.f) {
 #pragma unroll
       for (int r = 0; r < 16; ++r)
@@ -700,10 +706,12 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
       for (int r = 0; r < 16; ++r) bmax = fmaxf(bmax, sacc[r]);
     }
     bmax = max_halves(bmax);
-    // bent scores are held against m_run here, the others are relative to it
-    const bool need = MOD ? bmax > m_run + kLazyLog2 : bmax > lift;
+    constexpr bool bare = !rope && !MOD;
+    if constexpr (bare) bmax *= qs;
+    // REF's are relative to m_run, the others are held against it here
+    const bool need = REF ? bmax > lift : bmax > m_run + kLazyLog2;
     if (__any(need)) {
-      const float mn = !need ? m_run : (MOD || m_run == -INFINITY ? bmax : m_run + bmax);
+      const float mn = !need ? m_run : (!REF || m_run == -INFINITY ? bmax : m_run + bmax);
       const float alpha = !need ? 1.f : (m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - mn));
       l_run *= alpha;
 #pragma unroll
@@ -711,7 +719,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[ct][r] *= alpha;
       m_run = mn;
-      if constexpr (!MOD) {
+      if constexpr (REF) {
         const float by = need ? bmax : 0.f;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
@@ -722,12 +730,12 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
         lift = need ? kLazyLog2 : lift;
       }
     }
-    const float mneg = !MOD || m_run == -INFINITY ? 0.f : -m_run;
+    const float mneg = REF || m_run == -INFINITY ? 0.f : -m_run;
     float pr[16];
     float rsum = 0.f;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      pr[r] = __builtin_amdgcn_exp2f(MOD ? sacc[r] + mneg : sacc[r]);
+      pr[r] = __builtin_amdgcn_exp2f(REF ? sacc[r] : (bare ? fmaf(sacc[r], qs, mneg) : sacc[r] + mneg));
       rsum += pr[r];
     }
     l_run += rsum;
@@ -823,7 +831,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
   // the other two
   if (nb > np) {
     __syncthreads();
-    if (rope) {
+    if constexpr (rope) {
       rope_table<WIDE>(tid, D, L, freq, [&](int d, int pr, double2 cs) { tab64(d)[pr ^ ((pr >> 3) & 7)] = cs; });
       __syncthreads();
     }
@@ -1175,7 +1183,7 @@ extern "C" int32_t entmtp_tree_attn_paged(const entmtp_bank* bank, int32_t B, co
   a.window = window;
   a.q_scale = softcap > 0.f ? 2.f * kLog2e * (scale / softcap) : scale * kLog2e;
   a.cap_log2 = softcap * kLog2e;
-  a.theta = static_cast<double>(rope_theta);
+  const double theta = static_cast<double>(rope_theta);
   rope_freqs(rope_theta, a.freq);
   // a wavefront a head where they are few, so that long prefixes' many splits
   // take half the round trips: 26 rows of 32 heads at 8192 21.4 us (attention and
@@ -1187,11 +1195,13 @@ extern "C" int32_t entmtp_tree_attn_paged(const entmtp_bank* bank, int32_t B, co
   ENTMTP_CHECK_ARG(blocks <= INT32_MAX, ENTMTP_ERANGE, "%d rows of %d heads: too many", rows_cap, Hq);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(sh.items), dim3(kAttnThreads), 0, s, a); };
-  const bool mod = softcap > 0.f || window > 0 || slopes != nullptr, wide = wide_angles(a.theta);
-  if (mod)
-    wide ? go(paged_attn_kernel<true, true>) : go(paged_attn_kernel<false, true>);
+  const bool mod = softcap > 0.f || window > 0 || slopes != nullptr;
+  if (theta == 0.0)
+    mod ? go(paged_attn_kernel<kStill, true>) : go(paged_attn_kernel<kStill, false>);
+  else if (wide_angles(theta))
+    mod ? go(paged_attn_kernel<kWide, true>) : go(paged_attn_kernel<kWide, false>);
   else
-    wide ? go(paged_attn_kernel<true, false>) : go(paged_attn_kernel<false, false>);
+    mod ? go(paged_attn_kernel<kNear, true>) : go(paged_attn_kernel<kNear, false>);
   if (int32_t rc = launch_status("tree_attn_paged launch")) return rc;
   if (!sh.splits) return ENTMTP_OK;
   auto merge = [&](auto kernel) {
