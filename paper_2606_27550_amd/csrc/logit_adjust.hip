@@ -23,7 +23,7 @@
 // writes its own statistics partial (no barrier in the row loop) and a second
 // kernel merges a row's partials, a wavefront per row.
 // HBM bound, 8 bytes an entry and row, once the arithmetic fits beside it: 1024
-// rows of 128256 with everything asked for take 207 us, 5.1 TB/s (a large copy
+// rows of 128256 with everything asked for take 208 us, 5.1 TB/s (a large copy
 // reaches 5.2; 255 with divisions, reductions by LDS permutes, the argmax's
 // index kept entry by entry and stores through the caches).  26 rows of 32000
 // take 9.8 us, both kernels' latency.
@@ -191,7 +191,7 @@ __global__ __launch_bounds__(kAdjThreads) void logit_adjust_kernel(AdjustArgs p)
   float bias[kEntries];
   int b_held = -1;
   float4 par = make_float4(1.f, 0.f, 0.f, 1.f);
-  float rrep = 1.f;
+  double rrep = 1.0, rrep_lo = 0.0;   // 1 / rep: rounded, and what that left
   bool biased = false, counts = false;
   auto work = [&](float (&x)[kEntries], int i) {
     const int r = row_at(i);
@@ -200,7 +200,8 @@ __global__ __launch_bounds__(kAdjThreads) void logit_adjust_kernel(AdjustArgs p)
     if (b != b_held) {
       b_held = b;
       par = p.params[b];
-      rrep = 1.f / par.x;
+      rrep = 1.0 / static_cast<double>(par.x);
+      rrep_lo = fma(-rrep, static_cast<double>(par.x), 1.0) * rrep;
       counts = par.x != 1.f || par.y != 0.f || par.z != 0.f;
       const int bi = p.bias ? p.bias_idx[b] : -1;
       biased = bi >= 0 && bi < p.n_bias;
@@ -244,10 +245,14 @@ __global__ __launch_bounds__(kAdjThreads) void logit_adjust_kernel(AdjustArgs p)
           for (int e = 0; e < 4; ++e) {
             const int h = hist[4 * u + e], more = (said >> (8 * e)) & 0xff;
             float z = x[4 * u + e];
-            // z / rep: the reciprocal's product and a Newton step of it, which
-            // round as the division does (no step where one of them is infinite)
-            const float q = z * rrep, step = fmaf(fmaf(-q, par.x, z), rrep, q);
-            z = z > 0.f ? (fabsf(step) < INFINITY ? step : q) : z * par.x;
+            // z / rep as fp32 rounds it, by way of 64 bits: with the reciprocal's
+            // two words the product is the quotient to 2^-104 before its rounding
+            // to 53 bits.  Those hold a quotient that lies right where fp32's
+            // rounding turns (only one below the normal numbers can), and any other
+            // is 2^-49 of itself or more away from there.  (Infinity, by either.)
+            const double zd = static_cast<double>(z);
+            const float q = static_cast<float>(fma(zd, rrep, zd * rrep_lo));
+            z = z > 0.f && z < INFINITY ? q : z * par.x;
             const int c = (h & INT_MAX) + more;
             if (c > 0) z = (z - par.y * static_cast<float>(c)) - par.z;
             if ((h | more) != 0) x[4 * u + e] = z;
