@@ -605,8 +605,10 @@ int32_t entmtp_tree_attn_paged_plan(const entmtp_bank* bank, int32_t B, const in
  * [rows_cap][Hq][d], k_tree, v_tree [rows_cap][Hkv][d] bf16 hold the tree rows
  * where row_off put them; rows of no sequence, or of one without work, are
  * left alone in out.
- *   softcap  0: none; else, up to 1024, scores s = scale * (q . k) become
- *            softcap * tanh(s / softcap), to within softcap * 2^-21
+ *   softcap  0: none; else, up to 1024 and at least scale / 2^64, scores
+ *            s = scale * (q . k) become softcap * tanh(s / softcap), to within
+ *            softcap * 2^-21 (scale / softcap * sum |q_i k_i| has to stay a
+ *            finite fp32 number)
  *   slopes   NULL: none; else device fp32[Hq]: slopes[h] * (pos_q - pos_k) is
  *            taken off the score (after the cap)
  *   window   as the plan's: keys with pos_q - pos_k >= window are not seen

@@ -1138,9 +1138,11 @@ extern "C" int32_t entmtp_tree_attn_paged(const entmtp_bank* bank, int32_t B, co
   ENTMTP_CHECK_ARG(d == HD, ENTMTP_EINVAL, "head dim %d unsupported (built for %d)", d, HD);
   ENTMTP_CHECK_ARG(scale > 0.f && scale < INFINITY, ENTMTP_EINVAL, "scale must be positive");
   ENTMTP_CHECK_ARG(rope_theta >= 0.f && rope_theta < INFINITY, ENTMTP_EINVAL, "rope_theta must be >= 0");
-  // (1 - 2 / (e^2u + 1) is off by about 2^-22, the cap times that)
-  ENTMTP_CHECK_ARG(softcap >= 0.f && softcap <= kMaxCap && (softcap == 0.f || 4.f * (scale / softcap) < INFINITY),
-                   ENTMTP_EINVAL, "softcap = %g must be 0 or in (0, %g], scale / softcap finite",
+  // (1 - 2 / (e^2u + 1) is off by about 2^-22, the cap times that.  The query
+  // carries scale / softcap: past 2^64 ordinary ones would come near bf16's
+  // and the products' largest numbers, and infinities of both signs are no tanh.)
+  ENTMTP_CHECK_ARG(softcap >= 0.f && softcap <= kMaxCap && (softcap == 0.f || scale / softcap <= 0x1p64f),
+                   ENTMTP_EINVAL, "softcap = %g must be 0 or in (0, %g], scale / softcap at most 2^64",
                    static_cast<double>(softcap), static_cast<double>(kMaxCap));
   ENTMTP_CHECK_ARG((reinterpret_cast<uintptr_t>(plan) & 63u) == 0, ENTMTP_EINVAL, "the plan must be 64-byte aligned");
   ENTMTP_CHECK_ARG(aligned16(q) && aligned16(k_tree) && aligned16(v_tree) && aligned16(k_pool) && aligned16(v_pool) &&
