@@ -872,7 +872,8 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
       p.part_ml[prow * 2 + 1] = l_run;
     }
   }
-  const float il = l_run == 0.f ? 0.f : 1.f / l_run;   // 0: no key of the split is visible
+  // (a split may hold no key that the row sees: zeros; a whole row sees its own)
+  const float il = l_run == 0.f && nsplit > 1 ? 0.f : 1.f / l_run;
   auto pack = [&](float u, float v) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{u * il, v * il}), bf16x2));
   };
