@@ -619,9 +619,11 @@ int32_t entmtp_tree_attn_paged_plan(const entmtp_bank* bank, int32_t B, const in
  * A plan made for other sizes, another window or another bank leaves every
  * output alone.  Keys and values that are not finite reach the rows that see
  * them (from a tree node's value, or one that a window hides from part of the
- * tree, all dims become NaN) and no others; keys and values before the root's
- * window are not read.
- * Requirements: d == ENTMTP_HEAD_DIM; otherwise as the plan.
+ * tree, all dims become NaN; so do those of a row whose every visible score is
+ * minus infinity) and no others; keys and values before the root's window are
+ * not read.
+ * Requirements: d == ENTMTP_HEAD_DIM; q, k_tree, v_tree, pools, out and
+ * workspace 16-byte aligned; otherwise as the plan.
  * Errors (host-checked): EINVAL, ERANGE, ENOSPC, EHIP.
  */
 size_t entmtp_tree_attn_paged_workspace(const entmtp_bank* bank, int32_t B, int32_t rows_cap,
@@ -689,6 +691,7 @@ int32_t entmtp_kv_compact_paged(int32_t B, const int32_t* path, int32_t path_cap
  *            (not needed when no statistics are asked for); used by this call
  * Rows of no sequence (behind the last, or where the tree has fewer nodes) are
  * left alone in every output.
+ * Requirements: logits, out, params, history and bias 16-byte aligned.
  * Errors (host-checked): EINVAL, ERANGE, ENOSPC, EHIP.
  */
 size_t entmtp_logit_adjust_workspace(int32_t rows, int32_t V);

@@ -26,7 +26,7 @@
 // rows of 128256 with everything asked for take 208 us, 5.1 TB/s (a large copy
 // reaches 5.2; 255 with divisions, reductions by LDS permutes, the argmax's
 // index kept entry by entry and stores through the caches).  26 rows of 32000
-// take 9.8 us, both kernels' latency.
+// take 9.9 us, both kernels' latency.
 #include <cfloat>
 #include <climits>
 #include <type_traits>
@@ -489,10 +489,11 @@ extern "C" int32_t entmtp_logit_adjust(const entmtp_bank* bank, int32_t B, const
   a.n_masks = n_masks;
   a.words = mask_words;
   a.slices = adjust_slices(V);
-  // Rows a workgroup takes: as many as leave two rounds of the workgroups that
-  // are resident (four a CU, by registers), so that few rows fill the chip and
-  // many share their start.  128 rows of 128256: one row each 38.6 us, two 35.0;
-  // 1024 rows: four 207, eight 215; 26 rows of 128256: one 14.7.
+  // Rows a workgroup takes: as many as leave two rounds of four workgroups a CU
+  // (what registers let reside where V is a multiple of four; three elsewhere),
+  // so that few rows fill the chip and many share their start.  128 rows of
+  // 128256: one row each 38.6 us, two 35.0; 1024 rows: four 208, eight 215; 26
+  // rows of 128256: one 14.7.
   const long long fill = static_cast<long long>(rows) * a.slices / (8 * device_cus());
   a.group = static_cast<int>(fill < 1 ? 1 : (fill > kRows ? kRows : fill));
   const int step = (V & 3) ? 4 : 1;   // rows a workgroup's rows lie apart

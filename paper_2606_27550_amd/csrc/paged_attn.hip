@@ -20,22 +20,27 @@
 //    number comes by a scalar load one block ahead and costs no wait.  Pages
 //    outside the pool read as zeros (an empty buffer), never out of bounds.
 //  - Long prefixes split up to 128 ways (few heads and one sequence still fill
-//    the chip), and half a wavefront merges a row's partials.
+//    the chip); half a wavefront merges a row's partials, a whole one where the
+//    rows are few.
 //  - Rotated queries carry the scale (it shares their one rounding to bf16), and
 //    a block's products start from minus the row's reference, so they leave the
 //    matrix pipe as exponents of two.  Queries that are not rotated are exact in
 //    bf16 and stay as they are; their scores are scaled in fp32.
 //  - The score cap, distance bias and window live in an instance of their own;
 //    a window also cuts the key blocks that the plan hands out.
-// Few rows are HBM bound: 32 single tokens at 8192 (32:8 heads) take 188 us,
-// 5.7 TB/s; 26 nodes at 131000 110 us, 4.9.  Large trees are bound by the issue
-// of both pipes: a wave spends 16 products of 32 cycles and about 60 vector
-// instructions and 16 exponentials on a block, 500 cycles each, and two waves a
-// SIMD (512 registers between them, most of them the outputs and queries) hide
-// a third of it: eight 128-node trees at 8192 take 162 us, 0.85 PFLOP/s (a large
-// product reaches 1.31); 208 with a score cap, whose tanh adds two
-// transcendentals a score.  What is smaller is a chain of round trips: one token
-// at 63 takes 7.7 us.
+// Few rows are HBM bound: 32 single tokens at 8192 (32:8 heads) take 189-196 us,
+// 5.5 TB/s (a plain read reaches 6.4; nothing is fetched twice); 26 nodes at
+// 131000 110-116 us, 4.8.  Large trees are bound by the issue of both pipes:
+// counted per wave and block, 16 products keep the matrix pipe for 512 cycles,
+// 64 vector instructions and 16 exponentials the vector pipe for 450, and two
+// waves a SIMD (512 registers between them, most of them the outputs and
+// queries) overlap 170 of them, 960 cycles in all: eight 128-node trees at 8192
+// take 160-171 us, 0.84 PFLOP/s (a large product reaches 1.34).  A score cap's
+// tanh adds two transcendentals a score (950 vector cycles): 206-215 us; a
+// distance bias takes 211-220, no rotation 165-169.  What is smaller is a chain
+// of round trips: one token at 63 takes 7.6 us, 9.0 behind a table of more than
+// 22 pages of 16, whose prefixes could be split (a workgroup for every item
+// there could be, and the merge, which find nothing to do).
 #include <algorithm>
 #include <type_traits>
 
@@ -328,7 +333,12 @@ struct PagedArgs {
   const uint16_t* vt;
   uint16_t* kp;          // [n_pages][Hkv][P][HD]
   uint16_t* vp;
-  uint16_t* part_o;      // [part rows][HD] bf16: the split's output, normalised by its sum
+  // [part rows][HD]: the split's output, normalised by its sum so that it stays
+  // within its values' range, in bf16: in fp32 the whole output's error against
+  // 64 bits is 3.4-3.5e-3 instead of 3.7-3.9e-3 (the weights' and the query's
+  // roundings stay), and the bytes cost 3-6 % of long prefixes and windows, 15 % of 26
+  // nodes at 8192 (21.5 -> 24.7 us)
+  uint16_t* part_o;
   float* part_ml;        // [part rows][2]
   uint16_t* out;         // [rows_cap][Hq][HD]
   long long rows_at, items_at;

@@ -192,6 +192,7 @@ __device__ __forceinline__ SeqPlan resolve(const BatchArgs& p, int b) {
   return q;
 }
 
+// The sequence that owns index x of a device-planned batch's attend or merge
 // grid (MERGE), its plan included; T = 0 for an index past the last; total:
 // where the indexes end.  Lane i
 // of each wavefront reads sequence i's entries; a sequence whose tree index
