@@ -576,8 +576,10 @@ int32_t entmtp_page_map(const entmtp_bank* bank, int32_t B, const int32_t* topo,
  * there is none (topo[b] outside the bank, a status, a bad page, no room).  The
  * step's later calls take it in topo's place; so does the next plan of a step
  * that makes several (for layers with other windows), and the later calls then
- * the last one's, which has work for the sequences that every plan serves (a
- * plan is not made from its own: EINVAL).
+ * the last one's, which has work for the sequences that every plan serves (the
+ * layers of an earlier plan may have written the tree's slots of one that a
+ * later plan does not serve, never its prefix's; a plan is not made from its
+ * own: EINVAL).
  * NULL where plan is NULL or B out of range.
  *   window  0: none; else node i sees positions above pos(i) - window
  *   plan    device buffer of entmtp_tree_attn_paged_plan_bytes() bytes (0: bad
