@@ -23,7 +23,7 @@
 // writes its own statistics partial (no barrier in the row loop) and a second
 // kernel merges a row's partials, a wavefront per row.
 // HBM bound, 8 bytes an entry and row, once the arithmetic fits beside it: 1024
-// rows of 128256 with everything asked for take 208 us, 5.1 TB/s (a large copy
+// rows of 128256 with everything asked for take 209 us, 5.1 TB/s (a large copy
 // reaches 5.2; 255 with divisions, reductions by LDS permutes, the argmax's
 // index kept entry by entry and stores through the caches).  26 rows of 32000
 // take 9.9 us, both kernels' latency.
@@ -202,6 +202,7 @@ __global__ __launch_bounds__(kAdjThreads) void logit_adjust_kernel(AdjustArgs p)
       par = p.params[b];
       rrep = 1.0 / static_cast<double>(par.x);
       rrep_lo = fma(-rrep, static_cast<double>(par.x), 1.0) * rrep;
+      rrep_lo = rrep_lo == rrep_lo ? rrep_lo : 0.0;   // (a factor of infinity or zero)
       counts = par.x != 1.f || par.y != 0.f || par.z != 0.f;
       const int bi = p.bias ? p.bias_idx[b] : -1;
       biased = bi >= 0 && bi < p.n_bias;
@@ -492,7 +493,7 @@ extern "C" int32_t entmtp_logit_adjust(const entmtp_bank* bank, int32_t B, const
   // Rows a workgroup takes: as many as leave two rounds of four workgroups a CU
   // (what registers let reside where V is a multiple of four; three elsewhere),
   // so that few rows fill the chip and many share their start.  128 rows of
-  // 128256: one row each 38.6 us, two 35.0; 1024 rows: four 208, eight 215; 26
+  // 128256: one row each 38.6 us, two 35.0; 1024 rows: four 209, eight 215; 26
   // rows of 128256: one 14.7.
   const long long fill = static_cast<long long>(rows) * a.slices / (8 * device_cus());
   a.group = static_cast<int>(fill < 1 ? 1 : (fill > kRows ? kRows : fill));

@@ -27,7 +27,7 @@ def floats(g, n, lo, hi):
 
 
 @pytest.mark.parametrize("V", [1 << 16, (1 << 16) + 3])
-@pytest.mark.parametrize("reps", ["ordinary", "any", "edges"])
+@pytest.mark.parametrize("reps", ["ordinary", "any", "edges", "beyond"])
 def test_a_seen_logit_is_divided_as_fp32_divides(api, V, reps):
     g = np.random.default_rng(V + len(reps))
     B = 16
@@ -36,10 +36,13 @@ def test_a_seen_logit_is_divided_as_fp32_divides(api, V, reps):
                               np.nextafter(np.float32(2.0 ** 40), np.float32(np.inf)), 2.0 ** -149, 2.0 ** -127, 2.0 ** -126,
                               3.4028234e38, 2.0 ** 126, 2.0 ** 127, np.nextafter(np.float32(1), np.float32(2)),
                               np.nextafter(np.float32(1), np.float32(0)), np.nextafter(np.float32(2), np.float32(0)), 1.5,
-                              1.1754942e-38, 1e-39])}[reps].astype(np.float32)
+                              1.1754942e-38, 1e-39]),
+           "beyond": np.resize(np.array([np.inf, 0.0, -1.5, -1e-39]), B)}[reps].astype(np.float32)   # (not asked for)
     z = np.concatenate([floats(g, V // 2, -6, 6), floats(g, V // 4, -149, 127), floats(g, V - V // 2 - V // 4, -64, -56)])
     z = (z * g.choice(np.array([1, 1, 1, -1], np.float32), V)).astype(np.float32)
     z[:6] = [0.0, -0.0, np.inf, -np.inf, 2.0 ** -60, 2.0 ** 60]
+    if reps == "beyond":
+        z[2:4] = 1.0
     z = np.tile(z, (B, 1))
     for b in range(B):
         g.shuffle(z[b])
