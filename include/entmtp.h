@@ -55,6 +55,7 @@ extern "C" {
 #define ENTMTP_HEAD_DIM   128  /* the head dimension the attention kernels are built for */
 #define ENTMTP_B_MAX      16   /* sequences per batched call */
 #define ENTMTP_PAGED_B_MAX 256 /* sequences per call over a page pool */
+#define ENTMTP_FP4_ROW    68   /* bytes of a head's row of ENTMTP_HEAD_DIM values in 4 bits */
 
 /* status[b] of entmtp_page_map (and entmtp_tree_attn_paged_plan) */
 #define ENTMTP_PAGE_OK    0
@@ -281,6 +282,20 @@ int32_t entmtp_tree_attn_batched_device(const entmtp_bank* bank, int32_t B, cons
 int32_t entmtp_verify_logits(const entmtp_bf16* hidden, const entmtp_bf16* w_lm,
                              int32_t T, int32_t hid, int32_t V, float* logits,
                              void* stream);
+
+/*
+ * entmtp_verify_logits with the weights in 4 bits (their form is described at
+ * entmtp_quantize_fp4, which makes them): codes [V][hid / 2] and scales
+ * [V][hid / 32] bytes.  The weights enter the products as the numbers they stand for
+ * (exact in bf16, up to its largest), sums are fp32.  A weight row with a scale
+ * byte 255 has NaN logits.
+ * Requirements: 1 <= T <= 4096, 32 <= hid <= 65536, hid % 32 == 0, V >= 1, hidden,
+ * codes and logits 16-byte aligned.
+ * Errors (host-checked): EINVAL, EHIP.
+ */
+int32_t entmtp_verify_logits_fp4(const entmtp_bf16* hidden, const uint8_t* codes,
+                                 const uint8_t* scales, int32_t T, int32_t hid, int32_t V,
+                                 float* logits, void* stream);
 
 /*
  * Fused form of entmtp_verify_logits followed by entmtp_logit_stats: the
@@ -659,6 +674,150 @@ int32_t entmtp_kv_compact_paged(int32_t B, const int32_t* path, int32_t path_cap
                                 entmtp_bf16* v_pool, int32_t n_layers, int64_t layer_stride,
                                 int32_t n_pages, int32_t Hkv, int32_t page_size, int32_t d,
                                 void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* New rows on their way into the pool, and pools and weights in 4 bits.      */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * Four bits: a row's values lie in groups of 32 along the row.  A group has a
+ * scale byte s, the power of two 2^(s - 127) (255: not a number), and each value
+ * a code: bit 3 its sign, bits 0-2 one of 0, 1/2, 1, 3/2, 2, 3, 4, 6; the value
+ * is code x scale.  Two codes a byte, the first value in the lower half.
+ * A group of bf16 values is held so: with m the largest magnitude and e =
+ * floor(log2 m), one more where m >= 1.75 x 2^e, s = e - 2 + 127, at least 2 and
+ * at most 252; every value the nearest code (of two equally near ones the even
+ * one; beyond 6 the last); where a value is not finite s = 255 and all codes are
+ * zero (the whole group is no number).
+ * A 4-bit pool is k_pool / v_pool [n_pages][Hkv][page_size * ENTMTP_FP4_ROW]
+ * bytes: of a page's head the rows' codes, page_size x 64 bytes, then their
+ * scale bytes, page_size x 4.  Page numbers, slots and block tables are those of
+ * a bf16 pool.  A step over 4-bit pools runs as one over bf16 pools, with
+ *   entmtp_page_map
+ *   entmtp_tree_attn_paged_fp4_plan   run = entmtp_tree_attn_paged_topo(plan, B)
+ *   entmtp_tree_positions             with run in topo's place, for all layers
+ *   entmtp_kv_append_paged_fp4, entmtp_tree_attn_paged_fp4   layer by layer
+ *   entmtp_verify_logits or entmtp_verify_logits_fp4, and what follows
+ *   entmtp_kv_compact_paged_fp4
+ */
+
+/*
+ * x [rows][n] bf16 -> codes [rows][n / 2] and scales [rows][n / 32] bytes (as
+ * entmtp_verify_logits_fp4 takes its weights).
+ * Requirements: rows >= 1, n >= 32, n % 32 == 0, x 16-byte, codes 4-byte aligned.
+ * Errors (host-checked): EINVAL, EHIP.
+ */
+int32_t entmtp_quantize_fp4(const entmtp_bf16* x, int64_t rows, int32_t n, uint8_t* codes,
+                            uint8_t* scales, void* stream);
+
+/*
+ * Positions of a step's tree rows: pos[row_off[b] + i] = prefix_len[b] +
+ * depth(i) for node i of tree topo[b] (device int32[B] each), -1 in every other
+ * row of [0, rows): those of no sequence, of one whose topo[b] lies outside the
+ * bank (run in topo's place: of one that is not served), with prefix_len[b] < 0
+ * or within ENTMTP_T_MAX of 2^31, and behind a tree's nodes.
+ * Requirements: rows >= 1; sequences' rows do not overlap.
+ * Errors (host-checked): EINVAL, ERANGE, EHIP.
+ */
+int32_t entmtp_tree_positions(const entmtp_bank* bank, int32_t B, const int32_t* topo,
+                              const int32_t* prefix_len, const int32_t* row_off, int32_t rows,
+                              int32_t* pos, void* stream);
+
+/*
+ * One layer's new rows: queries and keys normed per head (optional) and turned
+ * to their positions, keys and values written to their slots of the pool -- a
+ * step's tree rows (positions of entmtp_tree_positions, slots of
+ * entmtp_page_map), or a prompt's.  For every row r with pos[r] >= 0:
+ *   norm    y = x / sqrt(mean(x^2) + eps) * weight, over the d values of a head
+ *           (q_norm / k_norm: bf16 [d], or NULL: none)
+ *   turn    pairs (c, c + d / 2) by the angle pos[r] * rope_theta^(-2 c / d)
+ *           (rope_theta 0: none)
+ *   q_out   [rows][Hq][d] bf16: the queries, rounded once
+ *   pool    slot slot_map[r] of every head (outside the pool: not written): the
+ *           key, computed in fp64 and rounded to fp32 and then to bf16, and the
+ *           value; in a 4-bit pool the codes of both (of the key so rounded)
+ *   k_out, v_out  [rows][Hkv][d] bf16, each may be NULL: key and value as the
+ *           pool holds them (of a 4-bit pool what the codes stand for), for an
+ *           attention over the prompt itself
+ * Rows with pos[r] < 0 are left alone in every output.  q and q_out may both be
+ * NULL.  q, k and v are rows of Hq x d, Hkv x d, Hkv x d values, their rows
+ * q_stride, k_stride, v_stride values apart (parts of one projection's output);
+ * q_out may be q, k_out k and v_out v where those are dense.  Slots that several
+ * rows name are left in an unspecified state; with a head that holds values
+ * that are not finite the row's norm, and all it makes of the head, is no number.
+ * Requirements: d == ENTMTP_HEAD_DIM, eps >= 0, strides multiples of 8, tensors
+ * and pools 16-byte aligned, slots as in entmtp_page_map.
+ * Errors (host-checked): EINVAL, ERANGE, EHIP.
+ */
+int32_t entmtp_kv_append_paged(const entmtp_bf16* q, int64_t q_stride, const entmtp_bf16* k,
+                               int64_t k_stride, const entmtp_bf16* v, int64_t v_stride,
+                               int32_t rows, int32_t Hq, int32_t Hkv, int32_t d,
+                               const int32_t* pos, const int32_t* slot_map,
+                               const entmtp_bf16* q_norm, const entmtp_bf16* k_norm, float eps,
+                               float rope_theta, entmtp_bf16* q_out, entmtp_bf16* k_pool,
+                               entmtp_bf16* v_pool, int32_t n_pages, int32_t page_size,
+                               entmtp_bf16* k_out, entmtp_bf16* v_out, void* stream);
+int32_t entmtp_kv_append_paged_fp4(const entmtp_bf16* q, int64_t q_stride, const entmtp_bf16* k,
+                                   int64_t k_stride, const entmtp_bf16* v, int64_t v_stride,
+                                   int32_t rows, int32_t Hq, int32_t Hkv, int32_t d,
+                                   const int32_t* pos, const int32_t* slot_map,
+                                   const entmtp_bf16* q_norm, const entmtp_bf16* k_norm, float eps,
+                                   float rope_theta, entmtp_bf16* q_out, uint8_t* k_pool,
+                                   uint8_t* v_pool, int32_t n_pages, int32_t page_size,
+                                   entmtp_bf16* k_out, entmtp_bf16* v_out, void* stream);
+
+/*
+ * The work list of entmtp_tree_attn_paged_fp4: as entmtp_tree_attn_paged_plan,
+ * for 4-bit pools (entmtp_tree_attn_paged_topo reads either).  The tree's rows
+ * are read from the pool like the prefix's, so their pages are checked too.
+ */
+size_t entmtp_tree_attn_paged_fp4_plan_bytes(const entmtp_bank* bank, int32_t B, int32_t rows_cap,
+                                             int32_t Hq, int32_t Hkv, int32_t max_pages,
+                                             int32_t page_size);
+int32_t entmtp_tree_attn_paged_fp4_plan(const entmtp_bank* bank, int32_t B, const int32_t* topo,
+                                        const int32_t* prefix_len, const int32_t* row_off,
+                                        const int32_t* status, const int32_t* block_table,
+                                        int32_t max_pages, int32_t page_size, int32_t n_pages,
+                                        int32_t rows_cap, int32_t Hq, int32_t Hkv, int32_t window,
+                                        int32_t* bad, void* plan, size_t plan_bytes, void* stream);
+
+/*
+ * One attention layer over 4-bit pools for the batch of a plan: node i of
+ * sequence b attends to the prefix and to its root-to-node path, whose rows
+ * entmtp_kv_append_paged_fp4 has put at positions prefix_len[b] + node of the
+ * block table.  q [rows_cap][Hq][d] bf16 holds the queries as they enter the
+ * products (turned already; entmtp_kv_append_paged_fp4's q_out); scale, softcap,
+ * slopes, window, out and workspace (of entmtp_tree_attn_paged_fp4_workspace()
+ * bytes) as for entmtp_tree_attn_paged.  A plan of other sizes, another window,
+ * another bank or a bf16 pool leaves every output alone.  Groups with scale byte
+ * 255 make a row that sees their key NaN, all its dims, and no other row.
+ * Requirements: d == ENTMTP_HEAD_DIM; q, pools, out and workspace 16-byte
+ * aligned; otherwise as the plan.
+ * Errors (host-checked): EINVAL, ERANGE, ENOSPC, EHIP.
+ */
+size_t entmtp_tree_attn_paged_fp4_workspace(const entmtp_bank* bank, int32_t B, int32_t rows_cap,
+                                            int32_t Hq, int32_t Hkv, int32_t d, int32_t max_pages,
+                                            int32_t page_size);
+int32_t entmtp_tree_attn_paged_fp4(const entmtp_bank* bank, int32_t B, const void* plan,
+                                   size_t plan_bytes, const entmtp_bf16* q, const uint8_t* k_pool,
+                                   const uint8_t* v_pool, int32_t n_pages, int32_t page_size,
+                                   const int32_t* block_table, int32_t max_pages, int32_t rows_cap,
+                                   int32_t Hq, int32_t Hkv, int32_t d, float scale, float softcap,
+                                   int32_t window, const float* slopes, entmtp_bf16* out,
+                                   void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * entmtp_kv_compact_paged over 4-bit pools: the rows' codes and scale bytes move
+ * as they are.  layer_stride: bytes from layer to layer, a multiple of 16.
+ * Requirements: d == ENTMTP_HEAD_DIM, 16-byte aligned pools.
+ * Errors (host-checked): EINVAL, ERANGE, EHIP.
+ */
+int32_t entmtp_kv_compact_paged_fp4(int32_t B, const int32_t* path, int32_t path_capacity,
+                                    const int32_t* accept_len, const int32_t* row_off,
+                                    const int32_t* slot_map, int32_t rows, uint8_t* k_pool,
+                                    uint8_t* v_pool, int32_t n_layers, int64_t layer_stride,
+                                    int32_t n_pages, int32_t Hkv, int32_t page_size, int32_t d,
+                                    void* stream);
 
 /*
  * Penalties, biases and grammar masks on the logits of a batch's tree rows,

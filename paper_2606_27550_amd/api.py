@@ -28,6 +28,7 @@ _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libentmtp.
 OK, EINVAL, ETREE, ERANGE, ENOSPC, EHIP, ETIMEDOUT = 0, -1, -2, -3, -4, -5, -6
 T_MAX, D_MAX, MASK_WORDS, HEAD_DIM, B_MAX = 256, 31, 8, 128, 16
 PAGED_B_MAX = 256
+FP4_ROW = 68   # bytes of a head's row in 4 bits
 PAGE_OK, PAGE_NONE, PAGE_RANGE, PAGE_FULL, PAGE_BAD = range(5)   # status of a mapped sequence
 
 _c_i32, _c_i64, _c_f32, _c_sz, _c_p = (ctypes.c_int32, ctypes.c_int64, ctypes.c_float,
@@ -79,6 +80,7 @@ _SIGNATURES = {
     "entmtp_kv_compact_batched_device": (_c_i32, [_c_i32, _c_p, _c_i32, _c_p, _c_p, _c_p, _c_p,
                                                   _c_i32, _c_i64, _c_i32, _c_i32, _c_i32, _c_p]),
     "entmtp_verify_logits": (_c_i32, [_c_p, _c_p, _c_i32, _c_i32, _c_i32, _c_p, _c_p]),
+    "entmtp_verify_logits_fp4": (_c_i32, [_c_p, _c_p, _c_p, _c_i32, _c_i32, _c_i32, _c_p, _c_p]),
     "entmtp_logit_stats": (_c_i32, [_c_p, _c_i32, _c_i32, _c_f32, _c_p, _c_p, _c_p, _c_p]),
     "entmtp_verify_logits_stats_workspace": (_c_sz, [_c_i32, _c_i32, _c_i32]),
     "entmtp_stats_partials_bytes": (_c_sz, [_c_i32, _c_i32, _c_i32]),
@@ -111,6 +113,20 @@ _SIGNATURES = {
                                [_c_f32, _c_f32, _c_f32, _c_i32, _c_p, _c_p, _c_p, _c_sz, _c_p]),
     "entmtp_kv_compact_paged": (_c_i32, [_c_i32, _c_p, _c_i32, _c_p, _c_p, _c_p, _c_i32, _c_p, _c_p,
                                          _c_i32, _c_i64, _c_i32, _c_i32, _c_i32, _c_i32, _c_p]),
+    "entmtp_quantize_fp4": (_c_i32, [_c_p, _c_i64, _c_i32, _c_p, _c_p, _c_p]),
+    "entmtp_tree_positions": (_c_i32, [_c_p, _c_i32, _c_p, _c_p, _c_p, _c_i32, _c_p, _c_p]),
+    "entmtp_kv_append_paged": (_c_i32, [_c_p, _c_i64] * 3 + [_c_i32] * 4 + [_c_p] * 4 + [_c_f32, _c_f32] +
+                               [_c_p] * 3 + [_c_i32, _c_i32] + [_c_p] * 3),
+    "entmtp_kv_append_paged_fp4": (_c_i32, [_c_p, _c_i64] * 3 + [_c_i32] * 4 + [_c_p] * 4 + [_c_f32, _c_f32] +
+                                   [_c_p] * 3 + [_c_i32, _c_i32] + [_c_p] * 3),
+    "entmtp_tree_attn_paged_fp4_plan_bytes": (_c_sz, [_c_p] + [_c_i32] * 6),
+    "entmtp_tree_attn_paged_fp4_plan": (_c_i32, [_c_p, _c_i32] + [_c_p] * 5 + [_c_i32] * 7 +
+                                        [_c_p, _c_p, _c_sz, _c_p]),
+    "entmtp_tree_attn_paged_fp4_workspace": (_c_sz, [_c_p] + [_c_i32] * 7),
+    "entmtp_tree_attn_paged_fp4": (_c_i32, [_c_p, _c_i32, _c_p, _c_sz] + [_c_p] * 3 + [_c_i32, _c_i32, _c_p] +
+                                   [_c_i32] * 5 + [_c_f32, _c_f32, _c_i32, _c_p, _c_p, _c_p, _c_sz, _c_p]),
+    "entmtp_kv_compact_paged_fp4": (_c_i32, [_c_i32, _c_p, _c_i32, _c_p, _c_p, _c_p, _c_i32, _c_p, _c_p,
+                                             _c_i32, _c_i64, _c_i32, _c_i32, _c_i32, _c_i32, _c_p]),
     "entmtp_logit_adjust_workspace": (_c_sz, [_c_i32, _c_i32]),
     "entmtp_logit_adjust": (_c_i32, [_c_p, _c_i32, _c_p, _c_p, _c_i32, _c_p, _c_p, _c_i32, _c_p, _c_p,
                                      _c_p, _c_i32, _c_p, _c_p, _c_i32, _c_i32, _c_p, _c_p, _c_p, _c_p,
@@ -537,6 +553,19 @@ def verify_logits(hidden, w_lm, logits, stream=None) -> None:
     _check(lib.entmtp_verify_logits(_p(hidden), _p(w_lm), T, hid, V, _p(logits), _stream(stream)))
 
 
+def verify_logits_fp4(hidden, codes, scales, logits, stream=None) -> None:
+    """hidden [T, hid] bf16, weights of quantize_fp4 (uint8 [V, hid / 2] and
+    [V, hid / 32]) -> logits [T, V] fp32."""
+    T, hid = _dims(hidden, "hidden", 2)
+    V, _ = _dims(codes, "codes", 2)
+    dev = _device(hidden, "hidden")
+    _need(hid % 32 == 0, "hidden is [T, hid] with hid a multiple of 32")
+    _check(lib.entmtp_verify_logits_fp4(_at(hidden, "hidden", _torch.bfloat16, (T, hid), dev),
+                                        _at(codes, "codes", _torch.uint8, (V, hid // 2), dev),
+                                        _at(scales, "scales", _torch.uint8, (V, hid // 32), dev), T, hid, V,
+                                        _at(logits, "logits", _torch.float32, (T, V), dev), _stream_on(stream, dev)))
+
+
 def verify_logits_stats_workspace(T: int, hid: int, V: int) -> int:
     return int(lib.entmtp_verify_logits_stats_workspace(T, hid, V))
 
@@ -924,6 +953,165 @@ def kv_compact_paged(path, accept_len, row_off, slot_map, k_pool, v_pool, stream
                                        _at(v_pool, "v_pool", bf, shape, dev),
                                        1 if len(shape) == 4 else shape[0], n_pages * Hkv * page * d,
                                        n_pages, Hkv, page, d, _stream_on(stream, dev)))
+
+
+# New rows on their way into the pool, and pools and weights in 4 bits.
+
+def quantize_fp4(x, codes, scales, stream=None) -> None:
+    """x [rows, n] bf16 -> codes uint8 [rows, n / 2] and scale bytes uint8 [rows, n / 32]."""
+    rows, n = _dims(x, "x", 2)
+    dev = _device(x, "x")
+    _need(n % 32 == 0, "x is [rows, n] with n a multiple of 32")
+    _check(lib.entmtp_quantize_fp4(_at(x, "x", _torch.bfloat16, (rows, n), dev), rows, n,
+                                   _at(codes, "codes", _torch.uint8, (rows, n // 2), dev),
+                                   _at(scales, "scales", _torch.uint8, (rows, n // 32), dev),
+                                   _stream_on(stream, dev)))
+
+
+def tree_positions(bank: Bank, topo, prefix_len, row_off, pos, stream=None) -> None:
+    """pos int32 [rows] of the step's tree rows: prefix_len[b] + the node's
+    depth, -1 in rows without one (topo: tree_attn_paged_topo(plan, B))."""
+    i32 = _torch.int32
+    B = _paged_batch(topo)
+    dev = _device(topo, "topo")
+    at, rows = _flat(pos, "pos", i32, dev)
+    _check(lib.entmtp_tree_positions(bank.handle, B, _at(topo, "topo", i32, (B,), dev),
+                                     _at(prefix_len, "prefix_len", i32, (B,), dev),
+                                     _at(row_off, "row_off", i32, (B + 1,), dev), rows, at,
+                                     _stream_on(stream, dev)))
+
+
+def _heads(t, name, dtype, dev):
+    """Pointer, row stride and heads of a tensor [rows, heads, d] whose rows are
+    dense (a part of a projection's output)."""
+    rows, H, d = _dims(t, name, 3)
+    _need(t.dtype is dtype and t.get_device() == dev, f"{name} must be {dtype} on the current device, cuda:{dev}")
+    step, head, one = t.stride()
+    _need((one == 1 or d <= 1) and (head == d or H <= 1) and (rows <= 1 or step >= H * d),
+          f"{name} must have dense rows that do not overlap")
+    return t.data_ptr(), (step if rows > 1 else -(-H * d // 8) * 8), H
+
+
+def _append(call, pool_dtype, page_of, q, k, v, pos, slot_map, rope_theta, q_out, k_pool, v_pool, q_norm, k_norm, eps,
+            k_out, v_out, stream):
+    bf, i32 = _torch.bfloat16, _torch.int32
+    rows, Hkv, d = _dims(k, "k", 3)
+    _need(_dims(v, "v", 3) == k.shape, "v has k's shape")
+    dev = _device(k, "k")
+    _need((q is None) == (q_out is None), "q and q_out go together")
+    qp, qs, Hq = (None, 0, 0) if q is None else _heads(q, "q", bf, dev)
+    _need(q is None or (q.shape[0] == rows and q.shape[2] == d), "q is [rows, Hq, d] with k's rows and d")
+    kp, ks, _ = _heads(k, "k", bf, dev)
+    vp, vs, _ = _heads(v, "v", bf, dev)
+    shape = getattr(k_pool, "shape", ())
+    n_pages, page = page_of(shape, Hkv, d)
+    weight = lambda t, name: None if t is None else _at(t, name, bf, (d,), dev)   # noqa: E731
+    held = lambda t, name: None if t is None else _at(t, name, bf, (rows, Hkv, d), dev)   # noqa: E731
+    _check(call(qp, qs, kp, ks, vp, vs, rows, Hq, Hkv, d, _at(pos, "pos", i32, (rows,), dev),
+                _at(slot_map, "slot_map", i32, (rows,), dev), weight(q_norm, "q_norm"), weight(k_norm, "k_norm"), eps,
+                rope_theta, None if q is None else _at(q_out, "q_out", bf, (rows, Hq, d), dev),
+                _at(k_pool, "k_pool", pool_dtype, shape, dev), _at(v_pool, "v_pool", pool_dtype, shape, dev), n_pages,
+                page, held(k_out, "k_out"), held(v_out, "v_out"), _stream_on(stream, dev)))
+
+
+def _page16(shape, Hkv, d):
+    _need(len(shape) == 4 and shape[1] == Hkv and shape[3] == d, "pools are [n_pages, Hkv, page_size, d]")
+    return shape[0], shape[2]
+
+
+def _page4(shape, Hkv, d):
+    _need(len(shape) == 3 and shape[1] == Hkv and shape[2] % FP4_ROW == 0,
+          f"4-bit pools are [n_pages, Hkv, page_size * {FP4_ROW}]")
+    return shape[0], shape[2] // FP4_ROW
+
+
+def kv_append_paged(q, k, v, pos, slot_map, rope_theta: float, q_out, k_pool, v_pool, q_norm=None, k_norm=None,
+                    eps: float = 1e-6, k_out=None, v_out=None, stream=None) -> None:
+    """q [rows, Hq, d] (or None), k, v [rows, Hkv, d] bf16, rows dense at any
+    stride; pos, slot_map int32 [rows]; q_norm, k_norm bf16 [d] or None; q_out
+    [rows, Hq, d]; pools bf16 [n_pages, Hkv, page_size, d]; k_out, v_out
+    [rows, Hkv, d] or None."""
+    _append(lib.entmtp_kv_append_paged, _torch.bfloat16, _page16, q, k, v, pos, slot_map, rope_theta, q_out, k_pool,
+            v_pool, q_norm, k_norm, eps, k_out, v_out, stream)
+
+
+def kv_append_paged_fp4(q, k, v, pos, slot_map, rope_theta: float, q_out, k_pool, v_pool, q_norm=None, k_norm=None,
+                        eps: float = 1e-6, k_out=None, v_out=None, stream=None) -> None:
+    """kv_append_paged into 4-bit pools, uint8 [n_pages, Hkv, page_size * FP4_ROW]."""
+    _append(lib.entmtp_kv_append_paged_fp4, _torch.uint8, _page4, q, k, v, pos, slot_map, rope_theta, q_out, k_pool,
+            v_pool, q_norm, k_norm, eps, k_out, v_out, stream)
+
+
+def tree_attn_paged_fp4_plan_bytes(bank: Bank, B: int, rows_cap: int, Hq: int, Hkv: int, max_pages: int,
+                                   page_size: int) -> int:
+    return int(lib.entmtp_tree_attn_paged_fp4_plan_bytes(bank.handle, B, rows_cap, Hq, Hkv, max_pages, page_size))
+
+
+def tree_attn_paged_fp4_plan(bank: Bank, topo, prefix_len, row_off, status, block_table, page_size: int,
+                             n_pages: int, rows_cap: int, Hq: int, Hkv: int, plan, window: int = 0,
+                             bad=None, stream=None) -> None:
+    """tree_attn_paged_plan for 4-bit pools (tree_attn_paged_topo reads either plan)."""
+    i32 = _torch.int32
+    B = _paged_batch(topo)
+    _, max_pages = _dims(block_table, "block_table", 2)
+    dev = _device(topo, "topo")
+    plan_p, size = _scratch(plan, "plan", dev)
+    _check(lib.entmtp_tree_attn_paged_fp4_plan(bank.handle, B, _at(topo, "topo", i32, (B,), dev),
+                                               _at(prefix_len, "prefix_len", i32, (B,), dev),
+                                               _at(row_off, "row_off", i32, (B + 1,), dev),
+                                               _at(status, "status", i32, (B,), dev),
+                                               _at(block_table, "block_table", i32, (B, max_pages), dev),
+                                               max_pages, page_size, n_pages, rows_cap, Hq, Hkv, window,
+                                               None if bad is None else _at(bad, "bad", i32, (B,), dev),
+                                               plan_p, size, _stream_on(stream, dev)))
+
+
+def tree_attn_paged_fp4_workspace(bank: Bank, B: int, rows_cap: int, Hq: int, Hkv: int, d: int, max_pages: int,
+                                  page_size: int) -> int:
+    return int(lib.entmtp_tree_attn_paged_fp4_workspace(bank.handle, B, rows_cap, Hq, Hkv, d, max_pages, page_size))
+
+
+def tree_attn_paged_fp4(bank: Bank, plan, q, k_pool, v_pool, block_table, scale: float, out, workspace,
+                        softcap: float = 0.0, window: int = 0, slopes=None, stream=None) -> None:
+    """q (kv_append_paged_fp4's q_out), out [rows_cap, Hq, d] bf16, pools uint8
+    [n_pages, Hkv, page_size * FP4_ROW] that hold the tree's rows already,
+    block_table int32 [B, max_pages]; plan of tree_attn_paged_fp4_plan, of the
+    same sizes and window; slopes fp32 [Hq] or None."""
+    bf, i32, u8 = _torch.bfloat16, _torch.int32, _torch.uint8
+    rows, Hq, d = _dims(q, "q", 3)
+    n_pages, Hkv, size = _dims(k_pool, "k_pool", 3)
+    _need(size % FP4_ROW == 0, f"4-bit pools are [n_pages, Hkv, page_size * {FP4_ROW}]")
+    B, max_pages = _dims(block_table, "block_table", 2)
+    dev = _device(q, "q")
+    plan_p, plan_size = _scratch(plan, "plan", dev)
+    ws, ws_size = (None, 0) if workspace is None else _scratch(workspace, "workspace", dev)
+    _check(lib.entmtp_tree_attn_paged_fp4(bank.handle, B, plan_p, plan_size, _at(q, "q", bf, (rows, Hq, d), dev),
+                                          _at(k_pool, "k_pool", u8, (n_pages, Hkv, size), dev),
+                                          _at(v_pool, "v_pool", u8, (n_pages, Hkv, size), dev), n_pages, size // FP4_ROW,
+                                          _at(block_table, "block_table", i32, (B, max_pages), dev), max_pages,
+                                          rows, Hq, Hkv, d, scale, softcap, window,
+                                          None if slopes is None else _at(slopes, "slopes", _torch.float32, (Hq,), dev),
+                                          _at(out, "out", bf, (rows, Hq, d), dev), ws, ws_size,
+                                          _stream_on(stream, dev)))
+
+
+def kv_compact_paged_fp4(path, accept_len, row_off, slot_map, k_pool, v_pool, stream=None) -> None:
+    """kv_compact_paged over 4-bit pools, uint8 [n_pages, Hkv, page_size *
+    FP4_ROW] (one layer) or [n_layers, n_pages, Hkv, page_size * FP4_ROW]."""
+    i32, u8 = _torch.int32, _torch.uint8
+    B, path_cap = _dims(path, "path", 2)
+    _need(1 <= B <= PAGED_B_MAX, f"path is [B, path_capacity] with 1 <= B <= {PAGED_B_MAX}")
+    shape = _dims(k_pool, "pools", 3, 4)
+    n_pages, Hkv, size = shape[-3:]
+    _need(size % FP4_ROW == 0, f"4-bit pools are [n_pages, Hkv, page_size * {FP4_ROW}]")
+    dev = _device(path, "path")
+    slots, rows = _flat(slot_map, "slot_map", i32, dev)
+    _check(lib.entmtp_kv_compact_paged_fp4(B, _at(path, "path", i32, (B, path_cap), dev), path_cap,
+                                           _at(accept_len, "accept_len", i32, (B,), dev),
+                                           _at(row_off, "row_off", i32, (B + 1,), dev), slots, rows,
+                                           _at(k_pool, "k_pool", u8, shape, dev), _at(v_pool, "v_pool", u8, shape, dev),
+                                           1 if len(shape) == 3 else shape[0], n_pages * Hkv * size, n_pages, Hkv,
+                                           size // FP4_ROW, HEAD_DIM, _stream_on(stream, dev)))
 
 
 def logit_adjust_workspace(rows: int, V: int) -> int:

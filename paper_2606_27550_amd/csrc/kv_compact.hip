@@ -9,6 +9,7 @@
 // registers before writing any.  The accept length is read on the device, so
 // the host does not wait for the verification result.
 #include "common.hpp"
+#include "fp4.hpp"
 #include "paged.hpp"
 
 namespace entmtp {
@@ -162,6 +163,59 @@ __global__ __launch_bounds__(kCompactThreads) void kv_compact_paged_kernel(Compa
   u32x4 val[ROWS];
   // (four rows at a time without a branch between their loads: a row that does
   // not move reads slot 0)
+#pragma unroll
+  for (int k = 0; k < ROWS; ++k)
+    if ((k / 4 == 0 || k / 4 * 4 <= a) && live) val[k] = *at(max(__builtin_amdgcn_readlane(src, k), 0));
+#pragma unroll
+  for (int k = 0; k < ROWS; ++k)
+    if (__builtin_amdgcn_readlane(src, k) >= 0 && live) *at(__builtin_amdgcn_readlane(dst, k)) = val[k];
+}
+
+// The same over a 4-bit pool: a row is 16 words of codes and a word of scale
+// bytes, a thread owns one word column.  (Columns of 16 bytes would leave a
+// row's scale word a column of its own kind in every wavefront.)
+struct CompactFp4Args {
+  uint8_t* kp;   // [n_layers] pools [n_pages][Hkv][P x 68], layer_stride apart
+  uint8_t* vp;
+  const int* path;
+  const int* accept_len;
+  const int* row_off;    // [B + 1]
+  const int* slot_map;   // [rows]
+  long long layer_stride;
+  int path_cap, rows, Hkv, shift, n_slots, groups;
+};
+
+template <int ROWS>
+__global__ __launch_bounds__(kCompactThreads) void kv_compact_fp4_kernel(CompactFp4Args p) {
+  constexpr int kCodeBytes = ENTMTP_HEAD_DIM / 2, kCodeWords = kCodeBytes / 4, kWords = kFp4RowBytes / 4;
+  const int b = blockIdx.y, layer = blockIdx.x / p.groups;
+  const int t = threadIdx.x, j = min(t & 63, ROWS - 1);
+  int a = p.accept_len[b];
+  const int r0 = p.row_off[b], r1 = p.row_off[b + 1];
+  int node = p.path[static_cast<size_t>(b) * p.path_cap + min(j, p.path_cap - 1)];
+  asm volatile("" : "+v"(node));
+  a = min(a, min(p.path_cap, ROWS) - 1);
+  if (a < 0) return;   // not verified (uniform)
+  int src = -1, dst = -1;
+  const int n = min(r1, p.rows) - r0;
+  if (j <= a && r0 >= 0 && node >= 0 && node < n && j < n && node != j) {
+    src = p.slot_map[r0 + node];
+    dst = p.slot_map[r0 + j];
+    if (src >= p.n_slots || dst < 0 || dst >= p.n_slots) src = -1;
+  }
+  const int per_tensor = p.Hkv * kWords;
+  const int col = (blockIdx.x % p.groups) * kCompactThreads + t;
+  const bool live = col < 2 * per_tensor;
+  uint8_t* const pool = (col >= per_tensor ? p.vp : p.kp) + layer * p.layer_stride;
+  const int g = col % per_tensor / kWords, w = col % kWords;   // (per_tensor is a multiple of kWords)
+  const int P = 1 << p.shift;
+  uint8_t* const mine = pool + static_cast<size_t>(g) * P * kFp4RowBytes + (w < kCodeWords ? 4 * w : (kCodeBytes << p.shift));
+  const int step = w < kCodeWords ? kCodeBytes : kFp4RowBytes - kCodeBytes;   // from row to row
+  auto at = [&](int slot) {   // (slot is uniform)
+    const size_t page = slot >> p.shift;
+    return reinterpret_cast<uint32_t*>(mine + page * p.Hkv * P * kFp4RowBytes + (slot & (P - 1)) * step);
+  };
+  uint32_t val[ROWS];
 #pragma unroll
   for (int k = 0; k < ROWS; ++k)
     if ((k / 4 == 0 || k / 4 * 4 <= a) && live) val[k] = *at(max(__builtin_amdgcn_readlane(src, k), 0));
@@ -357,4 +411,47 @@ extern "C" int32_t entmtp_kv_compact_paged(int32_t B, const int32_t* path, int32
   static_assert(ENTMTP_D_MAX + 1 <= 32, "the longest path");
   path_capacity <= 16 ? go(kv_compact_paged_kernel<16>) : go(kv_compact_paged_kernel<32>);
   return launch_status("kv_compact_paged launch");
+}
+
+extern "C" int32_t entmtp_kv_compact_paged_fp4(int32_t B, const int32_t* path, int32_t path_capacity,
+                                               const int32_t* accept_len, const int32_t* row_off,
+                                               const int32_t* slot_map, int32_t rows, uint8_t* k_pool, uint8_t* v_pool,
+                                               int32_t n_layers, int64_t layer_stride, int32_t n_pages, int32_t Hkv,
+                                               int32_t page_size, int32_t d, void* stream) {
+  clear_error();
+  ENTMTP_CHECK_ARG(paged_batch(B), ENTMTP_EINVAL, "B = %d outside [1, %d]", B, ENTMTP_PAGED_B_MAX);
+  ENTMTP_CHECK_ARG(path && accept_len && row_off && slot_map && k_pool && v_pool, ENTMTP_EINVAL,
+                   "path, accept_len, row_off, slot_map and pools must be non-NULL");
+  ENTMTP_CHECK_ARG(path_capacity >= 1 && rows >= 1, ENTMTP_EINVAL, "path_capacity = %d, rows = %d must be >= 1",
+                   path_capacity, rows);
+  if (int32_t rc = check_pool(n_pages, page_size)) return rc;
+  ENTMTP_CHECK_ARG(n_layers >= 1 && Hkv >= 1, ENTMTP_EINVAL, "bad sizes (n_layers %d, Hkv %d)", n_layers, Hkv);
+  ENTMTP_CHECK_ARG(d == ENTMTP_HEAD_DIM, ENTMTP_EINVAL, "head dim %d unsupported (built for %d)", d, ENTMTP_HEAD_DIM);
+  ENTMTP_CHECK_ARG(Hkv <= 65536, ENTMTP_ERANGE, "Hkv = %d too large", Hkv);
+  ENTMTP_CHECK_ARG(n_layers == 1 || layer_stride >= static_cast<int64_t>(n_pages) * page_size * Hkv * kFp4RowBytes,
+                   ENTMTP_EINVAL, "layer_stride %lld smaller than one layer", static_cast<long long>(layer_stride));
+  ENTMTP_CHECK_ARG(layer_stride % 16 == 0, ENTMTP_EINVAL, "layer_stride must keep 16-byte alignment");
+  ENTMTP_CHECK_ARG(aligned16(k_pool) && aligned16(v_pool), ENTMTP_EINVAL, "pools must be 16-byte aligned");
+  CompactFp4Args a{};
+  a.kp = k_pool;
+  a.vp = v_pool;
+  a.path = path;
+  a.accept_len = accept_len;
+  a.row_off = row_off;
+  a.slot_map = slot_map;
+  a.layer_stride = static_cast<long long>(layer_stride);
+  a.path_cap = path_capacity;
+  a.rows = rows;
+  a.Hkv = Hkv;
+  a.shift = page_shift(page_size);
+  a.n_slots = n_pages * page_size;
+  a.groups = (2 * Hkv * (kFp4RowBytes / 4) + kCompactThreads - 1) / kCompactThreads;
+  const int64_t blocks = static_cast<int64_t>(n_layers) * a.groups;
+  ENTMTP_CHECK_ARG(blocks <= INT32_MAX, ENTMTP_ERANGE, "%d layers of %d heads: too many", n_layers, Hkv);
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(blocks), B), dim3(kCompactThreads), 0,
+                       static_cast<hipStream_t>(stream), a);
+  };
+  path_capacity <= 16 ? go(kv_compact_fp4_kernel<16>) : go(kv_compact_fp4_kernel<32>);
+  return launch_status("kv_compact_paged_fp4 launch");
 }

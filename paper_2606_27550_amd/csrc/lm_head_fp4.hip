@@ -1,0 +1,214 @@
+// LM-head logits from 4-bit weights: z = X W^T, W in codes and group scales.
+//
+// The weights stream past the hidden states, which stay in registers.  A
+// workgroup of eight wavefronts takes up to 32 rows of X; wavefront w keeps
+// every eighth 128-wide step of them and takes the same steps of each 16-row
+// tile of W: a lane's 16 bytes are 32 codes of one group, which become bf16
+// numbers, exactly, on the way into the matrix instruction (16 x 16 x 32), so
+// that the products are exact and the sums those of the bf16 LM head.  The eight
+// partial sums of a tile meet in the LDS.  (The matrix instruction that takes
+// codes as they are, with X as two 8-bit numbers, sums its 128 products to
+// 4.6e-6 of the logits' norm; this one to 1e-7.)
+//
+// Up to 32 rows the weights' bytes bound it.
+#include <algorithm>
+
+#include "fp4.hpp"
+#include "stream_pipe.hpp"
+
+namespace entmtp {
+namespace {
+
+constexpr int kLmWaves = 8, kLmThreads = 64 * kLmWaves;
+constexpr int kLmStep = 128;    // values a matrix instruction takes
+constexpr int kLmTile = 16;     // rows of W
+constexpr int kLmGroup = 4;     // tiles between reductions
+
+struct LmFp4Args {
+  const uint16_t* x;       // [T][hid]
+  const uint8_t* codes;    // [V][hid / 2]
+  const uint8_t* scales;   // [V][hid / 32]
+  float* out;              // [T][V]
+  int T, hid, V;
+  int tiles, per;          // tiles of W, per workgroup
+  int chunks;              // of X's rows
+  int k0;                  // first step of this pass over hid
+  int add;                 // a later pass adds to the earlier ones
+};
+
+// KS: steps a wavefront; NT: 16-row tiles of X; NBUF: tiles of W in flight and
+// in use.
+template <int KS, int NT, int NBUF>
+__global__ __launch_bounds__(kLmThreads, 2) void lm_fp4_kernel(LmFp4Args p) {
+  __shared__ __attribute__((aligned(16))) f32x4 s_part[2][kLmWaves][kLmGroup][NT][64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int li = lane & 15, blk = lane >> 4;
+  // the chunks of X that share a range of W follow each other on one XCD
+  const int grp = static_cast<int>(blockIdx.x) >> 3;
+  const int chunk = grp % p.chunks, slice = (grp / p.chunks) * 8 + (static_cast<int>(blockIdx.x) & 7);
+  const int t0 = slice * p.per, t1 = min(t0 + p.per, p.tiles);
+  if (t0 >= t1) return;
+  const int row0 = chunk * 16 * NT;
+  const int kw = p.k0 + wave;   // this wavefront's steps: kw, kw + 8, ..
+
+  // where lane (row li, block blk) finds step s's 32 values in a row of W
+  int coff[KS], soff[KS];
+  bool there[KS];
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    const int k = (kw + s * kLmWaves) * kLmStep + 32 * blk;
+    there[s] = k < p.hid;
+    coff[s] = there[s] ? k / 2 : 0;
+    soff[s] = there[s] ? k / 32 : 0;
+  }
+  u32x4 wb[NBUF][KS];
+  uint32_t sb[NBUF][KS];
+  const int crow = p.hid / 2, srow = p.hid / 32;
+  auto load = [&](int buf, int tile) {
+    const int v = min(min(tile, t1 - 1) * kLmTile + li, p.V - 1);
+    const uint8_t* const c = p.codes + static_cast<size_t>(v) * crow;
+    const uint8_t* const s8 = p.scales + static_cast<size_t>(v) * srow;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      wb[buf][s] = *reinterpret_cast<const u32x4*>(c + coff[s]);
+      sb[buf][s] = s8[soff[s]];
+    }
+  };
+#pragma unroll
+  for (int k = 0; k < NBUF - 1; ++k) load(k, t0 + k);
+
+  // this lane's part of X: row li of each tile, the same 32 values of a step
+  u32x4 xb[NT][KS][4];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int row = row0 + 16 * n + li;
+    const uint16_t* const xr = p.x + static_cast<size_t>(min(row, p.T - 1)) * p.hid;
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        xb[n][s][j] = *reinterpret_cast<const u32x4*>(xr + 2 * coff[s] + 8 * j);
+        if (!there[s]) xb[n][s][j] = u32x4{0u, 0u, 0u, 0u};
+      }
+  }
+
+  const bool wide = (p.V & 3) == 0;
+  auto compute = [&](int buf, int k, int par) {
+    f32x4 acc[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      // (past the row X is zero and W's first values stand in, as numbers)
+      const float step = __uint_as_float((there[s] ? sb[buf][s] : 127u) << 23);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bf16x8 a = as_bf16x8(fp4_values(wb[buf][s][j], step));
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+          acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, as_bf16x8(xb[n][s][j]), acc[n], 0, 0, 0);
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) s_part[par][wave][k][n][lane] = acc[n];
+  };
+  auto reduce = [&](int tile, int par) {   // of tiles tile .. + 3
+    for (int i = tid; i < kLmGroup * NT * 64; i += kLmThreads) {
+      const int l = i & 63, n = (i >> 6) % NT, k = i / (64 * NT);
+      f32x4 z = s_part[par][0][k][n][l];
+#pragma unroll
+      for (int w = 1; w < kLmWaves; ++w) z += s_part[par][w][k][n][l];
+      const int row = row0 + 16 * n + (l & 15), v = (tile + k) * kLmTile + 4 * (l >> 4);
+      if (row >= p.T || tile + k >= t1 || v >= p.V) continue;
+      float* const o = p.out + static_cast<size_t>(row) * p.V + v;
+      if (wide) {
+        f32x4* const o4 = reinterpret_cast<f32x4*>(o);
+        *o4 = p.add ? *o4 + z : z;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (v + e < p.V) o[e] = p.add ? o[e] + z[e] : z[e];
+      }
+    }
+  };
+  int par = 0;
+  static_assert(kLmGroup % NBUF == 0, "a tile's buffer is known");
+  for (int t = t0; t < t1; t += kLmGroup) {
+#pragma unroll
+    for (int k = 0; k < kLmGroup; ++k) {
+      load((k + NBUF - 1) % NBUF, t + k + NBUF - 1);
+      compute(k % NBUF, k, par);
+    }
+    // (the other half is written while this one is read: one barrier a group)
+    wait_lds();
+    stage_barrier();
+    reduce(t, par);
+    par ^= 1;
+  }
+}
+
+}  // namespace
+}  // namespace entmtp
+
+using namespace entmtp;
+
+extern "C" int32_t entmtp_verify_logits_fp4(const entmtp_bf16* hidden, const uint8_t* codes, const uint8_t* scales,
+                                            int32_t T, int32_t hid, int32_t V, float* logits, void* stream) {
+  clear_error();
+  ENTMTP_CHECK_ARG(hidden && codes && scales && logits, ENTMTP_EINVAL, "hidden, codes, scales and logits must be non-NULL");
+  ENTMTP_CHECK_ARG(T >= 1 && T <= 4096, ENTMTP_EINVAL, "T = %d outside [1, 4096]", T);
+  ENTMTP_CHECK_ARG(hid >= kFp4Group && hid % kFp4Group == 0 && hid <= 65536, ENTMTP_EINVAL,
+                   "hid = %d must be a multiple of %d up to 65536", hid, kFp4Group);
+  ENTMTP_CHECK_ARG(V >= 1 && V <= INT32_MAX - 4096, ENTMTP_EINVAL, "V = %d out of range", V);
+  ENTMTP_CHECK_ARG(aligned16(hidden) && aligned16(codes) && aligned16(logits), ENTMTP_EINVAL,
+                   "hidden, codes and logits must be 16-byte aligned");
+  int cus = 256, dev = 0;
+  if (hipGetDevice(&dev) == hipSuccess) (void)hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
+  LmFp4Args a{};
+  a.x = hidden;
+  a.codes = codes;
+  a.scales = scales;
+  a.out = logits;
+  a.T = T;
+  a.hid = hid;
+  a.V = V;
+  a.tiles = (V + kLmTile - 1) / kLmTile;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  const int steps = (hid + kLmStep - 1) / kLmStep;
+  // a pass over hid holds at most 8 steps a wavefront (5 where it has two tiles of X)
+  const int nt = T > 16 ? 2 : 1, most = nt == 2 ? 5 : 8;
+  const int passes = (steps + most * kLmWaves - 1) / (most * kLmWaves);
+  const int ks = ((steps + passes - 1) / passes + kLmWaves - 1) / kLmWaves;
+  a.chunks = (T + 16 * nt - 1) / (16 * nt);
+  const int slices = std::max(1, cus / a.chunks / 8) * 8;
+  a.per = (a.tiles + slices - 1) / slices;
+  const int used = (a.tiles + a.per - 1) / a.per;
+  const dim3 grid(static_cast<uint32_t>((used + 7) / 8 * 8 * a.chunks));
+  for (int pass = 0; pass < passes; ++pass) {
+    a.k0 = pass * ks * kLmWaves;
+    a.add = pass > 0;
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kLmThreads), 0, s, a); };
+    if (nt == 1) {
+      switch (ks) {
+        case 1: go(lm_fp4_kernel<1, 1, 4>); break;
+        case 2: go(lm_fp4_kernel<2, 1, 4>); break;
+        case 3: go(lm_fp4_kernel<3, 1, 4>); break;
+        case 4: go(lm_fp4_kernel<4, 1, 4>); break;
+        case 5: go(lm_fp4_kernel<5, 1, 2>); break;
+        case 6: go(lm_fp4_kernel<6, 1, 2>); break;
+        case 7: go(lm_fp4_kernel<7, 1, 2>); break;
+        default: go(lm_fp4_kernel<8, 1, 2>);
+      }
+    } else {
+      switch (ks) {
+        case 1: go(lm_fp4_kernel<1, 2, 4>); break;
+        case 2: go(lm_fp4_kernel<2, 2, 4>); break;
+        case 3: go(lm_fp4_kernel<3, 2, 2>); break;
+        case 4: go(lm_fp4_kernel<4, 2, 2>); break;
+        default: go(lm_fp4_kernel<5, 2, 2>);
+      }
+    }
+    if (int32_t rc = launch_status("verify_logits_fp4 launch")) return rc;
+  }
+  return ENTMTP_OK;
+}

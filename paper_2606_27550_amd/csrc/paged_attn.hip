@@ -44,66 +44,12 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "attn_tile.hpp"
-#include "paged.hpp"
+#include "paged_plan.hpp"
 
 namespace entmtp {
 namespace {
 
-constexpr int kPagedSplits = 128;
-constexpr int kMaxKvHeads = 256;   // (work lists are counted in 32 bits)
-constexpr float kMaxCap = 1024.f;
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kPlanThreads = kPagedSeqs;   // a thread per sequence
-constexpr int kPlanMagic = 0x50a6ed01;
-
-// First 64 bytes of a plan: what it was made for (the attention does nothing
-// with a plan of something else) and the length of its work list.
-struct PlanHeader {
-  int magic, B, Hq, Hkv, shift, n_pages, max_pages, rows_cap, window, items;
-  uint32_t bank_lo, bank_hi;
-  int pad[4];
-};
-static_assert(sizeof(PlanHeader) == 64, "plan layout");
-
-// A sequence as the merge finds it.
-struct PlanSeq {
-  int row0, T, nsplit, rows_pad;
-  long long part_off;   // row offset of its split partials
-  int pad[2];
-};
-static_assert(sizeof(PlanSeq) == 32, "plan layout");
-
-// One workgroup's work.
-struct PlanItem {
-  int T, L, row0, D;         // T = 0: nothing to do
-  int off_mask, off_depth;   // the tree, bytes into the bank's arena
-  int b, g, qg, split, nsplit, blk_lo, blk_hi, rows_pad;
-  uint32_t part_lo, part_hi;
-};
-static_assert(sizeof(PlanItem) == 64, "plan layout");
-
-// A plan: header, sequences, the tree of every sequence that has work (-1: none),
-// the sequence of every tree row (a byte each; only rows that hold one are
-// written, the reader checks it against the sequence's record), work items.
-size_t plan_topo_at(int B) { return sizeof(PlanHeader) + sizeof(PlanSeq) * B; }
-size_t plan_rows_at(int B) { return plan_topo_at(B) + sizeof(int) * B; }
-size_t plan_items_at(int B, int rows_cap) { return (plan_rows_at(B) + rows_cap + 63) / 64 * 64; }
-static_assert(kPagedSeqs <= 256, "a sequence is a byte");
-
-__host__ __device__ inline int paged_splits(int nb, int t) {
-  if (nb <= kLoneBlocks) return 1;
-  int bound = nb / kMinBlocksPerSplit;
-  bound = bound > kPagedSplits ? kPagedSplits : bound;
-  const int ns = (nb + t - 1) / t;
-  return ns < 1 ? 1 : (ns > bound ? bound : ns);
-}
-
-// First key block a tree at prefix length L reads: the root's window starts at
-// position L + 1 - window.
-__host__ __device__ inline int first_pos(int L, int window) {
-  return window > 0 && L >= window ? L + 1 - window : 0;
-}
 
 // What the last split's part of the tree costs beyond its blocks, in prefix
 // blocks: a table of fp64 angles and, for each of the ntree blocks with tree
@@ -128,6 +74,7 @@ struct PlanArgs {
   uint8_t* plan;
   long long topo_at, rows_at, items_at, part_cap;
   int B, G, Hq, Hkv, shift, n_pages, max_pages, rows_cap, window, slots, items_cap, two;
+  int fp4;   // a plan for 4-bit pools: the tree's rows lie in the pool like the prefix's
 };
 
 // ceil(nb / t) as paged_splits clips it: the quotient by t's reciprocal is off
@@ -254,7 +201,8 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs p) {
   const int sL = s_L;
   if (s_seq.T > 0) {
     const int* row = p.table + static_cast<size_t>(b) * p.max_pages;
-    for (int e = (first_pos(sL, p.window) >> p.shift) + tid; e < (sL + P - 1) >> p.shift; e += kPlanThreads) {
+    for (int e = (first_pos(sL, p.window) >> p.shift) + tid; e < (sL + (p.fp4 ? s_seq.T : 0) + P - 1) >> p.shift;
+         e += kPlanThreads) {
       const int id = row[e];
       bad |= id < 0 || id >= p.n_pages;
     }
@@ -264,7 +212,7 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs p) {
   const PagedTree& tree = p.trees.t[s_tree];
   const int sns = s_seq.nsplit, sblk = s_nb0;
   const int snb = (sL + s_seq.T + KB - 1) / KB - sblk, sqg = query_groups(s_seq.rows_pad / kQTile);
-  const int extra = sT > 0 ? paged_tree_extra(snb, snb - (sL / KB - sblk), sns) : 0;
+  const int extra = sT > 0 && !p.fp4 ? paged_tree_extra(snb, snb - (sL / KB - sblk), sns) : 0;
   PlanItem* const list = reinterpret_cast<PlanItem*>(p.plan + p.items_at) + s_item0;
   // where split c begins: c (snb + extra) / sns, without the product's 33 bits
   const int share = (snb + extra) / sns, rest = (snb + extra) % sns;
@@ -303,7 +251,7 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs p) {
     if (p.bad) p.bad[b] = bad != 0;
     if (b == 0) {
       PlanHeader h{};
-      h.magic = kPlanMagic;
+      h.magic = p.fp4 ? kPlanMagicFp4 : kPlanMagic;
       h.B = p.B;
       h.Hq = p.Hq;
       h.Hkv = p.Hkv;
@@ -322,8 +270,7 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PlanArgs p) {
 
 // ---------------------------------------------------------------- attend --
 
-struct PagedArgs {
-  const uint8_t* plan;
+struct PagedArgs : PagedCall {
   const uint8_t* arena;
   const int* table;      // [B][max_pages]
   const int* slot_map;   // [rows_cap]
@@ -333,42 +280,10 @@ struct PagedArgs {
   const uint16_t* vt;
   uint16_t* kp;          // [n_pages][Hkv][P][HD]
   uint16_t* vp;
-  // [part rows][HD]: the split's output, normalised by its sum so that it stays
-  // within its values' range, in bf16: in fp32 the whole output's error against
-  // 64 bits is 3.4-3.5e-3 instead of 3.7-3.9e-3 (the weights' and the query's
-  // roundings stay), and the bytes cost 3-6 % of long prefixes and windows, 15 % of 26
-  // nodes at 8192 (21.5 -> 24.7 us)
-  uint16_t* part_o;
-  float* part_ml;        // [part rows][2]
-  uint16_t* out;         // [rows_cap][Hq][HD]
-  long long rows_at, items_at;
-  uint64_t bank;         // the bank's number
-  int B, G, Hq, Hkv, shift, n_pages, max_pages, rows_cap, window;
   float q_scale;     // scale log2(e), or with a cap 2 log2(e) scale / cap: of the rotated query, or the products
   float cap_log2;    // cap log2(e), 0: no cap
   double freq[kRopePairs];   // of the rotation's pairs
 };
-
-// Memory that earlier kernels wrote and this one only reads, by scalar loads.
-template <typename T>
-using Const = const __attribute__((address_space(4))) T*;
-template <typename T>
-__device__ __forceinline__ Const<T> as_const(const void* p) {
-  return (Const<T>)reinterpret_cast<uintptr_t>(p);
-}
-
-// A 64-byte record in one scalar load (field by field behind branches, a
-// header took a dozen round trips).
-typedef int i32x16 __attribute__((ext_vector_type(16)));
-__device__ __forceinline__ i32x16 record(const uint8_t* p) { return *as_const<i32x16>(p); }
-
-// Whether a plan's header h says that it was made for this call.
-__device__ __forceinline__ bool plan_is_ours(const PagedArgs& p, const PlanHeader& h) {
-  return ((h.magic ^ kPlanMagic) | (h.B ^ p.B) | (h.Hq ^ p.Hq) | (h.Hkv ^ p.Hkv) | (h.shift ^ p.shift) |
-          (h.n_pages ^ p.n_pages) | (h.max_pages ^ p.max_pages) | (h.rows_cap ^ p.rows_cap) | (h.window ^ p.window) |
-          static_cast<int>(h.bank_lo ^ static_cast<uint32_t>(p.bank)) |
-          static_cast<int>(h.bank_hi ^ static_cast<uint32_t>(p.bank >> 32))) == 0;
-}
 
 // A pair of bf16 values with those that are not finite as zeros (odd is set).
 __device__ __forceinline__ uint32_t finite_pair(uint32_t w, bool& odd) {
@@ -900,170 +815,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
     }
 }
 
-// ----------------------------------------------------------------- merge --
-
-// LANES threads (half a wavefront or a whole one) take a query head of a tree
-// row: lane c reads the (max, sum) of splits c, c + LANES, .., and each 32 lanes
-// hold the head's dims, four a lane, of kMergeAhead splits at a time -- a whole
-// wavefront's halves of 16 splits each, summed up at the end.  The first partial
-// outputs are requested with the (max, sum) pairs.  The row's sequence is found
-// by scalar loads: its number, then its record.
-// Round trips and little data: 512 rows of 32 heads in four splits take 8 us with
-// the launch.
-constexpr int kMergeThreads = 256;
-constexpr int kMergeAhead = 16;
-
-template <int LANES>
-__global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedArgs p) {
-  constexpr int kHeads = kMergeThreads / LANES;
-  constexpr int kPairs = kPagedSplits / LANES;   // (max, sum) pairs a lane
-  constexpr int kRound = LANES / 32 * kMergeAhead;
-  static_assert(LANES % kRound == 0, "a round's weights lie in one register");
-  const int groups = (p.Hq + kHeads - 1) / kHeads;
-  const int r = static_cast<int>(blockIdx.x) / groups;   // (below rows_cap, by the grid)
-  const int h = static_cast<int>(blockIdx.x) % groups * kHeads + threadIdx.x / LANES;
-  const i32x16 head = record(p.plan);
-  const size_t byte = static_cast<size_t>(p.rows_at) + r;
-  const uint32_t word = *as_const<uint32_t>(p.plan + (byte & ~size_t(3)));
-  const int b = min(static_cast<int>(word >> (8 * (byte & 3)) & 0xffu), p.B - 1);
-  typedef int i32x8 __attribute__((ext_vector_type(8)));
-  const PlanSeq sq =
-      __builtin_bit_cast(PlanSeq, *as_const<i32x8>(p.plan + sizeof(PlanHeader) + static_cast<size_t>(b) * sizeof(PlanSeq)));
-  if (!plan_is_ours(p, __builtin_bit_cast(PlanHeader, head)) | (r < sq.row0) | (r >= sq.row0 + sq.T) | (sq.nsplit == 1))
-    return;   // (a row of no sequence, or written by the attention)
-  if (h >= p.Hq) return;
-  const int nsplit = sq.nsplit, lane = threadIdx.x % LANES;
-  const int first = lane / 32 * kMergeAhead;   // this half's splits of a round
-  const int row = (h % p.G) * sq.T + (r - sq.row0);
-  const size_t base = sq.part_off + static_cast<size_t>(h / p.G) * sq.rows_pad + row;
-  const size_t stride = static_cast<size_t>(p.Hkv) * sq.rows_pad;   // from split to split
-  const uint16_t* const po = p.part_o + base * HD + 4 * (lane & 31);
-  float m[kPairs], l[kPairs];
-#pragma unroll
-  for (int k = 0; k < kPairs; ++k) {
-    m[k] = -INFINITY;
-    l[k] = 0.f;
-    if (lane + LANES * k < nsplit) {
-      const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + (base + (lane + LANES * k) * stride) * 2);
-      m[k] = ml.x;
-      l[k] = ml.y;
-    }
-  }
-  // (kBatch at a time without a branch between them: a split past the last is
-  // that one again, at no weight)
-  constexpr int kBatch = LANES == 64 ? kMergeAhead : 4;
-  uint2 ob[kMergeAhead];
-  auto request = [&](int c) {
-#pragma unroll
-    for (int k = 0; k < kMergeAhead; ++k)
-      if (k / kBatch == 0 || c + k / kBatch * kBatch < nsplit)
-        ob[k] = *reinterpret_cast<const uint2*>(po + min(c + first + k, nsplit - 1) * stride * HD);
-  };
-  request(0);
-  float M = m[0];
-#pragma unroll
-  for (int k = 1; k < kPairs; ++k) M = fmaxf(M, m[k]);
-#pragma unroll
-  for (int off = LANES / 2; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, LANES));
-  // (a split that sees no key of the row has max -inf and counts for nothing;
-  // where M is -inf too the row has a NaN score, kept in a sum)
-  float lsum = 0.f;
-#pragma unroll
-  for (int k = 0; k < kPairs; ++k) {
-    l[k] = m[k] == -INFINITY ? l[k] : l[k] * __builtin_amdgcn_exp2f(m[k] - M);
-    lsum += l[k];
-  }
-#pragma unroll
-  for (int off = LANES / 2; off >= 1; off >>= 1) lsum += __shfl_xor(lsum, off, LANES);
-  const float inv = 1.f / lsum;
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int c = 0; c < nsplit; c += kRound) {
-    if (c > 0) request(c);
-    float w = l[0];   // the splits' weights, lane s % LANES holding split s's
-#pragma unroll
-    for (int k = 1; k < kPairs; ++k) w = c >= LANES * k ? l[k] : w;   // (0 past the last split)
-#pragma unroll
-    for (int k = 0; k < kMergeAhead; ++k) {
-      const float wc = __shfl(w, (c + first + k) % LANES, LANES);
-      if (k / kBatch == 0 || c + k / kBatch * kBatch < nsplit) {
-        const uint2 v = c + first + k < nsplit ? ob[k] : uint2{0u, 0u};   // (the last one again may hold infinities)
-        acc.x = fmaf(wc, __uint_as_float(v.x << 16), acc.x);
-        acc.y = fmaf(wc, __uint_as_float(v.x & 0xffff0000u), acc.y);
-        acc.z = fmaf(wc, __uint_as_float(v.y << 16), acc.z);
-        acc.w = fmaf(wc, __uint_as_float(v.y & 0xffff0000u), acc.w);
-      }
-    }
-  }
-  if constexpr (LANES == 64) {
-    acc.x += __shfl_xor(acc.x, 32, 64);
-    acc.y += __shfl_xor(acc.y, 32, 64);
-    acc.z += __shfl_xor(acc.z, 32, 64);
-    acc.w += __shfl_xor(acc.w, 32, 64);
-    if (lane >= 32) return;
-  }
-  const uint2 pk = {__builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{acc.x * inv, acc.y * inv}), bf16x2)),
-                    __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{acc.z * inv, acc.w * inv}), bf16x2))};
-  *reinterpret_cast<uint2*>(p.out + (static_cast<size_t>(r) * p.Hq + h) * HD + 4 * lane) = pk;
-}
-
 // ------------------------------------------------------------------ host --
-
-size_t up256(size_t x) { return (x + 255) & ~size_t(255); }
-
-// What a batch of these sizes can need at most, wherever its rows lie apart
-// from each other.  A sequence has ceil(G T / 128) query groups, so the groups
-// number at most rows G / 128 + B, the streams (KV heads x groups) Hkv times
-// that; a split target t gives ceil(nb / t) <= nb / t + 1 splits, so the items
-// stay below work / t + streams, and t is at least the even share (half of it
-// where two rounds are allowed).  A (KV head, split) range is padded to eight.
-struct PagedShape {
-  int items = 0;
-  bool two = false, splits = false;
-  long long part_rows = 0;
-  size_t plan_bytes = 0, workspace = 0;
-};
-
-PagedShape paged_shape(const entmtp_bank* bank, int B, int rows_cap, int Hq, int Hkv, long long cap) {
-  PagedShape sh;
-  const int G = Hq / Hkv, slots = device_cus() * kWgPerCu;
-  int T_max = 0;
-  for (const TopoDesc& td : bank->desc) T_max = std::max(T_max, td.T);
-  const long long rows = std::min<long long>(rows_cap, static_cast<long long>(B) * T_max);
-  const long long groups = rows * G / (kTilesPerWg * kQTile) + B, streams = Hkv * groups;
-  sh.two = two_rounds(streams, slots);
-  const int bound = paged_splits(static_cast<int>((cap + KB - 1) / KB), 1);
-  sh.splits = bound > 1;
-  const int nqg = query_groups(rows_padded(G, T_max) / kQTile);
-  const long long all = static_cast<long long>(B) * ((static_cast<long long>(Hkv) * bound + 7) / 8 * 8) * nqg;
-  const long long most = (sh.two ? 2LL : 1LL) * slots + streams + (Hkv % 8 ? 7 * groups : 0);
-  sh.items = static_cast<int>(std::min(std::min(most, all), static_cast<long long>(INT32_MAX)));
-  if (sh.splits)
-    sh.part_rows = static_cast<long long>(sh.items) * std::min(kTilesPerWg * kQTile, rows_padded(G, T_max));
-  sh.plan_bytes = plan_items_at(B, rows_cap) + sizeof(PlanItem) * static_cast<size_t>(sh.items);
-  sh.workspace = up256(static_cast<size_t>(sh.part_rows) * HD * sizeof(uint16_t)) +
-                 up256(static_cast<size_t>(sh.part_rows) * 2 * sizeof(float));
-  return sh;
-}
-
-bool shape_ok(const entmtp_bank* bank, int B, int rows_cap, int Hq, int Hkv, int max_pages, int page_size) {
-  return bank && !bank->desc.empty() && paged_batch(B) && rows_cap >= 1 && Hq >= 1 && Hkv >= 1 && Hq % Hkv == 0 &&
-         Hq / Hkv <= 32 && Hkv <= kMaxKvHeads && page_shift(page_size) >= 0 && max_pages >= 1 &&
-         static_cast<int64_t>(max_pages) * page_size <= INT32_MAX - 1024;
-}
-
-int32_t check_batch(int32_t B, int32_t rows_cap, int32_t Hq, int32_t Hkv, int32_t max_pages, int32_t page_size,
-                    int32_t n_pages, int32_t window) {
-  ENTMTP_CHECK_ARG(paged_batch(B), ENTMTP_EINVAL, "B = %d outside [1, %d]", B, ENTMTP_PAGED_B_MAX);
-  ENTMTP_CHECK_ARG(rows_cap >= 1, ENTMTP_EINVAL, "rows_cap = %d < 1", rows_cap);
-  ENTMTP_CHECK_ARG(Hq >= 1 && Hkv >= 1, ENTMTP_EINVAL, "Hq = %d, Hkv = %d must be >= 1", Hq, Hkv);
-  ENTMTP_CHECK_ARG(Hq % Hkv == 0, ENTMTP_ERANGE, "Hq = %d is not a multiple of Hkv = %d", Hq, Hkv);
-  ENTMTP_CHECK_ARG(Hq / Hkv <= 32, ENTMTP_ERANGE, "query group %d too large", Hq / Hkv);
-  ENTMTP_CHECK_ARG(Hkv <= kMaxKvHeads, ENTMTP_ERANGE, "Hkv = %d too large", Hkv);
-  if (int32_t rc = check_pool(n_pages, page_size)) return rc;
-  if (int32_t rc = check_pages(max_pages, page_size)) return rc;
-  ENTMTP_CHECK_ARG(window >= 0, ENTMTP_EINVAL, "window = %d < 0", window);
-  return ENTMTP_OK;
-}
 
 }  // namespace
 }  // namespace entmtp
@@ -1088,18 +840,18 @@ extern "C" const int32_t* entmtp_tree_attn_paged_topo(const void* plan, int32_t 
   return reinterpret_cast<const int32_t*>(static_cast<const uint8_t*>(plan) + plan_topo_at(B));
 }
 
-extern "C" int32_t entmtp_tree_attn_paged_plan(const entmtp_bank* bank, int32_t B, const int32_t* topo,
-                                               const int32_t* prefix_len, const int32_t* row_off,
-                                               const int32_t* status, const int32_t* block_table, int32_t max_pages,
-                                               int32_t page_size, int32_t n_pages, int32_t rows_cap, int32_t Hq,
-                                               int32_t Hkv, int32_t window, int32_t* bad, void* plan,
-                                               size_t plan_bytes, void* stream) {
+int32_t entmtp::launch_paged_plan(bool fp4, const entmtp_bank* bank, int32_t B, const int32_t* topo,
+                                  const int32_t* prefix_len, const int32_t* row_off, const int32_t* status,
+                                  const int32_t* block_table, int32_t max_pages, int32_t page_size, int32_t n_pages,
+                                  int32_t rows_cap, int32_t Hq, int32_t Hkv, int32_t window, int32_t* bad, void* plan,
+                                  size_t plan_bytes, void* stream) {
   clear_error();
   if (int32_t rc = check_batch(B, rows_cap, Hq, Hkv, max_pages, page_size, n_pages, window)) return rc;
   ENTMTP_CHECK_ARG(topo && prefix_len && row_off && status && block_table && plan, ENTMTP_EINVAL,
                    "topo, prefix_len, row_off, status, block_table and plan must be non-NULL device arrays");
   ENTMTP_CHECK_ARG((reinterpret_cast<uintptr_t>(plan) & 63u) == 0, ENTMTP_EINVAL, "the plan must be 64-byte aligned");
   PlanArgs a{};
+  a.fp4 = fp4;
   if (int32_t rc = tree_table(bank, &a.trees)) return rc;
   const PagedShape sh = paged_shape(bank, B, rows_cap, Hq, Hkv, static_cast<long long>(max_pages) * page_size);
   ENTMTP_CHECK_ARG(sh.items < INT32_MAX / 64, ENTMTP_ERANGE, "%d rows of %d heads: too many", rows_cap, Hq);
@@ -1132,6 +884,16 @@ extern "C" int32_t entmtp_tree_attn_paged_plan(const entmtp_bank* bank, int32_t 
   a.two = sh.two;
   hipLaunchKernelGGL(paged_plan_kernel, dim3(B), dim3(kPlanThreads), 0, static_cast<hipStream_t>(stream), a);
   return launch_status("tree_attn_paged_plan launch");
+}
+
+extern "C" int32_t entmtp_tree_attn_paged_plan(const entmtp_bank* bank, int32_t B, const int32_t* topo,
+                                               const int32_t* prefix_len, const int32_t* row_off,
+                                               const int32_t* status, const int32_t* block_table, int32_t max_pages,
+                                               int32_t page_size, int32_t n_pages, int32_t rows_cap, int32_t Hq,
+                                               int32_t Hkv, int32_t window, int32_t* bad, void* plan,
+                                               size_t plan_bytes, void* stream) {
+  return launch_paged_plan(false, bank, B, topo, prefix_len, row_off, status, block_table, max_pages, page_size,
+                           n_pages, rows_cap, Hq, Hkv, window, bad, plan, plan_bytes, stream);
 }
 
 extern "C" int32_t entmtp_tree_attn_paged(const entmtp_bank* bank, int32_t B, const void* plan, size_t plan_bytes,
@@ -1168,9 +930,9 @@ extern "C" int32_t entmtp_tree_attn_paged(const entmtp_bank* bank, int32_t B, co
   ENTMTP_CHECK_ARG(sh.workspace == 0 || (workspace && workspace_bytes >= sh.workspace), ENTMTP_ENOSPC,
                    "workspace has %zu bytes, needs %zu", workspace ? workspace_bytes : size_t(0), sh.workspace);
   PagedArgs a{};
-  a.plan = static_cast<const uint8_t*>(plan);
+  fill_call(a, trees, sh, plan, B, n_pages, page_size, max_pages, rows_cap, Hq, Hkv, window, out, workspace,
+            kPlanMagic);
   a.arena = trees.arena;
-  a.bank = trees.bank;
   a.table = block_table;
   a.slot_map = slot_map;
   a.slopes = slopes;
@@ -1179,33 +941,11 @@ extern "C" int32_t entmtp_tree_attn_paged(const entmtp_bank* bank, int32_t B, co
   a.vt = v_tree;
   a.kp = k_pool;
   a.vp = v_pool;
-  a.part_o = static_cast<uint16_t*>(workspace);
-  a.part_ml = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) +
-                                       up256(static_cast<size_t>(sh.part_rows) * HD * sizeof(uint16_t)));
-  a.out = out;
-  a.rows_at = static_cast<long long>(plan_rows_at(B));
-  a.items_at = static_cast<long long>(plan_items_at(B, rows_cap));
-  a.B = B;
-  a.G = Hq / Hkv;
-  a.Hq = Hq;
-  a.Hkv = Hkv;
-  a.shift = page_shift(page_size);
-  a.n_pages = n_pages;
-  a.max_pages = max_pages;
-  a.rows_cap = rows_cap;
-  a.window = window;
   a.q_scale = softcap > 0.f ? 2.f * kLog2e * (scale / softcap) : scale * kLog2e;
   a.cap_log2 = softcap * kLog2e;
   const double theta = static_cast<double>(rope_theta);
   rope_freqs(rope_theta, a.freq);
-  // a wavefront a head where they are few, so that long prefixes' many splits
-  // take half the round trips: 26 rows of 32 heads at 8192 21.4 us (attention and
-  // merge) against 23.9 by half wavefronts, 8 rows of 8 heads at 32000 18.3
-  // against 26.4; 4096 heads are level, 32768 take 10 us more by whole ones
-  const bool few = static_cast<long long>(rows_cap) * Hq <= 4LL * device_cus();
-  const int heads = kMergeThreads / (few ? 64 : 32);
-  const long long blocks = static_cast<long long>(rows_cap) * ((Hq + heads - 1) / heads);
-  ENTMTP_CHECK_ARG(blocks <= INT32_MAX, ENTMTP_ERANGE, "%d rows of %d heads: too many", rows_cap, Hq);
+  ENTMTP_CHECK_ARG(merge_blocks(rows_cap, Hq) <= INT32_MAX, ENTMTP_ERANGE, "%d rows of %d heads: too many", rows_cap, Hq);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(sh.items), dim3(kAttnThreads), 0, s, a); };
   const bool mod = softcap > 0.f || window > 0 || slopes != nullptr;
@@ -1217,9 +957,5 @@ extern "C" int32_t entmtp_tree_attn_paged(const entmtp_bank* bank, int32_t B, co
     mod ? go(paged_attn_kernel<kNear, true>) : go(paged_attn_kernel<kNear, false>);
   if (int32_t rc = launch_status("tree_attn_paged launch")) return rc;
   if (!sh.splits) return ENTMTP_OK;
-  auto merge = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(blocks)), dim3(kMergeThreads), 0, s, a);
-  };
-  few ? merge(paged_merge_kernel<64>) : merge(paged_merge_kernel<32>);
-  return launch_status("tree_attn_paged merge launch");
+  return launch_merge(a, s);
 }
