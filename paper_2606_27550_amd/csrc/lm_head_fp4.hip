@@ -2,8 +2,8 @@
 //
 // The weights stream past the hidden states, which stay in registers.  A
 // workgroup of eight wavefronts takes up to 32 rows of X; wavefront w keeps
-// every eighth 128-wide step of them and takes the same steps of each 16-row
-// tile of W: a lane's 16 bytes are 32 codes of one group, which become bf16
+// an eighth of their length, in 128-wide steps, and takes the same steps of each
+// 16-row tile of W: a lane's 16 bytes are 32 codes of one group, which become bf16
 // numbers, exactly, on the way into the matrix instruction (16 x 16 x 32), so
 // that the products are exact and the sums those of the bf16 LM head.  The eight
 // partial sums of a tile meet in the LDS.  (The matrix instruction that takes
@@ -30,15 +30,15 @@ struct LmFp4Args {
   const uint8_t* scales;   // [V][hid / 32]
   float* out;              // [T][V]
   int T, hid, V;
-  int tiles, per;          // tiles of W, per workgroup
+  int tiles, slices;       // tiles of W, workgroups that share them
   int chunks;              // of X's rows
   int k0;                  // first step of this pass over hid
   int add;                 // a later pass adds to the earlier ones
 };
 
 // KS: steps a wavefront; NT: 16-row tiles of X; NBUF: tiles of W in flight and
-// in use.
-template <int KS, int NT, int NBUF>
+// in use; WHOLE: every wavefront has all its steps, and scale rows are whole words.
+template <int KS, int NT, int NBUF, bool WHOLE>
 __global__ __launch_bounds__(kLmThreads, 2) void lm_fp4_kernel(LmFp4Args p) {
   __shared__ __attribute__((aligned(16))) f32x4 s_part[2][kLmWaves][kLmGroup][NT][64];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -46,17 +46,24 @@ __global__ __launch_bounds__(kLmThreads, 2) void lm_fp4_kernel(LmFp4Args p) {
   // the chunks of X that share a range of W follow each other on one XCD
   const int grp = static_cast<int>(blockIdx.x) >> 3;
   const int chunk = grp % p.chunks, slice = (grp / p.chunks) * 8 + (static_cast<int>(blockIdx.x) & 7);
-  const int t0 = slice * p.per, t1 = min(t0 + p.per, p.tiles);
-  if (t0 >= t1) return;
+  // its tiles are slice, slice + slices, ..: the workgroups then read one stretch
+  // of W between them at any time (stretches of their own, a power of two apart,
+  // meet in the same memory channels)
+  if (slice >= p.slices) return;
+  const int n_tiles = (p.tiles - slice + p.slices - 1) / p.slices;
+  auto row_of = [&](int i) { return (slice + min(i, n_tiles - 1) * p.slices) * kLmTile; };
   const int row0 = chunk * 16 * NT;
-  const int kw = p.k0 + wave;   // this wavefront's steps: kw, kw + 8, ..
+  const int k0 = (p.k0 + wave * KS) * kLmStep + 32 * blk;   // of this lane's first 32 values
 
-  // where lane (row li, block blk) finds step s's 32 values in a row of W
-  int coff[KS], soff[KS];
+  // Step s of a row of W: the lane's 16 bytes of codes, and the four scale bytes
+  // of the step, of which it takes byte blk (a dword of four lanes: byte loads
+  // would be as many requests as the codes').  Past the row the first step's
+  // stand in, and X is zero.
   bool there[KS];
+  int coff[KS], soff[KS];
 #pragma unroll
   for (int s = 0; s < KS; ++s) {
-    const int k = (kw + s * kLmWaves) * kLmStep + 32 * blk;
+    const int k = k0 + s * kLmStep;
     there[s] = k < p.hid;
     coff[s] = there[s] ? k / 2 : 0;
     soff[s] = there[s] ? k / 32 : 0;
@@ -64,19 +71,28 @@ __global__ __launch_bounds__(kLmThreads, 2) void lm_fp4_kernel(LmFp4Args p) {
   u32x4 wb[NBUF][KS];
   uint32_t sb[NBUF][KS];
   const int crow = p.hid / 2, srow = p.hid / 32;
-  auto load = [&](int buf, int tile) {
-    const int v = min(min(tile, t1 - 1) * kLmTile + li, p.V - 1);
+  auto load = [&](int buf, int i) {
+    const int v = min(row_of(i) + li, p.V - 1);
     const uint8_t* const c = p.codes + static_cast<size_t>(v) * crow;
     const uint8_t* const s8 = p.scales + static_cast<size_t>(v) * srow;
+    if constexpr (WHOLE) {
+      // (all there: one run of codes and one of scale bytes)
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      wb[buf][s] = *reinterpret_cast<const u32x4*>(c + coff[s]);
-      sb[buf][s] = s8[soff[s]];
+      for (int s = 0; s < KS; ++s) wb[buf][s] = *reinterpret_cast<const u32x4*>(c + k0 / 2 + s * (kLmStep / 2));
+      struct __attribute__((packed, aligned(4))) Run {
+        uint32_t w[KS];
+      };
+      const Run r = *reinterpret_cast<const Run*>(s8 + (k0 - 32 * blk) / 32);
+#pragma unroll
+      for (int s = 0; s < KS; ++s) sb[buf][s] = r.w[s];
+    } else {
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        wb[buf][s] = *reinterpret_cast<const u32x4*>(c + coff[s]);
+        sb[buf][s] = s8[soff[s]];
+      }
     }
   };
-#pragma unroll
-  for (int k = 0; k < NBUF - 1; ++k) load(k, t0 + k);
-
   // this lane's part of X: row li of each tile, the same 32 values of a step
   u32x4 xb[NT][KS][4];
 #pragma unroll
@@ -88,8 +104,16 @@ __global__ __launch_bounds__(kLmThreads, 2) void lm_fp4_kernel(LmFp4Args p) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         xb[n][s][j] = *reinterpret_cast<const u32x4*>(xr + 2 * coff[s] + 8 * j);
-        if (!there[s]) xb[n][s][j] = u32x4{0u, 0u, 0u, 0u};
+        if (!WHOLE && !there[s]) xb[n][s][j] = u32x4{0u, 0u, 0u, 0u};
       }
+  }
+
+  // (the loads keep their order: a wait for a tile then leaves the later ones in flight)
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int k = 0; k < NBUF - 1; ++k) {
+    load(k, k);
+    __builtin_amdgcn_sched_barrier(0);
   }
 
   const bool wide = (p.V & 3) == 0;
@@ -100,7 +124,8 @@ __global__ __launch_bounds__(kLmThreads, 2) void lm_fp4_kernel(LmFp4Args p) {
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       // (past the row X is zero and W's first values stand in, as numbers)
-      const float step = __uint_as_float((there[s] ? sb[buf][s] : 127u) << 23);
+      const uint32_t b = WHOLE ? sb[buf][s] >> (8 * blk) & 0xffu : (there[s] ? sb[buf][s] : 127u);
+      const float step = fp4_step(b);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const bf16x8 a = as_bf16x8(fp4_values(wb[buf][s][j], step));
@@ -112,14 +137,14 @@ __global__ __launch_bounds__(kLmThreads, 2) void lm_fp4_kernel(LmFp4Args p) {
 #pragma unroll
     for (int n = 0; n < NT; ++n) s_part[par][wave][k][n][lane] = acc[n];
   };
-  auto reduce = [&](int tile, int par) {   // of tiles tile .. + 3
+  auto reduce = [&](int first, int par) {   // of tiles first .. + 3
     for (int i = tid; i < kLmGroup * NT * 64; i += kLmThreads) {
       const int l = i & 63, n = (i >> 6) % NT, k = i / (64 * NT);
       f32x4 z = s_part[par][0][k][n][l];
 #pragma unroll
       for (int w = 1; w < kLmWaves; ++w) z += s_part[par][w][k][n][l];
-      const int row = row0 + 16 * n + (l & 15), v = (tile + k) * kLmTile + 4 * (l >> 4);
-      if (row >= p.T || tile + k >= t1 || v >= p.V) continue;
+      const int row = row0 + 16 * n + (l & 15), v = row_of(first + k) + 4 * (l >> 4);
+      if (row >= p.T || first + k >= n_tiles || v >= p.V) continue;
       float* const o = p.out + static_cast<size_t>(row) * p.V + v;
       if (wide) {
         f32x4* const o4 = reinterpret_cast<f32x4*>(o);
@@ -133,10 +158,11 @@ __global__ __launch_bounds__(kLmThreads, 2) void lm_fp4_kernel(LmFp4Args p) {
   };
   int par = 0;
   static_assert(kLmGroup % NBUF == 0, "a tile's buffer is known");
-  for (int t = t0; t < t1; t += kLmGroup) {
+  for (int t = 0; t < n_tiles; t += kLmGroup) {
 #pragma unroll
     for (int k = 0; k < kLmGroup; ++k) {
       load((k + NBUF - 1) % NBUF, t + k + NBUF - 1);
+      __builtin_amdgcn_sched_barrier(0);
       compute(k % NBUF, k, par);
     }
     // (the other half is written while this one is read: one barrier a group)
@@ -180,34 +206,37 @@ extern "C" int32_t entmtp_verify_logits_fp4(const entmtp_bf16* hidden, const uin
   const int passes = (steps + most * kLmWaves - 1) / (most * kLmWaves);
   const int ks = ((steps + passes - 1) / passes + kLmWaves - 1) / kLmWaves;
   a.chunks = (T + 16 * nt - 1) / (16 * nt);
-  const int slices = std::max(1, cus / a.chunks / 8) * 8;
-  a.per = (a.tiles + slices - 1) / slices;
-  const int used = (a.tiles + a.per - 1) / a.per;
-  const dim3 grid(static_cast<uint32_t>((used + 7) / 8 * 8 * a.chunks));
+  a.slices = std::min(std::max(1, cus / a.chunks / 8) * 8, a.tiles);
+  const dim3 grid(static_cast<uint32_t>((a.slices + 7) / 8 * 8 * a.chunks));
   for (int pass = 0; pass < passes; ++pass) {
     a.k0 = pass * ks * kLmWaves;
     a.add = pass > 0;
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kLmThreads), 0, s, a); };
+    const bool whole = hid == passes * ks * kLmWaves * kLmStep && (reinterpret_cast<uintptr_t>(scales) & 3u) == 0;
+    auto go = [&](auto kernel, auto rest) {
+      hipLaunchKernelGGL(whole ? kernel : rest, grid, dim3(kLmThreads), 0, s, a);
+    };
+#define LM_FP4(KS, NT, NBUF) go(lm_fp4_kernel<KS, NT, NBUF, true>, lm_fp4_kernel<KS, NT, 2, false>)
     if (nt == 1) {
       switch (ks) {
-        case 1: go(lm_fp4_kernel<1, 1, 4>); break;
-        case 2: go(lm_fp4_kernel<2, 1, 4>); break;
-        case 3: go(lm_fp4_kernel<3, 1, 4>); break;
-        case 4: go(lm_fp4_kernel<4, 1, 4>); break;
-        case 5: go(lm_fp4_kernel<5, 1, 2>); break;
-        case 6: go(lm_fp4_kernel<6, 1, 2>); break;
-        case 7: go(lm_fp4_kernel<7, 1, 2>); break;
-        default: go(lm_fp4_kernel<8, 1, 2>);
+        case 1: LM_FP4(1, 1, 4); break;
+        case 2: LM_FP4(2, 1, 4); break;
+        case 3: LM_FP4(3, 1, 4); break;
+        case 4: LM_FP4(4, 1, 4); break;
+        case 5: LM_FP4(5, 1, 4); break;
+        case 6: LM_FP4(6, 1, 2); break;
+        case 7: LM_FP4(7, 1, 2); break;
+        default: LM_FP4(8, 1, 2);
       }
     } else {
       switch (ks) {
-        case 1: go(lm_fp4_kernel<1, 2, 4>); break;
-        case 2: go(lm_fp4_kernel<2, 2, 4>); break;
-        case 3: go(lm_fp4_kernel<3, 2, 2>); break;
-        case 4: go(lm_fp4_kernel<4, 2, 2>); break;
-        default: go(lm_fp4_kernel<5, 2, 2>);
+        case 1: LM_FP4(1, 2, 4); break;
+        case 2: LM_FP4(2, 2, 4); break;
+        case 3: LM_FP4(3, 2, 4); break;
+        case 4: LM_FP4(4, 2, 4); break;
+        default: LM_FP4(5, 2, 2);
       }
     }
+#undef LM_FP4
     if (int32_t rc = launch_status("verify_logits_fp4 launch")) return rc;
   }
   return ENTMTP_OK;
