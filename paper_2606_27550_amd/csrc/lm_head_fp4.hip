@@ -22,7 +22,9 @@ namespace {
 constexpr int kLmWaves = 8, kLmThreads = 64 * kLmWaves;
 constexpr int kLmStep = 128;    // values a matrix instruction takes
 constexpr int kLmTile = 16;     // rows of W
-constexpr int kLmGroup = 4;     // tiles between reductions
+constexpr int kLmGroup = 2;     // tiles between reductions
+constexpr int kLmRound = 4;     // tiles of the unrolled loop
+constexpr int kLmHeld = 64;     // 16 x 16 logits that a workgroup holds before it stores them
 
 struct LmFp4Args {
   const uint16_t* x;       // [T][hid]
@@ -41,6 +43,8 @@ struct LmFp4Args {
 template <int KS, int NT, int NBUF, bool WHOLE>
 __global__ __launch_bounds__(kLmThreads, 2) void lm_fp4_kernel(LmFp4Args p) {
   __shared__ __attribute__((aligned(16))) f32x4 s_part[2][kLmWaves][kLmGroup][NT][64];
+  constexpr int kHold = kLmHeld / NT;   // tiles of W
+  __shared__ __attribute__((aligned(16))) f32x4 s_out[kHold][NT][64];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int li = lane & 15, blk = lane >> 4;
   // the chunks of X that share a range of W follow each other on one XCD
@@ -137,14 +141,25 @@ __global__ __launch_bounds__(kLmThreads, 2) void lm_fp4_kernel(LmFp4Args p) {
 #pragma unroll
     for (int n = 0; n < NT; ++n) s_part[par][wave][k][n][lane] = acc[n];
   };
-  auto reduce = [&](int first, int par) {   // of tiles first .. + 3
+  // the sums of tiles first .. first + 1, kept
+  auto reduce = [&](int first, int par) {
     for (int i = tid; i < kLmGroup * NT * 64; i += kLmThreads) {
       const int l = i & 63, n = (i >> 6) % NT, k = i / (64 * NT);
       f32x4 z = s_part[par][0][k][n][l];
 #pragma unroll
       for (int w = 1; w < kLmWaves; ++w) z += s_part[par][w][k][n][l];
-      const int row = row0 + 16 * n + (l & 15), v = row_of(first + k) + 4 * (l >> 4);
-      if (row >= p.T || first + k >= n_tiles || v >= p.V) continue;
+      s_out[(first + k) % kHold][n][l] = z;
+    }
+  };
+  // Stores of tiles first .. end - 1.  (A store is waited for like the loads
+  // issued before and after it, so they go out together: two tiles at a time
+  // they cost 10 us of 64 at 27 rows of 128256.)
+  auto flush = [&](int first, int end) {
+    for (int i = tid; i < (end - first) * NT * 64; i += kLmThreads) {
+      const int l = i & 63, n = (i >> 6) % NT, k = first + i / (64 * NT);
+      const f32x4 z = s_out[k % kHold][n][l];
+      const int row = row0 + 16 * n + (l & 15), v = row_of(k) + 4 * (l >> 4);
+      if (row >= p.T || v >= p.V) continue;
       float* const o = p.out + static_cast<size_t>(row) * p.V + v;
       if (wide) {
         f32x4* const o4 = reinterpret_cast<f32x4*>(o);
@@ -156,20 +171,33 @@ __global__ __launch_bounds__(kLmThreads, 2) void lm_fp4_kernel(LmFp4Args p) {
       }
     }
   };
-  int par = 0;
-  static_assert(kLmGroup % NBUF == 0, "a tile's buffer is known");
-  for (int t = 0; t < n_tiles; t += kLmGroup) {
+  int par = 0, kept = 0;
+  static_assert(kLmRound % NBUF == 0 && kLmRound % kLmGroup == 0, "a tile's buffer is known");
+  static_assert(kHold % kLmRound == 0, "a round is kept whole");
+  for (int t = 0; t < n_tiles; t += kLmRound) {
 #pragma unroll
-    for (int k = 0; k < kLmGroup; ++k) {
+    for (int k = 0; k < kLmRound; ++k) {
       load((k + NBUF - 1) % NBUF, t + k + NBUF - 1);
       __builtin_amdgcn_sched_barrier(0);
-      compute(k % NBUF, k, par);
+      compute(k % NBUF, k % kLmGroup, par);
+      if (k % kLmGroup == kLmGroup - 1) {
+        // (the other half is written while this one is read: one barrier a group)
+        wait_lds();
+        stage_barrier();
+        reduce(t + k + 1 - kLmGroup, par);
+        par ^= 1;
+      }
     }
-    // (the other half is written while this one is read: one barrier a group)
-    wait_lds();
-    stage_barrier();
-    reduce(t, par);
-    par ^= 1;
+    if (t + kLmRound - kept == kHold || t + kLmRound >= n_tiles) {
+      wait_lds();
+      stage_barrier();
+      flush(kept, min(t + kLmRound, n_tiles));
+      kept = t + kLmRound;
+      if (kept < n_tiles) {
+        wait_lds();
+        stage_barrier();
+      }
+    }
   }
 }
 
