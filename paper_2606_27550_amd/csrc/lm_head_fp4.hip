@@ -39,8 +39,8 @@ struct LmFp4Args {
 };
 
 // KS: steps a wavefront; NT: 16-row tiles of X; NBUF: tiles of W in flight and
-// in use; WHOLE: every wavefront has all its steps, and scale rows are whole words.
-template <int KS, int NT, int NBUF, bool WHOLE>
+// in use.
+template <int KS, int NT, int NBUF>
 __global__ __launch_bounds__(kLmThreads, 2) void lm_fp4_kernel(LmFp4Args p) {
   __shared__ __attribute__((aligned(16))) f32x4 s_part[2][kLmWaves][kLmGroup][NT][64];
   constexpr int kHold = kLmHeld / NT;   // tiles of W
@@ -59,10 +59,8 @@ __global__ __launch_bounds__(kLmThreads, 2) void lm_fp4_kernel(LmFp4Args p) {
   const int row0 = chunk * 16 * NT;
   const int k0 = (p.k0 + wave * KS) * kLmStep + 32 * blk;   // of this lane's first 32 values
 
-  // Step s of a row of W: the lane's 16 bytes of codes, and the four scale bytes
-  // of the step, of which it takes byte blk (a dword of four lanes: byte loads
-  // would be as many requests as the codes').  Past the row the first step's
-  // stand in, and X is zero.
+  // Step s of a row of W: the lane's 16 bytes of codes and their scale byte.  Past
+  // the row the first step's stand in, and X is zero.
   bool there[KS];
   int coff[KS], soff[KS];
 #pragma unroll
@@ -79,22 +77,10 @@ __global__ __launch_bounds__(kLmThreads, 2) void lm_fp4_kernel(LmFp4Args p) {
     const int v = min(row_of(i) + li, p.V - 1);
     const uint8_t* const c = p.codes + static_cast<size_t>(v) * crow;
     const uint8_t* const s8 = p.scales + static_cast<size_t>(v) * srow;
-    if constexpr (WHOLE) {
-      // (all there: one run of codes and one of scale bytes)
 #pragma unroll
-      for (int s = 0; s < KS; ++s) wb[buf][s] = *reinterpret_cast<const u32x4*>(c + k0 / 2 + s * (kLmStep / 2));
-      struct __attribute__((packed, aligned(4))) Run {
-        uint32_t w[KS];
-      };
-      const Run r = *reinterpret_cast<const Run*>(s8 + (k0 - 32 * blk) / 32);
-#pragma unroll
-      for (int s = 0; s < KS; ++s) sb[buf][s] = r.w[s];
-    } else {
-#pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        wb[buf][s] = *reinterpret_cast<const u32x4*>(c + coff[s]);
-        sb[buf][s] = s8[soff[s]];
-      }
+    for (int s = 0; s < KS; ++s) {
+      wb[buf][s] = *reinterpret_cast<const u32x4*>(c + coff[s]);
+      sb[buf][s] = s8[soff[s]];
     }
   };
   // this lane's part of X: row li of each tile, the same 32 values of a step
@@ -108,7 +94,7 @@ __global__ __launch_bounds__(kLmThreads, 2) void lm_fp4_kernel(LmFp4Args p) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         xb[n][s][j] = *reinterpret_cast<const u32x4*>(xr + 2 * coff[s] + 8 * j);
-        if (!WHOLE && !there[s]) xb[n][s][j] = u32x4{0u, 0u, 0u, 0u};
+        if (!there[s]) xb[n][s][j] = u32x4{0u, 0u, 0u, 0u};
       }
   }
 
@@ -128,8 +114,7 @@ __global__ __launch_bounds__(kLmThreads, 2) void lm_fp4_kernel(LmFp4Args p) {
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       // (past the row X is zero and W's first values stand in, as numbers)
-      const uint32_t b = WHOLE ? sb[buf][s] >> (8 * blk) & 0xffu : (there[s] ? sb[buf][s] : 127u);
-      const float step = fp4_step(b);
+      const float step = fp4_step(there[s] ? sb[buf][s] : 127u);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const bf16x8 a = as_bf16x8(fp4_values(wb[buf][s][j], step));
@@ -201,6 +186,183 @@ __global__ __launch_bounds__(kLmThreads, 2) void lm_fp4_kernel(LmFp4Args p) {
   }
 }
 
+// ---------------------------------------------------------- whole lines --
+
+// The same where every wavefront has KS whole steps: its part of a tile, 16 rows
+// of 64 KS bytes, is copied to the LDS by whole lines, two tiles ahead.  Against
+// a lane's own 16 bytes to registers: one row of 32000 logits 16.6 -> 13.7 us, 27
+// rows 21.9 -> 19.0, 128 rows (5120 values) 63 -> 56; 27 rows of 128256 are level
+// (58-60, the plain read's rate is 46), 8 rows 49 -> 50.5.  Three tiles ahead are no
+// faster, nor one barrier for two tiles.
+// Chunk c (16 bytes) of row r of a tile lies at c ^ lm_swz(r), which spreads the 16
+// rows that a read takes over all banks.
+template <int KS>
+__device__ __forceinline__ int lm_swz(int r) {
+  return KS % 4 == 0 ? r & 15 : (KS % 2 == 0 ? r >> 1 & 7 : r >> 2 & 3);
+}
+
+// Four bytes a lane to the LDS, as buf_dma16.
+__device__ __forceinline__ void buf_dma4(__amdgpu_buffer_rsrc_t buf, uint32_t voff, void* lds) {
+  typedef __attribute__((address_space(3))) void lds_void;
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lds_void*)lds, 4, voff, 0, 0, 0);
+}
+
+// A wavefront's part of a tile: codes, and a dword of scale bytes a row and step.
+template <int KS>
+struct LmPart {
+  uint8_t codes[KS * 1024];
+  uint32_t scales[(KS + 3) / 4 * 64];
+};
+
+template <int KS, int NT>
+__global__ __launch_bounds__(kLmThreads, 2) void lm_fp4_stream_kernel(LmFp4Args p) {
+  constexpr int kScaleCopies = (KS + 3) / 4, kCopies = KS + kScaleCopies;
+  // the LDS: two tiles of W, partial sums of two, logits of kHold
+  constexpr int kFree = 160 * 1024 - 2 * static_cast<int>(sizeof(LmPart<KS>)) * kLmWaves - 2 * kLmWaves * NT * 1024;
+  constexpr int kHold = std::min(kFree / (NT * 1024), 48 / NT) / 2 * 2;
+  static_assert(kHold >= 2, "a round's logits are kept");
+  __shared__ __attribute__((aligned(16))) LmPart<KS> ring0[kLmWaves];
+  __shared__ __attribute__((aligned(16))) LmPart<KS> ring1[kLmWaves];
+  __shared__ __attribute__((aligned(16))) f32x4 s_part[2][kLmWaves][NT][64];
+  __shared__ __attribute__((aligned(16))) f32x4 s_out[kHold][NT][64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int li = lane & 15, blk = lane >> 4;
+  const int grp = static_cast<int>(blockIdx.x) >> 3;
+  const int chunk = grp % p.chunks, slice = (grp / p.chunks) * 8 + (static_cast<int>(blockIdx.x) & 7);
+  if (slice >= p.slices) return;
+  const int n_tiles = (p.tiles - slice + p.slices - 1) / p.slices;
+  auto row_of = [&](int i) { return (slice + min(i, n_tiles - 1) * p.slices) * kLmTile; };
+  const int row0 = chunk * 16 * NT;
+  const int crow = p.hid / 2, srow = p.hid / 32;
+  const int k0 = (p.k0 + wave * KS) * kLmStep;   // of this wavefront's values
+
+  // this lane's part of X: row li of each tile, 32 values of every step
+  u32x4 xb[NT][KS][4];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const uint16_t* const xr = p.x + static_cast<size_t>(min(row0 + 16 * n + li, p.T - 1)) * p.hid + k0 + 32 * blk;
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) xb[n][s][j] = *reinterpret_cast<const u32x4*>(xr + s * kLmStep + 8 * j);
+  }
+
+  // copies of a tile: place q of the part is chunk q % (4 KS) of row q / (4 KS)
+  uint32_t coff[KS], soff[kScaleCopies];
+  int crw[KS], srw[kScaleCopies];
+#pragma unroll
+  for (int j = 0; j < KS; ++j) {
+    const int q = 64 * j + lane;
+    crw[j] = q / (4 * KS);
+    coff[j] = 16 * (q % (4 * KS) ^ lm_swz<KS>(crw[j]));
+  }
+#pragma unroll
+  for (int j = 0; j < kScaleCopies; ++j) {
+    const int q = 64 * j + lane;
+    srw[j] = min(q / KS, 15);
+    soff[j] = 4 * (q % KS);
+  }
+  auto copy = [&](LmPart<KS>& to, int i) {
+    // (rows past the last are the last again, as are tiles)
+    const int v = row_of(i), last = p.V - 1 - v;
+    const __amdgpu_buffer_rsrc_t cbuf = dma_buffer(p.codes + static_cast<size_t>(v) * crow + k0 / 2, 0x7fffffff);
+    const __amdgpu_buffer_rsrc_t sbuf = dma_buffer(p.scales + static_cast<size_t>(v) * srow + k0 / 32, 0x7fffffff);
+#pragma unroll
+    for (int j = 0; j < KS; ++j) buf_dma16(cbuf, static_cast<uint32_t>(min(crw[j], last)) * crow + coff[j], to.codes + 1024 * j);
+#pragma unroll
+    for (int j = 0; j < kScaleCopies; ++j)
+      buf_dma4(sbuf, static_cast<uint32_t>(min(srw[j], last)) * srow + soff[j], to.scales + 64 * j);
+  };
+  u32x4 w[KS];
+  uint32_t sc[KS];
+  auto read = [&](const LmPart<KS>& from) {
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      w[s] = *reinterpret_cast<const u32x4*>(from.codes + 16 * (4 * KS * li + (4 * s + blk ^ lm_swz<KS>(li))));
+      sc[s] = from.scales[KS * li + s];
+    }
+  };
+  auto compute = [&](int par) {
+    f32x4 acc[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const float step = fp4_step(sc[s] >> (8 * blk) & 0xffu);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bf16x8 a = as_bf16x8(fp4_values(w[s][j], step));
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+          acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, as_bf16x8(xb[n][s][j]), acc[n], 0, 0, 0);
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) s_part[par][wave][n][lane] = acc[n];
+  };
+  // (a number a thread: by fours it would be two wavefronts' work, for which the
+  // others wait at the next barrier)
+  auto reduce = [&](int i, int par) {
+    if (tid < NT * 256) {
+      const float* const from = reinterpret_cast<const float*>(s_part[par]) + tid;
+      float z = from[0];
+#pragma unroll
+      for (int v = 1; v < kLmWaves; ++v) z += from[v * NT * 256];
+      reinterpret_cast<float*>(s_out[i % kHold])[tid] = z;
+    }
+  };
+  const bool wide = (p.V & 3) == 0;
+  auto flush = [&](int first, int end) {
+    for (int i = tid; i < (end - first) * NT * 64; i += kLmThreads) {
+      const int l = i & 63, n = (i >> 6) % NT, k = first + i / (64 * NT);
+      const f32x4 z = s_out[k % kHold][n][l];
+      const int row = row0 + 16 * n + (l & 15), v = row_of(k) + 4 * (l >> 4);
+      if (row >= p.T || v >= p.V) continue;
+      float* const o = p.out + static_cast<size_t>(row) * p.V + v;
+      if (wide) {
+        f32x4* const o4 = reinterpret_cast<f32x4*>(o);
+        *o4 = p.add ? *o4 + z : z;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (v + e < p.V) o[e] = p.add ? o[e] + z[e] : z[e];
+      }
+    }
+  };
+  // (X is waited for here, so that the counts are the copies' alone)
+  wait_vmcnt<0>();
+  copy(ring0[wave], 0);
+  copy(ring1[wave], 1);
+  int kept = 0;
+  for (int t = 0; t < n_tiles; t += 2) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      LmPart<KS>& mine = k ? ring1[wave] : ring0[wave];
+      wait_vmcnt<kCopies>();
+      read(mine);
+      wait_lds();
+      asm volatile("" ::: "memory");
+      copy(mine, t + k + 2);
+      compute(k);
+      // (the other half is written while this one is read: one barrier a tile)
+      wait_lds();
+      stage_barrier();
+      reduce(t + k, k);
+    }
+    if (t + 2 - kept == kHold || t + 2 >= n_tiles) {
+      wait_lds();
+      stage_barrier();
+      flush(kept, min(t + 2, n_tiles));
+      kept = t + 2;
+      if (kept < n_tiles) {
+        wait_lds();
+        stage_barrier();
+      }
+    }
+  }
+  wait_vmcnt<0>();   // (copies past the last tile)
+}
+
 }  // namespace
 }  // namespace entmtp
 
@@ -239,29 +401,31 @@ extern "C" int32_t entmtp_verify_logits_fp4(const entmtp_bf16* hidden, const uin
   for (int pass = 0; pass < passes; ++pass) {
     a.k0 = pass * ks * kLmWaves;
     a.add = pass > 0;
+    // (rows of W of whole words whose wavefronts' parts are alike, and the LDS's
+    // places of 16 bytes of them)
     const bool whole = hid == passes * ks * kLmWaves * kLmStep && (reinterpret_cast<uintptr_t>(scales) & 3u) == 0;
-    auto go = [&](auto kernel, auto rest) {
-      hipLaunchKernelGGL(whole ? kernel : rest, grid, dim3(kLmThreads), 0, s, a);
+    auto go = [&](auto stream_kernel, auto rest) {
+      hipLaunchKernelGGL(whole ? stream_kernel : rest, grid, dim3(kLmThreads), 0, s, a);
     };
-#define LM_FP4(KS, NT, NBUF) go(lm_fp4_kernel<KS, NT, NBUF, true>, lm_fp4_kernel<KS, NT, 2, false>)
+#define LM_FP4(KS, NT) go(lm_fp4_stream_kernel<KS, NT>, lm_fp4_kernel<KS, NT, 2>)
     if (nt == 1) {
       switch (ks) {
-        case 1: LM_FP4(1, 1, 4); break;
-        case 2: LM_FP4(2, 1, 4); break;
-        case 3: LM_FP4(3, 1, 4); break;
-        case 4: LM_FP4(4, 1, 4); break;
-        case 5: LM_FP4(5, 1, 4); break;
-        case 6: LM_FP4(6, 1, 2); break;
-        case 7: LM_FP4(7, 1, 2); break;
-        default: LM_FP4(8, 1, 2);
+        case 1: LM_FP4(1, 1); break;
+        case 2: LM_FP4(2, 1); break;
+        case 3: LM_FP4(3, 1); break;
+        case 4: LM_FP4(4, 1); break;
+        case 5: LM_FP4(5, 1); break;
+        case 6: LM_FP4(6, 1); break;
+        case 7: LM_FP4(7, 1); break;
+        default: LM_FP4(8, 1);
       }
     } else {
       switch (ks) {
-        case 1: LM_FP4(1, 2, 4); break;
-        case 2: LM_FP4(2, 2, 4); break;
-        case 3: LM_FP4(3, 2, 4); break;
-        case 4: LM_FP4(4, 2, 4); break;
-        default: LM_FP4(5, 2, 2);
+        case 1: LM_FP4(1, 2); break;
+        case 2: LM_FP4(2, 2); break;
+        case 3: LM_FP4(3, 2); break;
+        case 4: LM_FP4(4, 2); break;
+        default: LM_FP4(5, 2);
       }
     }
 #undef LM_FP4
