@@ -9,18 +9,24 @@
 // so that a key block of the tree differs from one of the prefix by its mask
 // alone.  The work list is that of paged_attn.hip: a workgroup takes a KV head's
 // query rows (four tiles of 32) and a range of 32-key blocks.
-//  - A wavefront streams its blocks by itself, from memory to registers, three
-//    ahead, and no barrier joins it to the others.  Where the rows fill one tile
-//    (or two) its wavefronts share the range, every fourth (second) block each,
-//    and meet in the LDS at the end: a few rows' blocks are a chain of products,
-//    softmax and products that one wavefront could not walk at memory's rate.
-//  - Keys enter the matrix instruction (32 x 32 x 64, 4-bit by 8-bit) as they lie
-//    in the pool, codes and scale bytes; the queries as two 8-bit numbers of four
-//    bits of mantissa each, which hold a bf16 number's eight, so that the scores
-//    are those of the bf16 query (one below 2^-14 of the largest of its 32 to
-//    within 2^-22 of that).
-//  - Values become bf16 numbers, exactly, on their way to the wavefront's part of
-//    the LDS, from which the products read them transposed.
+//  - Keys enter the matrix instruction (32 x 32 x 64, 4-bit by 6-bit: twice the
+//    rate of bf16) as they lie in the pool, codes and scale bytes.  A query, with
+//    the scale in base 2 taken into it, is two 6-bit numbers: hi, rounded to steps
+//    of at most 1/15 of the largest of its 32, and lo, the rest with a scale 2^4
+//    below.  Their sum is off by at most 2^-8 / 3.75 of that largest, less than a
+//    rounding to bf16 as a whole (root mean square 5e-4 of ordinary queries' against
+//    1.1e-3).
+//  - Values become bf16 numbers, exactly, on their way to the LDS, from which the
+//    products read them transposed.
+//  - Many rows (three or four tiles): the workgroup's wavefronts, a tile each,
+//    share the blocks, which come as codes by direct copies three ahead; every
+//    wavefront turns a quarter of a block's values into numbers, a block ahead,
+//    and takes the next block's scores before this one's softmax.
+//  - Few rows: a wavefront streams its blocks by itself, from memory to registers,
+//    three ahead, and no barrier joins it to the others: the range is shared by four
+//    (two tiles: two), every fourth block each, which meet in the LDS at the end --
+//    a few rows' blocks are a chain of products, softmax and products that one
+//    wavefront could not walk at memory's rate.
 #include <algorithm>
 #include <type_traits>
 
@@ -30,8 +36,16 @@
 namespace entmtp {
 namespace {
 
-constexpr int kFp4Ahead = 3;               // blocks in flight per wavefront
+constexpr int kFp4Ahead = 3;               // blocks in flight per wavefront (few rows)
+constexpr int kFp4Ring = 4;                // blocks in the LDS (many rows)
 constexpr int kFp4Stage = KB * HD * 2;     // bytes of a block's values in bf16
+
+// A block's rows as they lie in the pool: wavefront w's copies are the keys' (w = 0,
+// 1) or the values' (2, 3) 16 rows, codes and scale bytes (16 dwords, then zeros).
+struct Fp4Block {
+  uint8_t k[KB * HD / 2], v[KB * HD / 2];
+  uint32_t s[kAttnThreads / 64][64];
+};
 
 struct PagedFp4Args : PagedCall {
   const uint8_t* arena;
@@ -45,33 +59,79 @@ struct PagedFp4Args : PagedCall {
 };
 
 // Chunk c (16 bytes) of row r of the staged values lies at c ^ stage_swz(r): a
-// store takes one chunk of eight rows, a transposing read 32 lanes' 64 bytes of
-// four rows; both then cover all banks.
-__device__ __forceinline__ int stage_swz(int r) { return 4 * (r & 3) + ((r >> 2) & 3); }
+// store takes one chunk of 16 rows, or every other one of two, a transposing read
+// 32 lanes' 64 bytes of four rows; all then cover all banks.  Of the keys' codes
+// chunk c of row r lies at c ^ (r / 4 % 4).
+__device__ __forceinline__ int stage_swz(int r) { return 4 * (r & 3) + (((r >> 2) & 3) ^ (r & 1)); }
 
-// Two 8-bit operands of 16 bf16 values times inv (a power of two).
-__device__ __forceinline__ void query8(u32x4 a, u32x4 b, float inv, i32x8& hi, i32x8& lo, int at) {
+// Four bytes a lane to the LDS, as buf_dma16.
+__device__ __forceinline__ void buf_dma4(__amdgpu_buffer_rsrc_t buf, uint32_t voff, void* lds) {
+  typedef __attribute__((address_space(3))) void lds_void;
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lds_void*)lds, 4, voff, 0, 0, 0);
+}
+
+// 32 values (v: 8 words of bf16 pairs in each of two halves) times f as two 6-bit
+// operands of the matrix instruction; returns their scale bytes, hi's and lo's in
+// the next byte but one (not a number where a value is not finite).
+__device__ __forceinline__ uint32_t query6(const u32x4 (&v)[4], float f, i32x8& hi, i32x8& lo) {
+  float x[32];
+  uint32_t top = 0u;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const uint32_t w0 = j < 2 ? a[2 * (j & 1)] : b[2 * (j & 1)], w1 = j < 2 ? a[2 * (j & 1) + 1] : b[2 * (j & 1) + 1];
-    const float x0 = bf16_lo(w0) * inv, x1 = bf16_hi(w0) * inv, x2 = bf16_lo(w1) * inv, x3 = bf16_hi(w1) * inv;
-    int h = 0, l = 0;
-    h = __builtin_amdgcn_cvt_pk_fp8_f32(x0, x1, h, false);
-    h = __builtin_amdgcn_cvt_pk_fp8_f32(x2, x3, h, true);
-    const auto y = __builtin_amdgcn_cvt_pk_f32_fp8(h, false), z = __builtin_amdgcn_cvt_pk_f32_fp8(h, true);
-    l = __builtin_amdgcn_cvt_pk_fp8_f32((x0 - y[0]) * 32.f, (x1 - y[1]) * 32.f, l, false);
-    l = __builtin_amdgcn_cvt_pk_fp8_f32((x2 - z[0]) * 32.f, (x3 - z[1]) * 32.f, l, true);
-    hi[at + j] = h;
-    lo[at + j] = l;
+  for (int e = 0; e < 16; ++e) {
+    const uint32_t w = v[e >> 2][e & 3];
+    x[2 * e] = bf16_lo(w) * f;
+    x[2 * e + 1] = bf16_hi(w) * f;
+    top = max(top, max(__float_as_uint(x[2 * e]) & 0x7fffffffu, __float_as_uint(x[2 * e + 1]) & 0x7fffffffu));
   }
+  // (the largest in [3.75, 7.5) steps)
+  const int e = static_cast<int>((top + (1u << 20)) >> 23), b = e < 8 ? 6 : (e > 254 ? 252 : e - 2);
+  const float step = __uint_as_float(static_cast<uint32_t>(b) << 23), inv = __uint_as_float(static_cast<uint32_t>(254 - b) << 23);
+  f32x16 he, ho, le, lo_;
+#pragma unroll
+  for (int k = 0; k < 16; ++k) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float y = x[2 * k + h] * inv;
+      // rounded to an eighth of its power of two, at least of one
+      const float q = fmaxf(__uint_as_float(__float_as_uint(y) & 0x7f800000u), 1.f) * 0.125f;
+      const float c = q * 12582912.f;   // 1.5 x 2^23 of these steps
+      const float r = (y + c) - c;
+      if (h) {
+        ho[k] = r;
+        lo_[k] = (y - r) * 16.f;
+      } else {
+        he[k] = r;
+        le[k] = (y - r) * 16.f;
+      }
+    }
+  }
+  (void)step;
+  // (the instruction takes the even values first, then the odd ones)
+  const auto a = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(he, ho, 1.f);
+  const auto c = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(le, lo_, 1.f);
+#pragma unroll
+  for (int k = 0; k < 6; ++k) {
+    hi[k] = static_cast<int>(a[k]);
+    lo[k] = static_cast<int>(c[k]);
+  }
+  hi[6] = hi[7] = lo[6] = lo[7] = 0;
+  return top >= 0x7f800000u ? kFp4NaN | kFp4NaN << 16 : static_cast<uint32_t>(b) | static_cast<uint32_t>(b - 4) << 16;
 }
 
 // MOD: a score cap, distance bias or window.
 template <bool MOD>
 __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp4Args p) {
-  __shared__ __attribute__((aligned(16))) uint8_t s_val[kTilesPerWg][kFp4Stage];
+  // (one LDS object per slot, so that the compiler can tell the one being read
+  // from those that copies in flight write to)
+  __shared__ __attribute__((aligned(16))) Fp4Block raw0;
+  __shared__ __attribute__((aligned(16))) Fp4Block raw1;
+  __shared__ __attribute__((aligned(16))) Fp4Block raw2;
+  __shared__ __attribute__((aligned(16))) Fp4Block raw3;
+  __shared__ __attribute__((aligned(16))) uint8_t s_val[kTilesPerWg][kFp4Stage];   // (many rows: two in turn)
   __shared__ float2 s_ml[kTilesPerWg][KB];
+  __shared__ uint32_t s_odd[4];   // a block's keys with values that are no numbers, a bit each
   __shared__ uint8_t s_depth[ENTMTP_T_MAX];
+  Fp4Block* const ring[kFp4Ring] = {&raw0, &raw1, &raw2, &raw3};
   const int x = static_cast<int>(blockIdx.x);
   const i32x16 head = record(p.plan), item = record(p.plan + p.items_at + static_cast<size_t>(x) * sizeof(PlanItem));
   const PlanHeader h = __builtin_bit_cast(PlanHeader, head);
@@ -93,57 +153,24 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
   const Const<int> pages = as_const<int>(p.table + static_cast<size_t>(b) * p.max_pages);
   // positions before every row's window (their slots may be anyone's by now)
   const int w_lo = MOD ? first_pos(L, p.window) : 0;
+  auto page_at = [&](int pos) { return pages[min(pos >> p.shift, p.max_pages - 1)]; };
+  auto head_at = [&](int page) { return (static_cast<size_t>(page) * p.Hkv + g) * static_cast<size_t>(P * kFp4RowBytes); };
 
-  // this wavefront's blocks: number i is blk_lo + way + i ways; past the last
-  // the last one again
-  const int nb = live ? max(0, (blk_hi - blk_lo - way + ways - 1) / ways) : 0;
-  auto key_at = [&](int i) { return (blk_lo + way + max(min(i, nb - 1), 0) * ways) * KB; };
-  // a block's two runs of 16 keys lie in a page each
-  struct Block {
-    u32x4 k0, k1, v0, v1;
-    uint32_t ks, vs;
-    bool there;   // this lane's page lies in the pool
-  };
-  struct Pages {
-    int lo, hi;
-  };
-  auto pages_of = [&](int i) {
-    const int kb = key_at(i);
-    return Pages{pages[min(kb >> p.shift, p.max_pages - 1)], pages[min((kb + 16) >> p.shift, p.max_pages - 1)]};
-  };
-  auto load = [&](Block& s, int i, Pages pg) {
-    const int key = key_at(i) + li;
-    const int page = li < 16 ? pg.lo : pg.hi;
-    s.there = static_cast<unsigned>(page) < static_cast<unsigned>(p.n_pages);
-    if (MOD && key < w_lo) s.there = false;
-    const size_t base = (static_cast<size_t>(s.there ? page : 0) * p.Hkv + g) * static_cast<size_t>(P * kFp4RowBytes);
-    const int in = key & (P - 1);
-    const uint8_t *kr = p.kp + base, *vr = p.vp + base;
-    // key codes of dims 64 m + 32 lh .. + 31, value codes of dims 64 lh .. + 63
-    s.k0 = *reinterpret_cast<const u32x4*>(kr + in * (HD / 2) + 16 * lh);
-    s.k1 = *reinterpret_cast<const u32x4*>(kr + in * (HD / 2) + 16 * lh + 32);
-    s.ks = *reinterpret_cast<const uint32_t*>(kr + P * (HD / 2) + in * 4);
-    s.v0 = *reinterpret_cast<const u32x4*>(vr + in * (HD / 2) + 32 * lh);
-    s.v1 = *reinterpret_cast<const u32x4*>(vr + in * (HD / 2) + 32 * lh + 16);
-    s.vs = *reinterpret_cast<const uint32_t*>(vr + P * (HD / 2) + in * 4);
-  };
-
-  Block blk[kFp4Ahead];
-  Pages pg[kFp4Ahead + 1];
-#pragma unroll
-  for (int k = 0; k <= kFp4Ahead; ++k) pg[k] = pages_of(k);
-  // the query row (row r of KV head g: head g G + r / T, node r % T), its depth
+  // The query row (row r of KV head g: head g G + r / T, node r % T), its depth
   // and mask, all unconditional: rows past the tree read row 0, see every key
-  // and are never stored
+  // and are never stored.  Matrix instruction m of a block takes dims 64 m + 32 lh
+  // .. + 31.
   const int qrow = qt * kQTile + li;
   const bool qlive = live && qrow < GT;
   const int qnode = qlive ? qrow % T : 0;
   const int qhead = g * p.G + (qlive ? qrow / T : 0);
-  u32x4 qf[8];   // dims 64 m + 32 c + 16 lh .. + 15 (m, c in 0, 1) in qf[4 m + 2 c], [.. + 1]
+  u32x4 qf[2][4];
   {
-    const uint16_t* qp = p.q + (static_cast<size_t>(row0 + qnode) * p.Hq + qhead) * HD + 16 * lh;
+    const uint16_t* qp = p.q + (static_cast<size_t>(row0 + qnode) * p.Hq + qhead) * HD + 32 * lh;
 #pragma unroll
-    for (int s = 0; s < 8; ++s) qf[s] = *reinterpret_cast<const u32x4*>(qp + 32 * (s >> 1) + 8 * (s & 1));
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) qf[m][e] = *reinterpret_cast<const u32x4*>(qp + 64 * m + 8 * e);
   }
   const int qdepth = depth[qnode];
   const int tdepth = depth[min(tid, T - 1)];
@@ -153,62 +180,59 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
   float slope = 0.f;
   if constexpr (MOD)
     if (p.slopes) slope = p.slopes[qhead] * kLog2e;
-#pragma unroll
-  for (int k = 0; k < kFp4Ahead; ++k) load(blk[k], k, pg[k]);
-  Pages next = pg[kFp4Ahead];
-  s_depth[tid] = static_cast<uint8_t>(tdepth);
-  static_assert(kAttnThreads >= ENTMTP_T_MAX, "one thread per node");
-  if (MOD) {
-    wait_lds();
-    stage_barrier();
-  }
-  if (!qlive) mlo = mhi = u32x4{~0u, ~0u, ~0u, ~0u};
-  i32x8 qh[2], ql[2];
-  uint32_t qsc = 0u;   // scale bytes of this half's blocks: of hi for m = 0, 1, then of lo
-#pragma unroll
-  for (int m = 0; m < 2; ++m) {
-    uint32_t sc[2];
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      const u32x4 u = qf[4 * m + 2 * c], w = qf[4 * m + 2 * c + 1];
-      uint32_t top = max(bf16_top(u), bf16_top(w));
-      top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 32, 64)));
-      const int e = static_cast<int>(top >> 7), s = e < 14 ? 7 : e - 7;   // largest below 2^8
-      query8(u, w, __uint_as_float(static_cast<uint32_t>(254 - s) << 23), qh[m], ql[m], 4 * c);
-      sc[c] = top >= 0x7f80u ? kFp4NaN | kFp4NaN << 16 : static_cast<uint32_t>(s) | static_cast<uint32_t>(s - 5) << 16;
-    }
-    qsc |= (lh ? sc[1] : sc[0]) << (8 * m);
-  }
-  const float qs = p.q_scale;
-  const int qpos = L + qdepth;
-  const int w_row = MOD && p.window > 0 ? qpos - p.window + 1 : -1;   // the row's first position
-  const int w_hi = MOD && p.window > 0 ? L + D - p.window + 1 : -1;   // from here on every row sees the prefix
 
   // l_run: the sum of this lane's half of the keys (the halves meet at the end)
   float m_run = -INFINITY, l_run = 0.f;
+  // without MOD a block's products start from minus the row's reference (zero
+  // before its first), so that they come out as the exponents themselves; lift:
+  // how far a block's largest may pass the reference
+  f32x16 ref;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) ref[r] = 0.f;
+  float lift = -INFINITY;
   f32x16 o[4];
 #pragma unroll
   for (int ct = 0; ct < 4; ++ct)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[ct][r] = 0.f;
+  i32x8 qh[2], ql[2];
+  uint32_t qsc = 0u;   // scale bytes of hi for m = 0, 1, then of lo
+  const int qpos = L + qdepth;
+  const int w_row = MOD && p.window > 0 ? qpos - p.window + 1 : -1;   // the row's first position
+  const int w_hi = MOD && p.window > 0 ? L + D - p.window + 1 : -1;   // from here on every row sees the prefix
+  auto settle = [&]() __attribute__((always_inline)) {   // (behind the loads of the first blocks)
+    if (!qlive) mlo = mhi = u32x4{~0u, ~0u, ~0u, ~0u};
+#pragma unroll
+    for (int m = 0; m < 2; ++m) qsc |= query6(qf[m], p.q_scale, qh[m], ql[m]) << (8 * m);
+  };
 
-  // The values' part of the LDS: row li's chunks, and the transposing reads:
-  // row 4 lh + (lane % 16) / 4 of each 8 rows, dims 32 ct + 16 (li / 16) + 4 (lane % 4)
-  uint8_t* const stage = s_val[wave];
-  uint8_t* const srow = stage + li * 256;
-  const int sx = stage_swz(li);
+  // the transposing reads of the values: row 4 lh + (lane % 16) / 4 of each 8
+  // rows, dims 32 ct + 16 (li / 16) + 4 (lane % 4)
   const int vrow = 4 * lh + ((lane & 15) >> 2);
   const int vx = (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ stage_swz(vrow);   // (rows 8 on: chunk ^ 2)
-  const uint8_t* const vbase = stage + vrow * 256 + 8 * (lane & 1);
+  const int voff = vrow * 256 + 8 * (lane & 1);
 
-  auto key_of = [&](int r) { return 8 * (r >> 2) + 4 * lh + (r & 3); };   // accumulator r's key of the block
-  // The block's products as logits in base 2 (with MOD; else they are scaled in
-  // the exponent's fused multiply-add), key r at distance dist(r).
-  // tanh(u) = 1 - 2 / (e^2u + 1) with 2 u / ln 2 from the products: 0 and
-  // infinity of the exponential give -1 and 1.
-  auto bend = [&](f32x16& sacc, auto dist) {
+  // S^T = K Q^T of a block: row li's codes of dims 64 m + 32 lh .. + 31 and its scale bytes
+  auto scores = [&](const u32x4& k0, const u32x4& k1, uint32_t ks, f32x16& sacc) __attribute__((always_inline)) {
+    const i32x8 ka = {static_cast<int>(k0[0]), static_cast<int>(k0[1]), static_cast<int>(k0[2]), static_cast<int>(k0[3]), 0, 0, 0, 0};
+    const i32x8 kc = {static_cast<int>(k1[0]), static_cast<int>(k1[1]), static_cast<int>(k1[2]), static_cast<int>(k1[3]), 0, 0, 0, 0};
+    const int kscale = static_cast<int>(lh ? ks >> 8 : ks), qscale = static_cast<int>(qsc);
+    if constexpr (MOD) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) sacc[r] *= qs;
+      for (int r = 0; r < 16; ++r) sacc[r] = 0.f;
+    } else {
+      sacc = ref;
+    }
+    sacc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, ql[0], sacc, 4, 2, 0, kscale, 2, qscale);
+    sacc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kc, ql[1], sacc, 4, 2, 2, kscale, 3, qscale);
+    sacc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qh[0], sacc, 4, 2, 0, kscale, 0, qscale);
+    sacc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kc, qh[1], sacc, 4, 2, 2, kscale, 1, qscale);
+  };
+  auto key_of = [&](int r) { return 8 * (r >> 2) + 4 * lh + (r & 3); };   // accumulator r's key of the block
+  // MOD: the block's products (scaled by the query) as logits in base 2, key r at
+  // distance dist(r).  tanh(u) = 1 - 2 / (e^2u + 1) with 2 u / ln 2 from the
+  // products: 0 and infinity of the exponential give -1 and 1.
+  auto bend = [&](f32x16& sacc, auto dist) {
     if (p.cap_log2 > 0.f) {
 #pragma unroll
       for (int r = 0; r < 16; ++r)
@@ -219,45 +243,13 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
       for (int r = 0; r < 16; ++r) sacc[r] = fmaf(-slope, static_cast<float>(dist(r)), sacc[r]);
     }
   };
-
-  auto attend = [&](Block& s, int i) {
-    const int kb = key_at(i);
-    // keys of this half's dims: group 2 m + lh of matrix instruction m
-    uint32_t ks = s.ks, vs = s.vs;
-    if (!__all(s.there)) {   // (a page outside the pool: zeros)
-      if (!s.there) {
-        s.k0 = s.k1 = s.v0 = s.v1 = u32x4{0u, 0u, 0u, 0u};
-        ks = vs = 0x7f7f7f7fu;
-      }
-    }
-    ks = lh ? ks >> 8 : ks;
-    f32x16 sacc;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) sacc[r] = 0.f;
-    const i32x8 ka = {static_cast<int>(s.k0[0]), static_cast<int>(s.k0[1]), static_cast<int>(s.k0[2]), static_cast<int>(s.k0[3]), 0, 0, 0, 0};
-    const i32x8 kc = {static_cast<int>(s.k1[0]), static_cast<int>(s.k1[1]), static_cast<int>(s.k1[2]), static_cast<int>(s.k1[3]), 0, 0, 0, 0};
-    const int kscale = static_cast<int>(ks), qscale = static_cast<int>(qsc);
-    sacc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, ql[0], sacc, 4, 0, 0, kscale, 2, qscale);
-    sacc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kc, ql[1], sacc, 4, 0, 2, kscale, 3, qscale);
-    sacc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qh[0], sacc, 4, 0, 0, kscale, 0, qscale);
-    sacc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kc, qh[1], sacc, 4, 0, 2, kscale, 1, qscale);
-    // the values to the LDS; groups that are no numbers as zeros (a zero weight
-    // would make them NaNs in every row) and their keys noted
-    const uint32_t v2 = lh ? vs >> 16 : vs;   // groups 2 lh and 2 lh + 1
-    const uint32_t va = v2 & 0xffu, vb = v2 >> 8 & 0xffu;
-    const unsigned long long bad = __ballot(va == kFp4NaN || vb == kFp4NaN);
-    const uint32_t odd = static_cast<uint32_t>(bad) | static_cast<uint32_t>(bad >> 32);
-    const float sa = va == kFp4NaN ? 0.f : fp4_step(va), sb = vb == kFp4NaN ? 0.f : fp4_step(vb);
-#pragma unroll
-    for (int c = 0; c < 8; ++c) {
-      const uint32_t w = c < 4 ? s.v0[c & 3] : s.v1[c & 3];
-      *reinterpret_cast<u32x4*>(srow + (((8 * lh + c) ^ sx) << 4)) = fp4_values(w, c < 4 ? sa : sb);
-    }
-
-    // what every row sees of the block
+  // The softmax of the block at key kb (lazily raised maximum) and O^T += V^T P^T
+  // from its staged values; odd: its keys whose values are no numbers; prefix: the
+  // caller knows that every row sees every key; ahead: the next block's scores,
+  // which move with the reference they started from.
+  auto attend = [&](int kb, const uint8_t* stage, uint32_t odd, f32x16& sacc, f32x16& ahead, auto prefix) __attribute__((always_inline)) {
     uint32_t vis = ~0u;
-    const bool whole = kb + KB <= L && !(MOD && kb < w_hi);   // (uniform)
-    if (whole) {
+    if (decltype(prefix)::value || (kb + KB <= L && !(MOD && kb < w_hi))) {   // (uniform)
       if constexpr (MOD) bend(sacc, [&](int r) { return qpos - (kb + key_of(r)); });
     } else {
       const int rel = kb - L;
@@ -297,15 +289,16 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
         sacc[r] = __builtin_bit_cast(float, (m & __builtin_bit_cast(int, static_cast<float>(sacc[r]))) | (~m & INT32_C(-0x800000)));
       }
     }
-    if ((vis & odd) != 0u) l_run = NAN;
+    if (odd != 0u) {   // (uniform)
+      if ((vis & odd) != 0u) l_run = NAN;
+    }
     float bmax = -INFINITY;
 #pragma unroll
     for (int r = 0; r < 16; ++r) bmax = fmaxf(bmax, sacc[r]);
     bmax = max_halves(bmax);
-    if constexpr (!MOD) bmax *= qs;
-    const bool need = bmax > m_run + kLazyLog2;
+    const bool need = MOD ? bmax > m_run + kLazyLog2 : bmax > lift;
     if (__any(need)) {
-      const float mn = need ? bmax : m_run;
+      const float mn = !need ? m_run : (MOD || m_run == -INFINITY ? bmax : m_run + bmax);
       const float alpha = !need ? 1.f : (m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - mn));
       l_run *= alpha;
 #pragma unroll
@@ -313,13 +306,23 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[ct][r] *= alpha;
       m_run = mn;
+      if constexpr (!MOD) {
+        const float by = need ? bmax : 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          sacc[r] -= by;
+          ahead[r] -= by;
+          ref[r] -= by;
+        }
+        lift = need ? kLazyLog2 : lift;
+      }
     }
     const float mneg = m_run == -INFINITY ? 0.f : -m_run;
     float pr[16];
     float rsum = 0.f;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      pr[r] = __builtin_amdgcn_exp2f(MOD ? sacc[r] + mneg : fmaf(sacc[r], qs, mneg));
+      pr[r] = __builtin_amdgcn_exp2f(MOD ? sacc[r] + mneg : sacc[r]);
       rsum += pr[r];
     }
     l_run += rsum;
@@ -337,20 +340,200 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
     for (int ct = 0; ct < 4; ++ct)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const uint2 x0 = lds_read_tr(vbase + 16 * u * 256 + ((vx ^ (4 * ct)) << 4));
-        const uint2 x1 = lds_read_tr(vbase + (16 * u + 8) * 256 + ((vx ^ (4 * ct) ^ 2) << 4));
+        const uint2 x0 = lds_read_tr(stage + voff + 16 * u * 256 + ((vx ^ (4 * ct)) << 4));
+        const uint2 x1 = lds_read_tr(stage + voff + (16 * u + 8) * 256 + ((vx ^ (4 * ct) ^ 2) << 4));
         const u32x4 w = {x0.x, x0.y, x1.x, x1.y};
         o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(w), pf[u], o[ct], 0, 0, 0);
       }
   };
 
-  for (int i = 0; i < nb; i += kFp4Ahead) {
+  if (nt >= 3) {
+    // Many rows.  Round i waits for the codes of block i + 1, turns its values into
+    // numbers and takes its scores, then attends to block i; copies of block i + 4
+    // take block i's place, which no one reads behind the barrier.
+    const int nb = blk_hi - blk_lo;
+    const int np = max(0, min(nb, L / KB - blk_lo));   // blocks wholly in the prefix
+    const int n0 = MOD ? min(np, max(0, (w_hi + KB - 1) / KB - blk_lo)) : 0;   // of these, at the window's edge
+    auto pos_of = [&](int i) { return (blk_lo + min(i, nb - 1)) * KB + 16 * (wave & 1); };   // of this wavefront's copies
+    const int crow = lane >> 2, cchunk = wave < 2 ? (lane & 3) ^ ((crow >> 2) & 3) : lane & 3;
+    auto copy = [&](Fp4Block* to, int i, int page) __attribute__((always_inline)) {
+      const int pos = pos_of(i), in = pos & (P - 1);
+      const bool there = static_cast<unsigned>(page) < static_cast<unsigned>(p.n_pages);
+      const __amdgpu_buffer_rsrc_t buf =
+          dma_buffer((wave < 2 ? p.kp : p.vp) + head_at(there ? page : 0), there ? P * kFp4RowBytes : 0);
+      constexpr uint32_t kPast = 1u << 30;   // (past the buffer's end: zeros)
+      const uint32_t codes = MOD && pos + crow < w_lo ? kPast : (in + crow) * (HD / 2) + 16 * cchunk;
+      const uint32_t bytes = lane >= 16 || (MOD && pos + lane < w_lo) ? kPast : P * (HD / 2) + 4 * (in + lane);
+      buf_dma16(buf, codes, (wave < 2 ? to->k : to->v) + 1024 * (wave & 1));
+      buf_dma4(buf, bytes, to->s[wave]);
+    };
+    constexpr int kCopies = 2;
+    // thread (row tid / 8, eighth tid % 8 of it) turns 16 values into numbers;
+    // groups that are no numbers into zeros (a zero weight would make them NaNs in
+    // every row), and their keys are noted
+    const int trow = tid >> 3, tsw = stage_swz(trow);
+    auto turn = [&](const Fp4Block* from, uint8_t* stage, int i) __attribute__((always_inline)) {
+      const uint2 c = *reinterpret_cast<const uint2*>(from->v + 8 * tid);
+      const uint32_t sb = from->s[2 + (trow >> 4)][trow & 15] >> (8 * ((tid & 7) >> 1)) & 0xffu;
+      const unsigned long long bad = __ballot(sb == kFp4NaN);
+      if (bad != 0ull) {
+        if (sb == kFp4NaN) atomicOr(&s_odd[i & 3], 1u << trow);
+      }
+      const float step = sb == kFp4NaN ? 0.f : fp4_step(sb);
+      const u32x4 lo = fp4_values(sb == kFp4NaN ? 0u : c.x, step), hi = fp4_values(sb == kFp4NaN ? 0u : c.y, step);
+      uint8_t* const row = stage + trow * 256;
+      *reinterpret_cast<u32x4*>(row + (((2 * (tid & 7)) ^ tsw) << 4)) = lo;
+      *reinterpret_cast<u32x4*>(row + (((2 * (tid & 7) + 1) ^ tsw) << 4)) = hi;
+    };
+    auto score = [&](const Fp4Block* from, f32x16& sacc) __attribute__((always_inline)) {
+      const int sw = (li >> 2) & 3;
+      const u32x4 k0 = *reinterpret_cast<const u32x4*>(from->k + li * (HD / 2) + ((lh ^ sw) << 4));
+      const u32x4 k1 = *reinterpret_cast<const u32x4*>(from->k + li * (HD / 2) + (((2 + lh) ^ sw) << 4));
+      scores(k0, k1, from->s[li >> 4][li & 15], sacc);
+    };
+    int page[kFp4Ring];
 #pragma unroll
-    for (int k = 0; k < kFp4Ahead; ++k) {
-      if (i + k < nb) {   // (uniform)
-        attend(blk[k], i + k);
-        load(blk[k], i + k + kFp4Ahead, next);
-        next = pages_of(i + k + kFp4Ahead + 1);
+    for (int k = 0; k < kFp4Ring; ++k) page[k] = page_at(pos_of(k));
+#pragma unroll
+    for (int k = 0; k < kFp4Ring; ++k) copy(ring[k], k, page[k]);
+    int next = page_at(pos_of(kFp4Ring));
+    if (tid < 4) s_odd[tid] = 0u;
+    s_depth[tid] = static_cast<uint8_t>(tdepth);
+    static_assert(kAttnThreads >= ENTMTP_T_MAX, "one thread per node");
+    settle();
+    f32x16 sa, sb;
+    wait_vmcnt<(kFp4Ring - 1) * kCopies>();
+    stage_barrier();
+    turn(ring[0], s_val[0], 0);
+    if (live) score(ring[0], sa);
+    // (the odd keys' words: block i's is read in round i, cleared in the next and
+    // written again two rounds later)
+    auto round = [&](int i, auto kc, auto prefix) __attribute__((always_inline)) {
+      constexpr int k = decltype(kc)::value;
+      stage_barrier();
+      copy(ring[k], i + kFp4Ring, next);
+      next = page_at(pos_of(i + kFp4Ring + 1));
+      if (tid == 0) s_odd[(k + 3) & 3] = 0u;
+      turn(ring[(k + 1) % kFp4Ring], s_val[(k + 1) & 1], k + 1);
+      if (live) {
+        f32x16& cur = k & 1 ? sb : sa;
+        f32x16& ahead = k & 1 ? sa : sb;
+        score(ring[(k + 1) % kFp4Ring], ahead);
+        const uint32_t odd = __builtin_amdgcn_readfirstlane(s_odd[k]);
+        attend((blk_lo + i) * KB, s_val[k & 1], odd, cur, ahead, prefix);
+      }
+    };
+    int i0 = 0;
+    if (n0 == 0)
+      for (; i0 + kFp4Ring <= np; i0 += kFp4Ring) {
+        wait_vmcnt<(kFp4Ring - 2) * kCopies>();
+        round(i0, std::integral_constant<int, 0>{}, std::true_type{});
+        wait_vmcnt<(kFp4Ring - 2) * kCopies>();
+        round(i0 + 1, std::integral_constant<int, 1>{}, std::true_type{});
+        wait_vmcnt<(kFp4Ring - 2) * kCopies>();
+        round(i0 + 2, std::integral_constant<int, 2>{}, std::true_type{});
+        wait_vmcnt<(kFp4Ring - 2) * kCopies>();
+        round(i0 + 3, std::integral_constant<int, 3>{}, std::true_type{});
+      }
+    for (; i0 < nb; i0 += kFp4Ring) {
+      wait_vmcnt<(kFp4Ring - 2) * kCopies>();
+      round(i0, std::integral_constant<int, 0>{}, std::false_type{});
+      if (i0 + 1 >= nb) break;
+      wait_vmcnt<(kFp4Ring - 2) * kCopies>();
+      round(i0 + 1, std::integral_constant<int, 1>{}, std::false_type{});
+      if (i0 + 2 >= nb) break;
+      wait_vmcnt<(kFp4Ring - 2) * kCopies>();
+      round(i0 + 2, std::integral_constant<int, 2>{}, std::false_type{});
+      if (i0 + 3 >= nb) break;
+      wait_vmcnt<(kFp4Ring - 2) * kCopies>();
+      round(i0 + 3, std::integral_constant<int, 3>{}, std::false_type{});
+    }
+    wait_vmcnt<0>();   // (copies of blocks past the last)
+  } else {
+    // Few rows: this wavefront's blocks, number i at blk_lo + way + i ways (past the
+    // last the last one again); a block's two runs of 16 keys lie in a page each.
+    const int nb = max(0, (blk_hi - blk_lo - way + ways - 1) / ways);
+    auto key_at = [&](int i) { return (blk_lo + way + max(min(i, nb - 1), 0) * ways) * KB; };
+    struct Block {
+      u32x4 k0, k1, v0, v1;
+      uint32_t ks, vs;
+      bool there;   // this lane's page lies in the pool
+    };
+    struct Pages {
+      int lo, hi;
+    };
+    auto pages_of = [&](int i) { return Pages{page_at(key_at(i)), page_at(key_at(i) + 16)}; };
+    auto load = [&](Block& s, int i, Pages pg) {
+      const int key = key_at(i) + li;
+      const int page = li < 16 ? pg.lo : pg.hi;
+      s.there = static_cast<unsigned>(page) < static_cast<unsigned>(p.n_pages);
+      if (MOD && key < w_lo) s.there = false;
+      const size_t base = head_at(s.there ? page : 0);
+      const int in = key & (P - 1);
+      const uint8_t *kr = p.kp + base, *vr = p.vp + base;
+      // key codes of dims 64 m + 32 lh .. + 31, value codes of dims 64 lh .. + 63
+      s.k0 = *reinterpret_cast<const u32x4*>(kr + in * (HD / 2) + 16 * lh);
+      s.k1 = *reinterpret_cast<const u32x4*>(kr + in * (HD / 2) + 16 * lh + 32);
+      s.ks = *reinterpret_cast<const uint32_t*>(kr + P * (HD / 2) + in * 4);
+      s.v0 = *reinterpret_cast<const u32x4*>(vr + in * (HD / 2) + 32 * lh);
+      s.v1 = *reinterpret_cast<const u32x4*>(vr + in * (HD / 2) + 32 * lh + 16);
+      s.vs = *reinterpret_cast<const uint32_t*>(vr + P * (HD / 2) + in * 4);
+    };
+    Block blk[kFp4Ahead];
+    Pages pg[kFp4Ahead + 1];
+#pragma unroll
+    for (int k = 0; k <= kFp4Ahead; ++k) pg[k] = pages_of(k);
+#pragma unroll
+    for (int k = 0; k < kFp4Ahead; ++k) load(blk[k], k, pg[k]);
+    Pages next = pg[kFp4Ahead];
+    s_depth[tid] = static_cast<uint8_t>(tdepth);
+    if (MOD) {
+      wait_lds();
+      stage_barrier();
+    }
+    settle();
+    uint8_t* const stage = s_val[wave];
+    uint8_t* const srow = stage + li * 256;
+    const int sx = stage_swz(li);
+    auto step = [&](Block& s, int i) __attribute__((always_inline)) {
+      uint32_t ks = s.ks, vs = s.vs;
+      if (!__all(s.there)) {   // (a page outside the pool: zeros)
+        if (!s.there) {
+          s.k0 = s.k1 = s.v0 = s.v1 = u32x4{0u, 0u, 0u, 0u};
+          ks = vs = 0x7f7f7f7fu;
+        }
+      }
+      f32x16 sacc;
+      scores(s.k0, s.k1, ks, sacc);
+      // the values to the LDS; groups that are no numbers as zeros (a zero weight
+      // would make them NaNs in every row) and their keys noted
+      const uint32_t v2 = lh ? vs >> 16 : vs;   // groups 2 lh and 2 lh + 1
+      const uint32_t va = v2 & 0xffu, vb = v2 >> 8 & 0xffu;
+      const unsigned long long bad = __ballot(va == kFp4NaN || vb == kFp4NaN);
+      const uint32_t odd = static_cast<uint32_t>(bad) | static_cast<uint32_t>(bad >> 32);
+      if (odd != 0u) {   // (uniform)
+        if (va == kFp4NaN) s.v0 = u32x4{0u, 0u, 0u, 0u};
+        if (vb == kFp4NaN) s.v1 = u32x4{0u, 0u, 0u, 0u};
+      }
+      const float sa = fp4_step(va == kFp4NaN ? 127u : va), sb = fp4_step(vb == kFp4NaN ? 127u : vb);
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        const uint32_t w = c < 4 ? s.v0[c & 3] : s.v1[c & 3];
+        *reinterpret_cast<u32x4*>(srow + (((8 * lh + c) ^ sx) << 4)) = fp4_values(w, c < 4 ? sa : sb);
+      }
+      f32x16 none;   // (no scores ahead)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) none[r] = 0.f;
+      attend(key_at(i), stage, odd, sacc, none, std::false_type{});
+    };
+    for (int i = 0; i < nb; i += kFp4Ahead) {
+#pragma unroll
+      for (int k = 0; k < kFp4Ahead; ++k) {
+        if (i + k < nb) {   // (uniform)
+          step(blk[k], i + k);
+          load(blk[k], i + k + kFp4Ahead, next);
+          next = pages_of(i + k + kFp4Ahead + 1);
+        }
       }
     }
   }
