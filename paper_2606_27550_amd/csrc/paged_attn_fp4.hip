@@ -59,10 +59,28 @@ struct PagedFp4Args : PagedCall {
 };
 
 // Chunk c (16 bytes) of row r of the staged values lies at c ^ stage_swz(r): a
-// store takes one chunk of 16 rows, or every other one of two, a transposing read
-// 32 lanes' 64 bytes of four rows; all then cover all banks.  Of the keys' codes
-// chunk c of row r lies at c ^ (r / 4 % 4).
-__device__ __forceinline__ int stage_swz(int r) { return 4 * (r & 3) + (((r >> 2) & 3) ^ (r & 1)); }
+// store takes one chunk of 16 rows, every other one of two, or every fourth of
+// four, a transposing read 64 bytes of four rows or 32 of eight; all then cover all
+// banks.  (Eight rows on: chunk ^ 1, sixteen: the same.)  Of the keys' codes chunk
+// c of row r lies at c ^ (r / 4 % 4).
+__device__ __forceinline__ int stage_swz(int r) {
+  return 4 * (r & 3) + ((((r >> 3) & 1) | ((r >> 1) & 2)) ^ (r & 3));
+}
+
+// The largest of a lane's value and those of the lanes 16, 32 and 48 away.
+__device__ __forceinline__ float max_quarters(float x) {
+  const uint32_t u = __float_as_uint(x);
+  const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return max_halves(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+
+// 16 or 4 bytes at byte voff of the buffer (zeros past its end).
+__device__ __forceinline__ u32x4 buf_load16(__amdgpu_buffer_rsrc_t buf, uint32_t voff) {
+  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(buf, static_cast<int>(voff), 0, 0));
+}
+__device__ __forceinline__ uint32_t buf_load4(__amdgpu_buffer_rsrc_t buf, uint32_t voff) {
+  return __builtin_bit_cast(uint32_t, buf_load(buf, voff));
+}
 
 // Four bytes a lane to the LDS, as buf_dma16.
 __device__ __forceinline__ void buf_dma4(__amdgpu_buffer_rsrc_t buf, uint32_t voff, void* lds) {
@@ -159,18 +177,20 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
   // The query row (row r of KV head g: head g G + r / T, node r % T), its depth
   // and mask, all unconditional: rows past the tree read row 0, see every key
   // and are never stored.  Matrix instruction m of a block takes dims 64 m + 32 lh
-  // .. + 31.
-  const int qrow = qt * kQTile + li;
+  // .. + 31 (small: the only one dims 32 lq .. + 31).
+  const bool small = GT <= 16;   // (16 columns of queries: lane % 16, groups of 32 dims: lane / 16)
+  const int lc = lane & 15, lq = lane >> 4;
+  const int qrow = qt * kQTile + (small ? lc : li);
   const bool qlive = live && qrow < GT;
   const int qnode = qlive ? qrow % T : 0;
   const int qhead = g * p.G + (qlive ? qrow / T : 0);
   u32x4 qf[2][4];
   {
-    const uint16_t* qp = p.q + (static_cast<size_t>(row0 + qnode) * p.Hq + qhead) * HD + 32 * lh;
+    const uint16_t* qp = p.q + (static_cast<size_t>(row0 + qnode) * p.Hq + qhead) * HD + 32 * (small ? lq : lh);
 #pragma unroll
     for (int m = 0; m < 2; ++m)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) qf[m][e] = *reinterpret_cast<const u32x4*>(qp + 64 * m + 8 * e);
+      for (int e = 0; e < 4; ++e) qf[m][e] = *reinterpret_cast<const u32x4*>(qp + (small ? 0 : 64 * m) + 8 * e);
   }
   const int qdepth = depth[qnode];
   const int tdepth = depth[min(tid, T - 1)];
@@ -186,10 +206,266 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
   // without MOD a block's products start from minus the row's reference (zero
   // before its first), so that they come out as the exponents themselves; lift:
   // how far a block's largest may pass the reference
+  float lift = -INFINITY;
+  const int qpos = L + qdepth;
+  const int w_row = MOD && p.window > 0 ? qpos - p.window + 1 : -1;   // the row's first position
+  const int w_hi = MOD && p.window > 0 ? L + D - p.window + 1 : -1;   // from here on every row sees the prefix
+  // The keys of the block at kb, which reaches into the tree or past it, that the
+  // row sees, a bit each.
+  auto seen = [&](int kb) __attribute__((always_inline)) {
+    const int rel = kb - L;
+    auto word = [&](int w) {   // (w is uniform)
+      uint32_t m = 0u;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) m = w == k ? (k < 4 ? mlo[k & 3] : mhi[k & 3]) : m;
+      return m;
+    };
+    uint32_t vis = ~0u;
+    if (rel + KB > 0) {
+      if (rel < 0) {
+        const int npre = -rel;
+        vis = (0xFFFFFFFFu >> (32 - npre)) | (mlo[0] << npre);
+      } else {
+        const int wi = rel >> 5, sh = rel & 31;
+        const uint32_t lo = word(wi), hi = word(wi + 1);
+        vis = sh ? (lo >> sh) | (hi << (32 - sh)) : lo;
+      }
+    }
+    if (nkeys - kb < KB) vis &= (1u << (nkeys - kb)) - 1u;
+    return vis;
+  };
+  // Where the row's output (one split) or its partial goes; of the latter's (max,
+  // sum) one lane of the row stores them.
+  auto target = [&]() __attribute__((always_inline)) {
+    if (nsplit == 1) {
+      const int r = qrow < GT ? qrow : 0;
+      return p.out + (static_cast<size_t>(row0 + r % T) * p.Hq + g * p.G + r / T) * HD;
+    }
+    const long long part = static_cast<long long>((static_cast<unsigned long long>(it.part_hi) << 32) | it.part_lo);
+    const size_t prow = part + (static_cast<size_t>(split) * p.Hkv + g) * it.rows_pad + qrow;
+    if ((small ? lq : lh) == 0 && qrow < GT) {
+      p.part_ml[prow * 2 + 0] = m_run;
+      p.part_ml[prow * 2 + 1] = l_run;
+    }
+    return p.part_o + prow * HD;
+  };
+
+  if (small) {
+    // At most 16 rows: as the few below, with 16 columns of queries (16 x 16 x 128 for
+    // the scores of 16 keys, 16 x 16 x 32 for the outputs' 16 dims), half of the
+    // products and of the softmax, and copies of whole runs of 16 rows.
+    const int nb = max(0, (blk_hi - blk_lo - wave + 3) / 4);
+    auto key_at = [&](int i) { return (blk_lo + wave + max(min(i, nb - 1), 0) * 4) * KB; };
+    struct Block {
+      u32x4 k[2], v[2];
+      uint32_t ks[2], vs[2];
+    };
+    struct Pages {
+      int lo, hi;
+    };
+    auto pages_of = [&](int i) { return Pages{page_at(key_at(i)), page_at(key_at(i) + 16)}; };
+    constexpr uint32_t kPast = 1u << 30;   // (past the buffer's end: zeros)
+    // (run j of 16 keys; a key's codes by lane (key lc, group lq), a value's by lane
+    // (row lane / 4, group lane % 4))
+    auto load = [&](Block& s, int i, Pages pg) __attribute__((always_inline)) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int pos = key_at(i) + 16 * j, in = pos & (P - 1), page = j ? pg.hi : pg.lo;
+        const bool there = static_cast<unsigned>(page) < static_cast<unsigned>(p.n_pages);
+        const size_t at = head_at(there ? page : 0);
+        const __amdgpu_buffer_rsrc_t kb = dma_buffer(p.kp + at, there ? P * kFp4RowBytes : 0);
+        const __amdgpu_buffer_rsrc_t vb = dma_buffer(p.vp + at, there ? P * kFp4RowBytes : 0);
+        const uint32_t kpast = MOD && pos + lc < w_lo ? kPast : 0, vpast = MOD && pos + (lane >> 2) < w_lo ? kPast : 0;
+        s.k[j] = buf_load16(kb, kpast + (in + lc) * (HD / 2) + 16 * lq);
+        s.ks[j] = buf_load4(kb, kpast + P * (HD / 2) + 4 * (in + lc));
+        s.v[j] = buf_load16(vb, vpast + in * (HD / 2) + 16 * lane);
+        s.vs[j] = buf_load4(vb, vpast + P * (HD / 2) + 4 * (in + (lane >> 2)));
+      }
+    };
+    constexpr int kAhead = 4;
+    Block blk[kAhead];
+    Pages pg[kAhead + 1];
+#pragma unroll
+    for (int k = 0; k <= kAhead; ++k) pg[k] = pages_of(k);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) load(blk[k], k, pg[k]);
+    Pages next = pg[kAhead];
+    s_depth[tid] = static_cast<uint8_t>(tdepth);
+    if (MOD) {
+      wait_lds();
+      stage_barrier();
+    }
+    if (!qlive) mlo = mhi = u32x4{~0u, ~0u, ~0u, ~0u};
+    i32x8 hi, lo;
+    const int qscale = static_cast<int>(query6(qf[0], p.q_scale, hi, lo));   // bytes 0 and 2
+    f32x4 out[8], base = {0.f, 0.f, 0.f, 0.f};   // (base: minus the row's reference)
+#pragma unroll
+    for (int ct = 0; ct < 8; ++ct) out[ct] = f32x4{0.f, 0.f, 0.f, 0.f};
+    uint8_t* const stage = s_val[wave];
+    const int wrow = lane >> 2, wsw = stage_swz(wrow);   // (row 16 on: the same)
+    const int rrow = 4 * lq + (lc >> 2), rsw = stage_swz(rrow);
+    uint8_t* const put = stage + wrow * 256;
+    const uint8_t* const get = stage + rrow * 256 + 8 * (lane & 1);
+    auto step = [&](Block& s, int i) __attribute__((always_inline)) {
+      const int kb = key_at(i);
+      f32x4 sc[2];
+      uint32_t odd = 0u;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const i32x8 ka = {static_cast<int>(s.k[j][0]), static_cast<int>(s.k[j][1]), static_cast<int>(s.k[j][2]), static_cast<int>(s.k[j][3]), 0, 0, 0, 0};
+        const int kscale = static_cast<int>(s.ks[j] >> (8 * lq));
+        sc[j] = MOD ? f32x4{0.f, 0.f, 0.f, 0.f} : base;
+        sc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ka, lo, sc[j], 4, 2, 0, kscale, 2, qscale);
+        sc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ka, hi, sc[j], 4, 2, 0, kscale, 0, qscale);
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const uint32_t b = s.vs[j] >> (8 * (lane & 3)) & 0xffu;
+        const unsigned long long bad = __ballot(b == kFp4NaN);
+        if (bad != 0ull) {   // (uniform) rows' groups as nibbles, a bit a row
+          if (b == kFp4NaN) s.v[j] = u32x4{0u, 0u, 0u, 0u};
+          unsigned long long m = bad | bad >> 1;
+          m |= m >> 2;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) odd |= static_cast<uint32_t>(m >> (4 * r) & 1ull) << (16 * j + r);
+        }
+        const float st = fp4_step(b == kFp4NaN ? 127u : b);
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          *reinterpret_cast<u32x4*>(put + 16 * j * 256 + (((4 * (lane & 3) + c) ^ wsw) << 4)) = fp4_values(s.v[j][c], st);
+      }
+      auto key_of = [&](int j, int r) { return 16 * j + 4 * lq + r; };
+      auto bend16 = [&](auto dist) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            if (p.cap_log2 > 0.f)
+              sc[j][r] = fmaf(-2.f * p.cap_log2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(sc[j][r]) + 1.f), p.cap_log2);
+            if (p.slopes) sc[j][r] = fmaf(-slope, static_cast<float>(dist(key_of(j, r))), sc[j][r]);
+          }
+      };
+      uint32_t vis = ~0u;
+      if (kb + KB <= L && !(MOD && kb < w_hi)) {   // (uniform)
+        if constexpr (MOD) bend16([&](int n) { return qpos - (kb + n); });
+      } else {
+        vis = seen(kb);
+        if constexpr (MOD) {
+          auto pos_k = [&](int n) {
+            const int j = kb + n - L;
+            return j < 0 ? kb + n : L + s_depth[min(j, ENTMTP_T_MAX - 1)];
+          };
+          bend16([&](int n) { return qpos - pos_k(n); });
+          if (min(kb, L) < w_hi) {
+            for (int n = 0; n < KB; ++n)
+              if (pos_k(n) < w_row) vis &= ~(1u << n);
+          }
+        }
+        const uint32_t mine = vis >> (4 * lq);
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if ((mine >> (16 * j + r) & 1u) == 0u) sc[j][r] = -INFINITY;
+      }
+      if (odd != 0u) {   // (uniform)
+        if ((vis & odd) != 0u) l_run = NAN;
+      }
+      float bmax = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])),
+                         fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
+      bmax = max_quarters(bmax);
+      const bool need = MOD ? bmax > m_run + kLazyLog2 : bmax > lift;
+      if (__any(need)) {
+        const float mn = !need ? m_run : (MOD || m_run == -INFINITY ? bmax : m_run + bmax);
+        const float alpha = !need ? 1.f : (m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - mn));
+        l_run *= alpha;
+#pragma unroll
+        for (int ct = 0; ct < 8; ++ct) out[ct] *= alpha;
+        m_run = mn;
+        if constexpr (!MOD) {
+          const float by = need ? bmax : 0.f;
+          sc[0] -= by;
+          sc[1] -= by;
+          base -= by;
+          lift = need ? kLazyLog2 : lift;
+        }
+      }
+      const float mneg = m_run == -INFINITY ? 0.f : -m_run;
+      u32x4 w;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        float e[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          e[r] = __builtin_amdgcn_exp2f(MOD ? sc[j][r] + mneg : sc[j][r]);
+          l_run += e[r];
+        }
+        w[2 * j] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{e[0], e[1]}), bf16x2));
+        w[2 * j + 1] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{e[2], e[3]}), bf16x2));
+      }
+#pragma unroll
+      for (int ct = 0; ct < 8; ++ct) {
+        const uint8_t* const at = get + (((2 * ct + ((lane & 3) >> 1)) ^ rsw) << 4);
+        const uint2 x0 = lds_read_tr(at), x1 = lds_read_tr(at + 16 * 256);
+        out[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(u32x4{x0.x, x0.y, x1.x, x1.y}), as_bf16x8(w), out[ct], 0, 0, 0);
+      }
+    };
+    for (int i = 0; i < nb; i += kAhead) {
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        if (i + k < nb) {   // (uniform)
+          step(blk[k], i + k);
+          load(blk[k], i + k + kAhead, next);
+          next = pages_of(i + k + kAhead + 1);
+        }
+      }
+    }
+    l_run += __shfl_xor(l_run, 16, 64);
+    l_run += __shfl_xor(l_run, 32, 64);
+    // the four wavefronts' sums meet
+    for (int half = 2; half >= 1; half >>= 1) {
+      __syncthreads();
+      if (wave >= half && wave < 2 * half) {
+        f32x4* const at = reinterpret_cast<f32x4*>(s_val[wave - half]);
+#pragma unroll
+        for (int ct = 0; ct < 8; ++ct) at[ct * 64 + lane] = out[ct];
+        if (lq == 0) s_ml[wave - half][lc] = make_float2(m_run, l_run);
+      }
+      __syncthreads();
+      if (wave < half) {
+        const f32x4* const at = reinterpret_cast<const f32x4*>(s_val[wave]);
+        const float2 ml = s_ml[wave][lc];
+        const float mn = fmaxf(m_run, ml.x);
+        // (no key seen: max -inf, nothing to add; a NaN of the sum stays)
+        const float a0 = m_run == mn ? 1.f : __builtin_amdgcn_exp2f(m_run - mn);
+        const float a1 = ml.x == mn ? 1.f : __builtin_amdgcn_exp2f(ml.x - mn);
+        m_run = mn;
+        l_run = l_run * a0 + ml.y * a1;
+#pragma unroll
+        for (int ct = 0; ct < 8; ++ct) {
+          const f32x4 v = at[ct * 64 + lane];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) out[ct][e] = out[ct][e] * a0 + v[e] * a1;
+        }
+      }
+    }
+    if (wave > 0) return;
+    uint16_t* const dst = target();
+    const float il = l_run == 0.f && nsplit > 1 ? 0.f : 1.f / l_run;
+    if (qrow < GT) {
+#pragma unroll
+      for (int ct = 0; ct < 8; ++ct) {
+        const uint2 v = {__builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{out[ct][0] * il, out[ct][1] * il}), bf16x2)),
+                         __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{out[ct][2] * il, out[ct][3] * il}), bf16x2))};
+        *reinterpret_cast<uint2*>(dst + 16 * ct + 4 * lq) = v;
+      }
+    }
+    return;
+  }
+
   f32x16 ref;
 #pragma unroll
   for (int r = 0; r < 16; ++r) ref[r] = 0.f;
-  float lift = -INFINITY;
   f32x16 o[4];
 #pragma unroll
   for (int ct = 0; ct < 4; ++ct)
@@ -197,9 +473,6 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
     for (int r = 0; r < 16; ++r) o[ct][r] = 0.f;
   i32x8 qh[2], ql[2];
   uint32_t qsc = 0u;   // scale bytes of hi for m = 0, 1, then of lo
-  const int qpos = L + qdepth;
-  const int w_row = MOD && p.window > 0 ? qpos - p.window + 1 : -1;   // the row's first position
-  const int w_hi = MOD && p.window > 0 ? L + D - p.window + 1 : -1;   // from here on every row sees the prefix
   auto settle = [&]() __attribute__((always_inline)) {   // (behind the loads of the first blocks)
     if (!qlive) mlo = mhi = u32x4{~0u, ~0u, ~0u, ~0u};
 #pragma unroll
@@ -209,7 +482,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
   // the transposing reads of the values: row 4 lh + (lane % 16) / 4 of each 8
   // rows, dims 32 ct + 16 (li / 16) + 4 (lane % 4)
   const int vrow = 4 * lh + ((lane & 15) >> 2);
-  const int vx = (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ stage_swz(vrow);   // (rows 8 on: chunk ^ 2)
+  const int vx = (2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ stage_swz(vrow);   // (rows 8 on: chunk ^ 1)
   const int voff = vrow * 256 + 8 * (lane & 1);
 
   // S^T = K Q^T of a block: row li's codes of dims 64 m + 32 lh .. + 31 and its scale bytes
@@ -247,29 +520,12 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
   // from its staged values; odd: its keys whose values are no numbers; prefix: the
   // caller knows that every row sees every key; ahead: the next block's scores,
   // which move with the reference they started from.
-  auto attend = [&](int kb, const uint8_t* stage, uint32_t odd, f32x16& sacc, f32x16& ahead, auto prefix) __attribute__((always_inline)) {
+  auto attend = [&](int kb, const uint8_t* stage, uint32_t odd, f32x16& sacc, auto& ahead, auto prefix) __attribute__((always_inline)) {
     uint32_t vis = ~0u;
     if (decltype(prefix)::value || (kb + KB <= L && !(MOD && kb < w_hi))) {   // (uniform)
       if constexpr (MOD) bend(sacc, [&](int r) { return qpos - (kb + key_of(r)); });
     } else {
-      const int rel = kb - L;
-      auto word = [&](int w) {   // (w is uniform)
-        uint32_t m = 0u;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) m = w == k ? (k < 4 ? mlo[k & 3] : mhi[k & 3]) : m;
-        return m;
-      };
-      if (rel + KB <= 0) {
-        vis = ~0u;
-      } else if (rel < 0) {
-        const int npre = -rel;
-        vis = (0xFFFFFFFFu >> (32 - npre)) | (mlo[0] << npre);
-      } else {
-        const int wi = rel >> 5, sh = rel & 31;
-        const uint32_t lo = word(wi), hi = word(wi + 1);
-        vis = sh ? (lo >> sh) | (hi << (32 - sh)) : lo;
-      }
-      if (nkeys - kb < KB) vis &= (1u << (nkeys - kb)) - 1u;
+      vis = seen(kb);
       if constexpr (MOD) {
         // (a tree key's position is that of its depth)
         auto pos_k = [&](int n) {
@@ -311,7 +567,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           sacc[r] -= by;
-          ahead[r] -= by;
+          if constexpr (!std::is_null_pointer_v<std::remove_cv_t<std::remove_reference_t<decltype(ahead)>>>) ahead[r] -= by;
           ref[r] -= by;
         }
         lift = need ? kLazyLog2 : lift;
@@ -341,7 +597,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const uint2 x0 = lds_read_tr(stage + voff + 16 * u * 256 + ((vx ^ (4 * ct)) << 4));
-        const uint2 x1 = lds_read_tr(stage + voff + (16 * u + 8) * 256 + ((vx ^ (4 * ct) ^ 2) << 4));
+        const uint2 x1 = lds_read_tr(stage + voff + (16 * u + 8) * 256 + ((vx ^ (4 * ct) ^ 1) << 4));
         const u32x4 w = {x0.x, x0.y, x1.x, x1.y};
         o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(w), pf[u], o[ct], 0, 0, 0);
       }
@@ -521,9 +777,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
         const uint32_t w = c < 4 ? s.v0[c & 3] : s.v1[c & 3];
         *reinterpret_cast<u32x4*>(srow + (((8 * lh + c) ^ sx) << 4)) = fp4_values(w, c < 4 ? sa : sb);
       }
-      f32x16 none;   // (no scores ahead)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) none[r] = 0.f;
+      std::nullptr_t none{};   // (no scores ahead)
       attend(key_at(i), stage, odd, sacc, none, std::false_type{});
     };
     for (int i = 0; i < nb; i += kFp4Ahead) {
@@ -579,19 +833,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
   // half lh) holds dims 32 ct + 8 j + 4 lh + i in o[ct][4 j + i]; the halves
   // trade a chunk so that each stores 16 bytes: lane 0..31 dims 8 j .. 8 j + 7
   // of even j, lane 32..63 of odd j.
-  uint16_t* dst;
-  if (nsplit == 1) {
-    const int r = qrow < GT ? qrow : 0;
-    dst = p.out + (static_cast<size_t>(row0 + r % T) * p.Hq + g * p.G + r / T) * HD;
-  } else {
-    const long long part = static_cast<long long>((static_cast<unsigned long long>(it.part_hi) << 32) | it.part_lo);
-    const size_t prow = part + (static_cast<size_t>(split) * p.Hkv + g) * it.rows_pad + qrow;
-    dst = p.part_o + prow * HD;
-    if (lh == 0 && qrow < GT) {
-      p.part_ml[prow * 2 + 0] = m_run;
-      p.part_ml[prow * 2 + 1] = l_run;
-    }
-  }
+  uint16_t* const dst = target();
   // (a split may hold no key that the row sees: zeros; a whole row sees its own)
   const float il = l_run == 0.f && nsplit > 1 ? 0.f : 1.f / l_run;
   auto pack = [&](float u, float v) {
