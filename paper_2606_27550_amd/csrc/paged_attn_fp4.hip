@@ -36,7 +36,7 @@
 namespace entmtp {
 namespace {
 
-constexpr int kFp4Ahead = 3;               // blocks in flight per wavefront (few rows)
+constexpr int kFp4Ahead = 2;               // blocks in flight per wavefront (few rows)
 constexpr int kFp4Ring = 4;                // blocks in the LDS (many rows)
 constexpr int kFp4Stage = KB * HD * 2;     // bytes of a block's values in bf16
 
@@ -282,7 +282,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
         s.vs[j] = buf_load4(vb, vpast + P * (HD / 2) + 4 * (in + (lane >> 2)));
       }
     };
-    constexpr int kAhead = 4;
+    constexpr int kAhead = 2;
     Block blk[kAhead];
     Pages pg[kAhead + 1];
 #pragma unroll
@@ -410,16 +410,20 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
         out[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(u32x4{x0.x, x0.y, x1.x, x1.y}), as_bf16x8(w), out[ct], 0, 0, 0);
       }
     };
-    for (int i = 0; i < nb; i += kAhead) {
+    // (whole rounds without a branch, so that a wait for a block leaves the later
+    // ones in flight; the last blocks have been asked for by then)
+    int i0 = 0;
+    for (; i0 + kAhead <= nb; i0 += kAhead) {
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
-        if (i + k < nb) {   // (uniform)
-          step(blk[k], i + k);
-          load(blk[k], i + k + kAhead, next);
-          next = pages_of(i + k + kAhead + 1);
-        }
+        step(blk[k], i0 + k);
+        load(blk[k], i0 + k + kAhead, next);
+        next = pages_of(i0 + k + kAhead + 1);
       }
     }
+#pragma unroll
+    for (int k = 0; k < kAhead - 1; ++k)
+      if (i0 + k < nb) step(blk[k], i0 + k);
     l_run += __shfl_xor(l_run, 16, 64);
     l_run += __shfl_xor(l_run, 32, 64);
     // the four wavefronts' sums meet
