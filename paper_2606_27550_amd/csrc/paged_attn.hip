@@ -791,7 +791,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_kernel(PagedArgs p
   } else {
     const long long part = static_cast<long long>((static_cast<unsigned long long>(it.part_hi) << 32) | it.part_lo);
     const size_t prow = part + (static_cast<size_t>(split) * p.Hkv + g) * it.rows_pad + row;
-    dst = p.part_o + prow * HD;
+    dst = static_cast<uint16_t*>(p.part_o) + prow * HD;
     if (lh == 0 && row < GT) {
       p.part_ml[prow * 2 + 0] = m_run;
       p.part_ml[prow * 2 + 1] = l_run;
@@ -957,5 +957,5 @@ extern "C" int32_t entmtp_tree_attn_paged(const entmtp_bank* bank, int32_t B, co
     mod ? go(paged_attn_kernel<kNear, true>) : go(paged_attn_kernel<kNear, false>);
   if (int32_t rc = launch_status("tree_attn_paged launch")) return rc;
   if (!sh.splits) return ENTMTP_OK;
-  return launch_merge(a, s);
+  return launch_merge<false>(a, s);
 }

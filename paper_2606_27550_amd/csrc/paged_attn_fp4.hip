@@ -234,20 +234,26 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
     if (nkeys - kb < KB) vis &= (1u << (nkeys - kb)) - 1u;
     return vis;
   };
-  // Where the row's output (one split) or its partial goes; of the latter's (max,
-  // sum) one lane of the row stores them.
-  auto target = [&]() __attribute__((always_inline)) {
-    if (nsplit == 1) {
-      const int r = qrow < GT ? qrow : 0;
-      return p.out + (static_cast<size_t>(row0 + r % T) * p.Hq + g * p.G + r / T) * HD;
-    }
+  // The row's place in the output (one split), or among the partials; of the
+  // latter's (max, sum) one lane of the row stores them.
+  auto out_row = [&]() __attribute__((always_inline)) {
+    const int r = qrow < GT ? qrow : 0;
+    return p.out + (static_cast<size_t>(row0 + r % T) * p.Hq + g * p.G + r / T) * HD;
+  };
+  // (top: the largest magnitude of the row's normalised output; by: what brings it
+  // to [2^14, 2^15), where the smaller ones keep fp16's eleven bits)
+  auto part_row = [&](float top, float& by) __attribute__((always_inline)) {
+    const int e = max(static_cast<int>(__float_as_uint(top) >> 23), 15);
+    by = e == 255 ? 1.f : __uint_as_float(static_cast<uint32_t>(268 - e) << 23);
+    const float undo = e == 255 ? 1.f : __uint_as_float(static_cast<uint32_t>(e - 14) << 23);
     const long long part = static_cast<long long>((static_cast<unsigned long long>(it.part_hi) << 32) | it.part_lo);
     const size_t prow = part + (static_cast<size_t>(split) * p.Hkv + g) * it.rows_pad + qrow;
-    if ((small ? lq : lh) == 0 && qrow < GT) {
-      p.part_ml[prow * 2 + 0] = m_run;
-      p.part_ml[prow * 2 + 1] = l_run;
-    }
-    return p.part_o + prow * HD;
+    if ((small ? lq : lh) == 0 && qrow < GT) *reinterpret_cast<float4*>(p.part_ml + prow * 4) = make_float4(m_run, l_run, undo, 0.f);
+    return static_cast<uint16_t*>(p.part_o) + prow * HD;
+  };
+  typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+  auto halves = [](float a, float b) __attribute__((always_inline)) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), f16x2));
   };
 
   if (small) {
@@ -454,8 +460,28 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
       }
     }
     if (wave > 0) return;
-    uint16_t* const dst = target();
-    const float il = l_run == 0.f && nsplit > 1 ? 0.f : 1.f / l_run;
+    if (nsplit > 1) {
+      // (a split may hold no key that the row sees: zeros)
+      const float il = l_run == 0.f ? 0.f : 1.f / l_run;
+      float top = 0.f, by;
+#pragma unroll
+      for (int ct = 0; ct < 8; ++ct)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          out[ct][e] *= il;
+          top = fmaxf(top, fabsf(out[ct][e]));
+        }
+      uint16_t* const dst = part_row(max_quarters(top), by);
+      if (qrow < GT) {
+#pragma unroll
+        for (int ct = 0; ct < 8; ++ct)
+          *reinterpret_cast<uint2*>(dst + 16 * ct + 4 * lq) =
+              uint2{halves(out[ct][0] * by, out[ct][1] * by), halves(out[ct][2] * by, out[ct][3] * by)};
+      }
+      return;
+    }
+    const float il = 1.f / l_run;   // (a whole row sees its own key)
+    uint16_t* const dst = out_row();
     if (qrow < GT) {
 #pragma unroll
       for (int ct = 0; ct < 8; ++ct) {
@@ -834,14 +860,30 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
   if (!live || way > 0) return;
 
   // this wave's tile: the output (one split) or its partial.  Lane (query li,
-  // half lh) holds dims 32 ct + 8 j + 4 lh + i in o[ct][4 j + i]; the halves
-  // trade a chunk so that each stores 16 bytes: lane 0..31 dims 8 j .. 8 j + 7
-  // of even j, lane 32..63 of odd j.
-  uint16_t* const dst = target();
+  // half lh) holds dims 32 ct + 8 j + 4 lh + i in o[ct][4 j + i].
+  // The halves trade a chunk so that each stores 16 bytes: lane 0..31 dims 8 j ..
+  // 8 j + 7 of even j, lane 32..63 of odd j.
   // (a split may hold no key that the row sees: zeros; a whole row sees its own)
   const float il = l_run == 0.f && nsplit > 1 ? 0.f : 1.f / l_run;
+  uint16_t* dst;
+  float by = 1.f;
+  const bool whole = nsplit == 1;   // (uniform)
+#pragma unroll
+  for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[ct][r] *= il;
+  if (whole) {
+    dst = out_row();
+  } else {
+    float top = 0.f;
+#pragma unroll
+    for (int ct = 0; ct < 4; ++ct)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) top = fmaxf(top, fabsf(o[ct][r]));
+    dst = part_row(max_halves(top), by);
+  }
   auto pack = [&](float u, float v) {
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{u * il, v * il}), bf16x2));
+    return whole ? __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{u, v}), bf16x2)) : halves(u * by, v * by);
   };
 #pragma unroll
   for (int ct = 0; ct < 4; ++ct)
@@ -870,7 +912,8 @@ extern "C" size_t entmtp_tree_attn_paged_fp4_plan_bytes(const entmtp_bank* bank,
 extern "C" size_t entmtp_tree_attn_paged_fp4_workspace(const entmtp_bank* bank, int32_t B, int32_t rows_cap,
                                                        int32_t Hq, int32_t Hkv, int32_t d, int32_t max_pages,
                                                        int32_t page_size) {
-  return entmtp_tree_attn_paged_workspace(bank, B, rows_cap, Hq, Hkv, d, max_pages, page_size);
+  if (!shape_ok(bank, B, rows_cap, Hq, Hkv, max_pages, page_size) || d != HD) return 0;
+  return fp4_workspace(paged_shape(bank, B, rows_cap, Hq, Hkv, static_cast<long long>(max_pages) * page_size));
 }
 
 extern "C" int32_t entmtp_tree_attn_paged_fp4_plan(const entmtp_bank* bank, int32_t B, const int32_t* topo,
@@ -908,8 +951,9 @@ extern "C" int32_t entmtp_tree_attn_paged_fp4(const entmtp_bank* bank, int32_t B
   ENTMTP_CHECK_ARG(sh.items < INT32_MAX / 64, ENTMTP_ERANGE, "%d rows of %d heads: too many", rows_cap, Hq);
   ENTMTP_CHECK_ARG(plan_bytes >= sh.plan_bytes, ENTMTP_ENOSPC, "the plan has %zu bytes, needs %zu", plan_bytes,
                    sh.plan_bytes);
-  ENTMTP_CHECK_ARG(sh.workspace == 0 || (workspace && workspace_bytes >= sh.workspace), ENTMTP_ENOSPC,
-                   "workspace has %zu bytes, needs %zu", workspace ? workspace_bytes : size_t(0), sh.workspace);
+  const size_t need = fp4_workspace(sh);
+  ENTMTP_CHECK_ARG(need == 0 || (workspace && workspace_bytes >= need), ENTMTP_ENOSPC,
+                   "workspace has %zu bytes, needs %zu", workspace ? workspace_bytes : size_t(0), need);
   ENTMTP_CHECK_ARG(merge_blocks(rows_cap, Hq) <= INT32_MAX, ENTMTP_ERANGE, "%d rows of %d heads: too many", rows_cap, Hq);
   PagedFp4Args a{};
   fill_call(a, trees, sh, plan, B, n_pages, page_size, max_pages, rows_cap, Hq, Hkv, window, out, workspace,
@@ -927,5 +971,5 @@ extern "C" int32_t entmtp_tree_attn_paged_fp4(const entmtp_bank* bank, int32_t B
   softcap > 0.f || window > 0 || slopes != nullptr ? go(paged_attn_fp4_kernel<true>) : go(paged_attn_fp4_kernel<false>);
   if (int32_t rc = launch_status("tree_attn_paged_fp4 launch")) return rc;
   if (!sh.splits) return ENTMTP_OK;
-  return launch_merge(a, s);
+  return launch_merge<true>(a, s);
 }

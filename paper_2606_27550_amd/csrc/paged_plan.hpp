@@ -5,6 +5,7 @@
 #pragma once
 
 #include <algorithm>
+#include <type_traits>
 
 #include "attn_tile.hpp"
 #include "paged.hpp"
@@ -70,12 +71,14 @@ __host__ __device__ inline int first_pos(int L, int window) {
 struct PagedCall {
   const uint8_t* plan;
   // [part rows][HD]: the split's output, normalised by its sum so that it stays
-  // within its values' range, in bf16: in fp32 the whole output's error against
-  // 64 bits is 3.4-3.5e-3 instead of 3.7-3.9e-3 (the weights' and the query's
-  // roundings stay), and the bytes cost 3-6 % of long prefixes and windows, 15 % of 26
-  // nodes at 8192 (21.5 -> 24.7 us)
-  uint16_t* part_o;
-  float* part_ml;        // [part rows][2]
+  // within its values' range.  Of bf16 pools in bf16: in fp32 the whole output's
+  // error against 64 bits is 3.4-3.5e-3 instead of 3.7-3.9e-3 (the weights' and the
+  // query's roundings stay), and the bytes cost 3-6 % of long prefixes and windows,
+  // 15 % of 26 nodes at 8192 (21.5 -> 24.7 us).  Of 4-bit pools in fp16, the
+  // row's largest scaled to [2^14, 2^15): 1.9e-3 instead of 2.9e-3 with bf16 (the
+  // output's own rounding being 1.7e-3 of it), at the same bytes.
+  void* part_o;
+  float* part_ml;        // [part rows][2]: max, sum; of 4-bit pools [4]: what undoes the scaling, too
   uint16_t* out;         // [rows_cap][Hq][HD]
   long long rows_at, items_at;
   uint64_t bank;         // the bank's number
@@ -116,7 +119,8 @@ __device__ __forceinline__ bool plan_is_ours(const PagedCall& p, const PlanHeade
 constexpr int kMergeThreads = 256;
 constexpr int kMergeAhead = 16;
 
-template <int LANES>
+// HALF: partials in scaled fp16.
+template <int LANES, bool HALF>
 static __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedCall p) {
   constexpr int kHeads = kMergeThreads / LANES;
   constexpr int kPairs = kPagedSplits / LANES;   // (max, sum) pairs a lane
@@ -140,16 +144,25 @@ static __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(Paged
   const int row = (h % p.G) * sq.T + (r - sq.row0);
   const size_t base = sq.part_off + static_cast<size_t>(h / p.G) * sq.rows_pad + row;
   const size_t stride = static_cast<size_t>(p.Hkv) * sq.rows_pad;   // from split to split
-  const uint16_t* const po = p.part_o + base * HD + 4 * (lane & 31);
-  float m[kPairs], l[kPairs];
+  const uint16_t* const po = static_cast<const uint16_t*>(p.part_o) + base * HD + 4 * (lane & 31);
+  float m[kPairs], l[kPairs], scale[kPairs];
 #pragma unroll
   for (int k = 0; k < kPairs; ++k) {
     m[k] = -INFINITY;
     l[k] = 0.f;
+    scale[k] = 1.f;
     if (lane + LANES * k < nsplit) {
-      const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + (base + (lane + LANES * k) * stride) * 2);
-      m[k] = ml.x;
-      l[k] = ml.y;
+      const size_t at = base + (lane + LANES * k) * stride;
+      if constexpr (HALF) {
+        const float4 ml = *reinterpret_cast<const float4*>(p.part_ml + at * 4);
+        m[k] = ml.x;
+        l[k] = ml.y;
+        scale[k] = ml.z;
+      } else {
+        const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + at * 2);
+        m[k] = ml.x;
+        l[k] = ml.y;
+      }
     }
   }
   // (kBatch at a time without a branch between them: a split past the last is
@@ -175,6 +188,7 @@ static __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(Paged
   for (int k = 0; k < kPairs; ++k) {
     l[k] = m[k] == -INFINITY ? l[k] : l[k] * __builtin_amdgcn_exp2f(m[k] - M);
     lsum += l[k];
+    if constexpr (HALF) l[k] *= scale[k];   // (from here on the partial's weight)
   }
 #pragma unroll
   for (int off = LANES / 2; off >= 1; off >>= 1) lsum += __shfl_xor(lsum, off, LANES);
@@ -189,11 +203,20 @@ static __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(Paged
     for (int k = 0; k < kMergeAhead; ++k) {
       const float wc = __shfl(w, (c + first + k) % LANES, LANES);
       if (k / kBatch == 0 || c + k / kBatch * kBatch < nsplit) {
-        const uint2 v = c + first + k < nsplit ? ob[k] : uint2{0u, 0u};   // (the last one again may hold infinities)
-        acc.x = fmaf(wc, __uint_as_float(v.x << 16), acc.x);
-        acc.y = fmaf(wc, __uint_as_float(v.x & 0xffff0000u), acc.y);
-        acc.z = fmaf(wc, __uint_as_float(v.y << 16), acc.z);
-        acc.w = fmaf(wc, __uint_as_float(v.y & 0xffff0000u), acc.w);
+        const bool in = c + first + k < nsplit;   // (the last one again may hold infinities)
+        float4 v;
+        if constexpr (HALF) {
+          typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+          const f16x2 a = __builtin_bit_cast(f16x2, static_cast<uint32_t>(ob[k].x)), b = __builtin_bit_cast(f16x2, static_cast<uint32_t>(ob[k].y));
+          v = make_float4(static_cast<float>(a[0]), static_cast<float>(a[1]), static_cast<float>(b[0]), static_cast<float>(b[1]));
+        }
+        else
+          v = make_float4(__uint_as_float(ob[k].x << 16), __uint_as_float(ob[k].x & 0xffff0000u),
+                          __uint_as_float(ob[k].y << 16), __uint_as_float(ob[k].y & 0xffff0000u));
+        acc.x = fmaf(wc, in ? v.x : 0.f, acc.x);
+        acc.y = fmaf(wc, in ? v.y : 0.f, acc.y);
+        acc.z = fmaf(wc, in ? v.z : 0.f, acc.z);
+        acc.w = fmaf(wc, in ? v.w : 0.f, acc.w);
       }
     }
   }
@@ -223,7 +246,7 @@ struct PagedShape {
   int items = 0;
   bool two = false, splits = false;
   long long part_rows = 0;
-  size_t plan_bytes = 0, workspace = 0;
+  size_t plan_bytes = 0, workspace = 0;   // (the workspace: of bf16 pools)
 };
 
 inline PagedShape paged_shape(const entmtp_bank* bank, int B, int rows_cap, int Hq, int Hkv, long long cap) {
@@ -274,14 +297,19 @@ int32_t launch_paged_plan(bool fp4, const entmtp_bank* bank, int32_t B, const in
                           int32_t max_pages, int32_t page_size, int32_t n_pages, int32_t rows_cap, int32_t Hq,
                           int32_t Hkv, int32_t window, int32_t* bad, void* plan, size_t plan_bytes, void* stream);
 
-// Fills what PagedCall holds but for the output pointers' splits; the workspace
-// has been checked against sh.
+// Bytes of a call's workspace over 4-bit pools.
+inline size_t fp4_workspace(const PagedShape& sh) {
+  return up256(static_cast<size_t>(sh.part_rows) * HD * sizeof(uint16_t)) +
+         up256(static_cast<size_t>(sh.part_rows) * 4 * sizeof(float));
+}
+
+// Fills what PagedCall holds; the workspace has been checked against sh.
 inline void fill_call(PagedCall& a, const TreeTable& trees, const PagedShape& sh, const void* plan, int32_t B,
                       int32_t n_pages, int32_t page_size, int32_t max_pages, int32_t rows_cap, int32_t Hq,
                       int32_t Hkv, int32_t window, entmtp_bf16* out, void* workspace, int magic) {
   a.plan = static_cast<const uint8_t*>(plan);
   a.bank = trees.bank;
-  a.part_o = static_cast<uint16_t*>(workspace);
+  a.part_o = workspace;
   a.part_ml = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) +
                                        up256(static_cast<size_t>(sh.part_rows) * HD * sizeof(uint16_t)));
   a.out = out;
@@ -311,12 +339,14 @@ inline long long merge_blocks(int32_t rows_cap, int32_t Hq) {
   const int heads = kMergeThreads / (merge_few(rows_cap, Hq) ? 64 : 32);
   return static_cast<long long>(rows_cap) * ((Hq + heads - 1) / heads);
 }
+template <bool HALF>
 inline int32_t launch_merge(const PagedCall& a, hipStream_t s) {
   const dim3 blocks(static_cast<uint32_t>(merge_blocks(a.rows_cap, a.Hq)));
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, blocks, dim3(kMergeThreads), 0, s, a); };
   if (merge_few(a.rows_cap, a.Hq))
-    hipLaunchKernelGGL(paged_merge_kernel<64>, blocks, dim3(kMergeThreads), 0, s, a);
+    go(paged_merge_kernel<64, HALF>);
   else
-    hipLaunchKernelGGL(paged_merge_kernel<32>, blocks, dim3(kMergeThreads), 0, s, a);
+    go(paged_merge_kernel<32, HALF>);
   return launch_status("tree_attn_paged merge launch");
 }
 
