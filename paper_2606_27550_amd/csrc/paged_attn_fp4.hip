@@ -11,11 +11,11 @@
 // query rows (four tiles of 32) and a range of 32-key blocks.
 //  - Keys enter the matrix instruction (32 x 32 x 64, 4-bit by 6-bit: twice the
 //    rate of bf16) as they lie in the pool, codes and scale bytes.  A query, with
-//    the scale in base 2 taken into it, is two 6-bit numbers: hi, rounded to steps
-//    of at most 1/15 of the largest of its 32, and lo, the rest with a scale 2^4
-//    below.  Their sum is off by at most 2^-8 / 3.75 of that largest, less than a
-//    rounding to bf16 as a whole (root mean square 5e-4 of ordinary queries' against
-//    1.1e-3).
+//    the scale in base 2 taken into it, is the sum of three 6-bit numbers, each what
+//    the one before leaves with a scale 2^3 below: off by at most 2^-10 / 3.75 of the
+//    largest of its 32.  (Two, 2^4 apart, leave outputs 2.9e-3 off in the norm where
+//    three leave 2.3e-3, most of it the weights' rounding; large trees and long
+//    prefixes took 4-7 % less.)
 //  - Values become bf16 numbers, exactly, on their way to the LDS, from which the
 //    products read them transposed.
 //  - Many rows (three or four tiles): the workgroup's wavefronts, a tile each,
@@ -88,10 +88,13 @@ __device__ __forceinline__ void buf_dma4(__amdgpu_buffer_rsrc_t buf, uint32_t vo
   __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lds_void*)lds, 4, voff, 0, 0, 0);
 }
 
-// 32 values (v: 8 words of bf16 pairs in each of two halves) times f as two 6-bit
-// operands of the matrix instruction; returns their scale bytes, hi's and lo's in
-// the next byte but one (not a number where a value is not finite).
-__device__ __forceinline__ uint32_t query6(const u32x4 (&v)[4], float f, i32x8& hi, i32x8& lo) {
+// 32 values (v: their bf16 pairs) times f as the sum of three 6-bit operands of the
+// matrix instruction, a scale of 2^3 between them; returns the largest's scale byte
+// (not a number where a value is not finite).
+struct Query6 {
+  i32x8 part[3];
+};
+__device__ __forceinline__ uint32_t query6(const u32x4 (&v)[4], float f, Query6& q) {
   float x[32];
   uint32_t top = 0u;
 #pragma unroll
@@ -101,39 +104,31 @@ __device__ __forceinline__ uint32_t query6(const u32x4 (&v)[4], float f, i32x8& 
     x[2 * e + 1] = bf16_hi(w) * f;
     top = max(top, max(__float_as_uint(x[2 * e]) & 0x7fffffffu, __float_as_uint(x[2 * e + 1]) & 0x7fffffffu));
   }
-  // (the largest in [3.75, 7.5) steps)
-  const int e = static_cast<int>((top + (1u << 20)) >> 23), b = e < 8 ? 6 : (e > 254 ? 252 : e - 2);
-  const float step = __uint_as_float(static_cast<uint32_t>(b) << 23), inv = __uint_as_float(static_cast<uint32_t>(254 - b) << 23);
-  f32x16 he, ho, le, lo_;
+  // (the largest in [3.75, 7.5) steps of the scale)
+  const int e = static_cast<int>((top + (1u << 20)) >> 23), b = e < 12 ? 10 : (e > 254 ? 252 : e - 2);
+  const float inv = __uint_as_float(static_cast<uint32_t>(254 - b) << 23);
 #pragma unroll
-  for (int k = 0; k < 16; ++k) {
+  for (int k = 0; k < 32; ++k) x[k] *= inv;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const float y = x[2 * k + h] * inv;
-      // rounded to an eighth of its power of two, at least of one
-      const float q = fmaxf(__uint_as_float(__float_as_uint(y) & 0x7f800000u), 1.f) * 0.125f;
-      const float c = q * 12582912.f;   // 1.5 x 2^23 of these steps
-      const float r = (y + c) - c;
-      if (h) {
-        ho[k] = r;
-        lo_[k] = (y - r) * 16.f;
-      } else {
-        he[k] = r;
-        le[k] = (y - r) * 16.f;
+  for (int n = 0; n < 3; ++n) {
+    f32x16 even, odd;   // (the instruction takes the even values first, then the odd ones)
+#pragma unroll
+    for (int k = 0; k < 32; ++k) {
+      float r = x[k];   // (the last part: rounded by the instruction)
+      if (n < 2) {
+        // to eighths, then to four bits of mantissa: a number of the format
+        r = (x[k] + 1572864.f) - 1572864.f;   // 1.5 x 2^23 / 8
+        r = __uint_as_float((__float_as_uint(r) + 0x80000u) & 0xfff00000u);
+        x[k] = (x[k] - r) * 8.f;
       }
+      (k & 1 ? odd : even)[k >> 1] = r;
     }
-  }
-  (void)step;
-  // (the instruction takes the even values first, then the odd ones)
-  const auto a = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(he, ho, 1.f);
-  const auto c = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(le, lo_, 1.f);
+    const auto six = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, 1.f);
 #pragma unroll
-  for (int k = 0; k < 6; ++k) {
-    hi[k] = static_cast<int>(a[k]);
-    lo[k] = static_cast<int>(c[k]);
+    for (int k = 0; k < 6; ++k) q.part[n][k] = static_cast<int>(six[k]);
+    q.part[n][6] = q.part[n][7] = 0;
   }
-  hi[6] = hi[7] = lo[6] = lo[7] = 0;
-  return top >= 0x7f800000u ? kFp4NaN | kFp4NaN << 16 : static_cast<uint32_t>(b) | static_cast<uint32_t>(b - 4) << 16;
+  return top >= 0x7f800000u ? kFp4NaN : static_cast<uint32_t>(b);
 }
 
 // MOD: a score cap, distance bias or window.
@@ -148,6 +143,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
   __shared__ __attribute__((aligned(16))) uint8_t s_val[kTilesPerWg][kFp4Stage];   // (many rows: two in turn)
   __shared__ float2 s_ml[kTilesPerWg][KB];
   __shared__ uint32_t s_odd[4];   // a block's keys with values that are no numbers, a bit each
+  __shared__ uint32_t s_mask[kTilesPerWg][KB][ENTMTP_MASK_WORDS + 1];   // the rows' ancestors, a wavefront's own
   __shared__ uint8_t s_depth[ENTMTP_T_MAX];
   Fp4Block* const ring[kFp4Ring] = {&raw0, &raw1, &raw2, &raw3};
   const int x = static_cast<int>(blockIdx.x);
@@ -194,8 +190,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
   }
   const int qdepth = depth[qnode];
   const int tdepth = depth[min(tid, T - 1)];
-  u32x4 mlo = *reinterpret_cast<const u32x4*>(mask + qnode * ENTMTP_MASK_WORDS);
-  u32x4 mhi = *reinterpret_cast<const u32x4*>(mask + qnode * ENTMTP_MASK_WORDS + 4);
+  const u32x4 qmask = *reinterpret_cast<const u32x4*>(mask + qnode * ENTMTP_MASK_WORDS + 4 * lh);
   static_assert(ENTMTP_MASK_WORDS == 8, "a mask row is two 16-byte loads");
   float slope = 0.f;
   if constexpr (MOD)
@@ -210,21 +205,21 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
   const int qpos = L + qdepth;
   const int w_row = MOD && p.window > 0 ? qpos - p.window + 1 : -1;   // the row's first position
   const int w_hi = MOD && p.window > 0 ? L + D - p.window + 1 : -1;   // from here on every row sees the prefix
+  auto keep_mask = [&]() __attribute__((always_inline)) {   // (read by the wavefront that writes it)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s_mask[wave][small ? lc : li][4 * lh + e] = qlive ? qmask[e] : ~0u;
+  };
   // The keys of the block at kb, which reaches into the tree or past it, that the
   // row sees, a bit each.
   auto seen = [&](int kb) __attribute__((always_inline)) {
     const int rel = kb - L;
-    auto word = [&](int w) {   // (w is uniform)
-      uint32_t m = 0u;
-#pragma unroll
-      for (int k = 0; k < 8; ++k) m = w == k ? (k < 4 ? mlo[k & 3] : mhi[k & 3]) : m;
-      return m;
-    };
+    const uint32_t* const row = s_mask[wave][small ? lc : li];
+    auto word = [&](int w) { return w < ENTMTP_MASK_WORDS ? row[w] : 0u; };   // (w is uniform)
     uint32_t vis = ~0u;
     if (rel + KB > 0) {
       if (rel < 0) {
         const int npre = -rel;
-        vis = (0xFFFFFFFFu >> (32 - npre)) | (mlo[0] << npre);
+        vis = (0xFFFFFFFFu >> (32 - npre)) | (word(0) << npre);
       } else {
         const int wi = rel >> 5, sh = rel & 31;
         const uint32_t lo = word(wi), hi = word(wi + 1);
@@ -301,9 +296,10 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
       wait_lds();
       stage_barrier();
     }
-    if (!qlive) mlo = mhi = u32x4{~0u, ~0u, ~0u, ~0u};
-    i32x8 hi, lo;
-    const int qscale = static_cast<int>(query6(qf[0], p.q_scale, hi, lo));   // bytes 0 and 2
+    keep_mask();
+    Query6 qs;
+    const uint32_t qb = query6(qf[0], p.q_scale, qs);
+    const int qscale = static_cast<int>(qb == kFp4NaN ? 0xffffffu : qb | (qb - 3) << 8 | (qb - 6) << 16);
     f32x4 out[8], base = {0.f, 0.f, 0.f, 0.f};   // (base: minus the row's reference)
 #pragma unroll
     for (int ct = 0; ct < 8; ++ct) out[ct] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -321,8 +317,9 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
         const i32x8 ka = {static_cast<int>(s.k[j][0]), static_cast<int>(s.k[j][1]), static_cast<int>(s.k[j][2]), static_cast<int>(s.k[j][3]), 0, 0, 0, 0};
         const int kscale = static_cast<int>(s.ks[j] >> (8 * lq));
         sc[j] = MOD ? f32x4{0.f, 0.f, 0.f, 0.f} : base;
-        sc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ka, lo, sc[j], 4, 2, 0, kscale, 2, qscale);
-        sc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ka, hi, sc[j], 4, 2, 0, kscale, 0, qscale);
+        sc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ka, qs.part[2], sc[j], 4, 2, 0, kscale, 2, qscale);
+        sc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ka, qs.part[1], sc[j], 4, 2, 0, kscale, 1, qscale);
+        sc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ka, qs.part[0], sc[j], 4, 2, 0, kscale, 0, qscale);
       }
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
@@ -501,12 +498,17 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
   for (int ct = 0; ct < 4; ++ct)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[ct][r] = 0.f;
-  i32x8 qh[2], ql[2];
-  uint32_t qsc = 0u;   // scale bytes of hi for m = 0, 1, then of lo
+  Query6 qs[2];
+  uint32_t qsc = 0u, qsl = 0u;   // scale bytes of the first part for m = 0, 1, and the second's; the third's
   auto settle = [&]() __attribute__((always_inline)) {   // (behind the loads of the first blocks)
-    if (!qlive) mlo = mhi = u32x4{~0u, ~0u, ~0u, ~0u};
+    keep_mask();
 #pragma unroll
-    for (int m = 0; m < 2; ++m) qsc |= query6(qf[m], p.q_scale, qh[m], ql[m]) << (8 * m);
+    for (int m = 0; m < 2; ++m) {
+      const uint32_t b = query6(qf[m], p.q_scale, qs[m]);
+      const bool odd = b == kFp4NaN;
+      qsc |= (b | (odd ? b : b - 3) << 16) << (8 * m);
+      qsl |= (odd ? b : b - 6) << (8 * m);
+    }
   };
 
   // the transposing reads of the values: row 4 lh + (lane % 16) / 4 of each 8
@@ -526,10 +528,13 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
     } else {
       sacc = ref;
     }
-    sacc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, ql[0], sacc, 4, 2, 0, kscale, 2, qscale);
-    sacc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kc, ql[1], sacc, 4, 2, 2, kscale, 3, qscale);
-    sacc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qh[0], sacc, 4, 2, 0, kscale, 0, qscale);
-    sacc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kc, qh[1], sacc, 4, 2, 2, kscale, 1, qscale);
+    const int kl = static_cast<int>(qsl);
+    sacc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qs[0].part[2], sacc, 4, 2, 0, kscale, 0, kl);
+    sacc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kc, qs[1].part[2], sacc, 4, 2, 2, kscale, 1, kl);
+    sacc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qs[0].part[1], sacc, 4, 2, 0, kscale, 2, qscale);
+    sacc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kc, qs[1].part[1], sacc, 4, 2, 2, kscale, 3, qscale);
+    sacc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qs[0].part[0], sacc, 4, 2, 0, kscale, 0, qscale);
+    sacc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kc, qs[1].part[0], sacc, 4, 2, 2, kscale, 1, qscale);
   };
   auto key_of = [&](int r) { return 8 * (r >> 2) + 4 * lh + (r & 3); };   // accumulator r's key of the block
   // MOD: the block's products (scaled by the query) as logits in base 2, key r at
