@@ -705,7 +705,6 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
       copy(ring[k], i + kFp4Ring, next);
       next = page_at(pos_of(i + kFp4Ring + 1));
       if (tid == 0) s_odd[(k + 3) & 3] = 0u;
-      turn(ring[(k + 1) % kFp4Ring], s_val[(k + 1) & 1], k + 1);
       if (live) {
         f32x16& cur = k & 1 ? sb : sa;
         f32x16& ahead = k & 1 ? sa : sb;
@@ -713,6 +712,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
         const uint32_t odd = __builtin_amdgcn_readfirstlane(s_odd[k]);
         attend((blk_lo + i) * KB, s_val[k & 1], odd, cur, ahead, prefix);
       }
+      turn(ring[(k + 1) % kFp4Ring], s_val[(k + 1) & 1], k + 1);
     };
     int i0 = 0;
     if (n0 == 0)

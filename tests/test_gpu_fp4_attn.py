@@ -2,9 +2,13 @@
 
 The pages' numbers are exact in bf16, so the oracle's attention over bf16 pages
 applies, with its bounds: per element roundings to bf16 (weights, a split's
-partial, the output: 2^-8 of the value each, and the query's, which does not
-occur here) pushed through the softmax; over a whole output those of three
-roundings, 2^-7 in the 2-norm as for bf16 pages.
+partial, the output: 2^-8 of the value each, and the query's) pushed through the
+softmax; over a whole output 2^-7 in the 2-norm as for bf16 pages.  A partial is
+fp16 here, which is less.  A query enters as three 6-bit numbers: the first leaves
+1/16 of a step in which the largest of its 32 numbers is 3.75 to 7.5 (below 2; up to
+1/4 above), the others 2^-3 of that each, so that it is off by at most 2^-10 steps,
+2^-10 / 3.75 of the largest.  The oracle allows it 2^-8 of every number; the check
+asserts that this moves no row's scores by more.
 """
 import math
 
@@ -77,6 +81,14 @@ def check(c, out, idle=(), nan=(), softcap=0.0, window=0, slopes=None):
         ref, _, off = po.tree_attention_paged(c["q"][r], *rows, kp, vp, c["table"][b], int(L), TREES[t], SCALE, 0.0, softcap,
                                               window, slopes)
         left[r] = False
+        keys = orc.bf16_to_f64(np.concatenate([kp[c["table"][b][j]] for j in range(-(-(L + T) // c["page"]))], 1))[:, :L + T]
+        q = np.abs(orc.bf16_to_f64(c["q"][r]))
+        q[~np.isfinite(q)] = 0
+        top = np.repeat(q.reshape(T, c["Hq"], 4, 32).max(3), 32, 2)
+        for g in range(c["Hkv"]):
+            of = slice(g * c["Hq"] // c["Hkv"], (g + 1) * c["Hq"] // c["Hkv"])
+            k = np.nan_to_num(np.abs(keys[g])).T
+            assert ((top[:, of] @ k).max(-1) * 2.0 ** -10 / 3.75 <= (q[:, of] @ k).max(-1) * 2.0 ** -8).all()
         fine = np.array([i not in nan for i in range(r0, r0 + T)])
         assert np.isnan(got[r][~fine]).all()
         err = np.abs(got[r] - ref)[fine]
