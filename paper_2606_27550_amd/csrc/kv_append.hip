@@ -197,7 +197,7 @@ __global__ __launch_bounds__(kAppendThreads) void kv_append_kernel(AppendArgs p)
   }
 }
 
-// A workgroup a sequence, and one for the rows behind the last.
+// A workgroup a sequence, and one for the rows before the first and behind the last.
 struct PositionArgs {
   TreeTable trees;
   const int* topo;
@@ -209,17 +209,25 @@ struct PositionArgs {
 
 __global__ __launch_bounds__(ENTMTP_T_MAX) void tree_positions_kernel(PositionArgs p) {
   const int b = blockIdx.x, tid = threadIdx.x;
-  if (b == p.B) {   // (row_off below zero or past the rows: as far as there are rows)
-    for (int r = max(p.row_off[p.B], 0) + tid; r < p.rows; r += ENTMTP_T_MAX) p.pos[r] = -1;
+  // (offsets of any size: as far as there are rows, counted in 64 bits)
+  auto clear = [&](long long first, long long end) {
+    for (long long r = first + tid; r < end; r += ENTMTP_T_MAX) p.pos[r] = -1;
+  };
+  auto within = [&](int r) { return min(max(r, 0), p.rows); };
+  if (b == p.B) {
+    clear(0, within(p.row_off[0]));
+    clear(within(p.row_off[p.B]), p.rows);
     return;
   }
-  const int tr = p.topo[b], L = p.len[b], r0 = p.row_off[b], r1 = min(p.row_off[b + 1], p.rows);
+  const int tr = p.topo[b], L = p.len[b], r0 = p.row_off[b], r1 = within(p.row_off[b + 1]);
   if (r0 < 0) return;
-  const bool named = tr >= 0 && tr < p.trees.n && L >= 0;
+  const bool named = tr >= 0 && tr < p.trees.n;
   const PagedTree& tree = p.trees.t[named ? tr : 0];
   const int* const depth = reinterpret_cast<const int*>(p.trees.arena + tree.off_depth);
-  const bool fits = named && tree.T <= r1 - r0 && L <= INT32_MAX - ENTMTP_T_MAX;
-  for (int i = tid; i < r1 - r0; i += ENTMTP_T_MAX) p.pos[r0 + i] = fits && i < tree.T ? L + depth[i] : -1;
+  // (r1 - r0 above -2^31: both are at least zero)
+  const int T = named && tree.T <= r1 - r0 && L >= 0 && L <= INT32_MAX - ENTMTP_T_MAX ? tree.T : 0;
+  for (int i = tid; i < T; i += ENTMTP_T_MAX) p.pos[r0 + i] = L + depth[i];
+  clear(static_cast<long long>(r0) + T, r1);
 }
 
 template <bool FP4>

@@ -144,8 +144,8 @@ __global__ __launch_bounds__(kCompactThreads) void kv_compact_paged_kernel(Compa
   a = min(a, min(p.path_cap, ROWS) - 1);
   if (a < 0) return;   // not verified (uniform)
   int src = -1, dst = -1;
-  const int n = min(r1, p.rows) - r0;
-  if (j <= a && r0 >= 0 && node >= 0 && node < n && j < n && node != j) {
+  const int n = r0 < 0 ? 0 : min(max(r1, 0), p.rows) - r0;   // (offsets of any size)
+  if (j <= a && node >= 0 && node < n && j < n && node != j) {
     src = p.slot_map[r0 + node];
     dst = p.slot_map[r0 + j];
     if (src >= p.n_slots || dst < 0 || dst >= p.n_slots) src = -1;
@@ -197,8 +197,8 @@ __global__ __launch_bounds__(kCompactThreads) void kv_compact_fp4_kernel(Compact
   a = min(a, min(p.path_cap, ROWS) - 1);
   if (a < 0) return;   // not verified (uniform)
   int src = -1, dst = -1;
-  const int n = min(r1, p.rows) - r0;
-  if (j <= a && r0 >= 0 && node >= 0 && node < n && j < n && node != j) {
+  const int n = r0 < 0 ? 0 : min(max(r1, 0), p.rows) - r0;   // (offsets of any size)
+  if (j <= a && node >= 0 && node < n && j < n && node != j) {
     src = p.slot_map[r0 + node];
     dst = p.slot_map[r0 + j];
     if (src >= p.n_slots || dst < 0 || dst >= p.n_slots) src = -1;

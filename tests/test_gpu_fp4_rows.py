@@ -244,6 +244,30 @@ def test_positions_of_sequences_without_work(api):
     np.testing.assert_array_equal(host(pos), want)   # (the last tree does not fit its rows)
 
 
+def test_positions_with_rows_before_and_wild_offsets(api):
+    """Rows before the first sequence's have no position; offsets outside the rows, down to the lowest number, write nothing."""
+    bank = api.Bank(TREES)
+    pos = torch.full((40,), 77, dtype=torch.int32, device="cuda")
+    api.tree_positions(bank, i32([0, 0]), i32([9, 4]), i32([5, 6, 7]), pos)
+    want = np.full(40, -1)
+    want[5], want[6] = 9, 4
+    np.testing.assert_array_equal(host(pos), want)
+    low, high = -2 ** 31, 2 ** 31 - 1
+    for off in ([7, low], [low, high], [high, low], [high, high], [-3, 5]):
+        room = torch.full((400,), 77, dtype=torch.int32, device="cuda")
+        api.tree_positions(bank, i32([2]), i32([9]), i32(off), room[:40])
+        assert (host(room)[40:] == 77).all() and (host(room)[:40] <= 0).sum() + (host(room)[:40] == 77).sum() == 40
+
+
+@pytest.mark.parametrize("off", [[7, -2 ** 31], [-2 ** 31, 2 ** 31 - 1], [2 ** 31 - 1, -2 ** 31], [-1, 9]])
+def test_compact_with_wild_offsets(api, off):
+    pools = [np.random.default_rng(3).integers(0, 256, (4, 2, 16 * 68), dtype=np.uint8) for _ in "kv"]
+    d = [dev(p) for p in pools]
+    api.kv_compact_paged_fp4(i32([[0, 2, 3]]), i32([2]), i32(off), i32(np.arange(20)), *d)
+    for p, t in zip(pools, d):
+        np.testing.assert_array_equal(host(t), p)
+
+
 @pytest.mark.parametrize("layers,page,cap", [(1, 16, 32), (3, 64, 5), (2, 256, 17)])
 def test_compact(api, layers, page, cap):
     say("kv_compact_paged_fp4", layers, page, cap)
