@@ -286,8 +286,9 @@ int32_t entmtp_verify_logits(const entmtp_bf16* hidden, const entmtp_bf16* w_lm,
 /*
  * entmtp_verify_logits with the weights in 4 bits (their form is described at
  * entmtp_quantize_fp4, which makes them): codes [V][hid / 2] and scales
- * [V][hid / 32] bytes.  The weights enter the products as the numbers they stand for
- * (exact in bf16, up to its largest), sums are fp32.  A weight row with a scale
+ * [V][hid / 32] bytes, those of entmtp_quantize_fp4 (others up to 254 too, as long
+ * as the values are bf16 numbers; below its smallest normal one they may count as
+ * zero).  The weights enter the products as the numbers they stand for, sums are fp32.  A weight row with a scale
  * byte 255 has NaN logits.
  * Requirements: 1 <= T <= 4096, 32 <= hid <= 65536, hid % 32 == 0, V >= 1, hidden,
  * codes and logits 16-byte aligned.
@@ -790,7 +791,9 @@ int32_t entmtp_tree_attn_paged_fp4_plan(const entmtp_bank* bank, int32_t B, cons
  * slopes, window, out and workspace (of entmtp_tree_attn_paged_fp4_workspace()
  * bytes) as for entmtp_tree_attn_paged.  A plan of other sizes, another window,
  * another bank or a bf16 pool leaves every output alone.  Groups with scale byte
- * 255 make a row that sees their key NaN, all its dims, and no other row.
+ * 255 (of values also 253 and 254, which no append makes) make a row that sees
+ * their key NaN, all its dims, and no other row; what lies in slots that no row
+ * sees does not matter.
  * Requirements: d == ENTMTP_HEAD_DIM; q, pools, out and workspace 16-byte
  * aligned; otherwise as the plan.
  * Errors (host-checked): EINVAL, ERANGE, ENOSPC, EHIP.

@@ -13,6 +13,7 @@ constexpr int kFp4Group = 32;
 constexpr int kFp4RowBytes = ENTMTP_HEAD_DIM / 2 + ENTMTP_HEAD_DIM / kFp4Group;   // of a head's row: 68
 static_assert(kFp4RowBytes == ENTMTP_FP4_ROW, "the header's row");
 constexpr uint32_t kFp4NaN = 255;
+constexpr uint32_t kFp4Top = 252;   // from here on 6 steps pass bf16's largest number
 
 typedef __bf16 bf16v2 __attribute__((ext_vector_type(2)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
@@ -24,7 +25,7 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 // value is not finite.
 __device__ __forceinline__ uint32_t fp4_scale(uint32_t top) {
   const int e = static_cast<int>((top + 0x20u) >> 7) - 2;   // (the carry is that of a mantissa of 1.75 or more)
-  return top >= 0x7f80u ? kFp4NaN : static_cast<uint32_t>(e < 2 ? 2 : (e > 252 ? 252 : e));
+  return top >= 0x7f80u ? kFp4NaN : static_cast<uint32_t>(e < 2 ? 2 : (e > static_cast<int>(kFp4Top) ? kFp4Top : e));
 }
 __device__ __forceinline__ float fp4_step(uint32_t b) { return __uint_as_float(b << 23); }   // b in [1, 254]
 

@@ -324,15 +324,15 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const uint32_t b = s.vs[j] >> (8 * (lane & 3)) & 0xffu;
-        const unsigned long long bad = __ballot(b == kFp4NaN);
+        const unsigned long long bad = __ballot(b > kFp4Top);
         if (bad != 0ull) {   // (uniform) rows' groups as nibbles, a bit a row
-          if (b == kFp4NaN) s.v[j] = u32x4{0u, 0u, 0u, 0u};
+          if (b > kFp4Top) s.v[j] = u32x4{0u, 0u, 0u, 0u};
           unsigned long long m = bad | bad >> 1;
           m |= m >> 2;
 #pragma unroll
           for (int r = 0; r < 16; ++r) odd |= static_cast<uint32_t>(m >> (4 * r) & 1ull) << (16 * j + r);
         }
-        const float st = fp4_step(b == kFp4NaN ? 127u : b);
+        const float st = fp4_step(b > kFp4Top ? 127u : b);
 #pragma unroll
         for (int c = 0; c < 4; ++c)
           *reinterpret_cast<u32x4*>(put + 16 * j * 256 + (((4 * (lane & 3) + c) ^ wsw) << 4)) = fp4_values(s.v[j][c], st);
@@ -660,18 +660,19 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
     };
     constexpr int kCopies = 2;
     // thread (row tid / 8, eighth tid % 8 of it) turns 16 values into numbers;
-    // groups that are no numbers into zeros (a zero weight would make them NaNs in
-    // every row), and their keys are noted
+    // groups that are no numbers, or hold infinities as bf16 numbers, into zeros (a
+    // zero weight would make them NaNs in every row), and their keys are noted
     const int trow = tid >> 3, tsw = stage_swz(trow);
     auto turn = [&](const Fp4Block* from, uint8_t* stage, int i) __attribute__((always_inline)) {
       const uint2 c = *reinterpret_cast<const uint2*>(from->v + 8 * tid);
       const uint32_t sb = from->s[2 + (trow >> 4)][trow & 15] >> (8 * ((tid & 7) >> 1)) & 0xffu;
-      const unsigned long long bad = __ballot(sb == kFp4NaN);
+      const bool none = sb > kFp4Top;
+      const unsigned long long bad = __ballot(none);
       if (bad != 0ull) {
-        if (sb == kFp4NaN) atomicOr(&s_odd[i & 3], 1u << trow);
+        if (none) atomicOr(&s_odd[i & 3], 1u << trow);
       }
-      const float step = sb == kFp4NaN ? 0.f : fp4_step(sb);
-      const u32x4 lo = fp4_values(sb == kFp4NaN ? 0u : c.x, step), hi = fp4_values(sb == kFp4NaN ? 0u : c.y, step);
+      const float step = none ? 0.f : fp4_step(sb);
+      const u32x4 lo = fp4_values(none ? 0u : c.x, step), hi = fp4_values(none ? 0u : c.y, step);
       uint8_t* const row = stage + trow * 256;
       *reinterpret_cast<u32x4*>(row + (((2 * (tid & 7)) ^ tsw) << 4)) = lo;
       *reinterpret_cast<u32x4*>(row + (((2 * (tid & 7) + 1) ^ tsw) << 4)) = hi;
@@ -800,13 +801,13 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
       // would make them NaNs in every row) and their keys noted
       const uint32_t v2 = lh ? vs >> 16 : vs;   // groups 2 lh and 2 lh + 1
       const uint32_t va = v2 & 0xffu, vb = v2 >> 8 & 0xffu;
-      const unsigned long long bad = __ballot(va == kFp4NaN || vb == kFp4NaN);
+      const unsigned long long bad = __ballot(va > kFp4Top || vb > kFp4Top);
       const uint32_t odd = static_cast<uint32_t>(bad) | static_cast<uint32_t>(bad >> 32);
       if (odd != 0u) {   // (uniform)
-        if (va == kFp4NaN) s.v0 = u32x4{0u, 0u, 0u, 0u};
-        if (vb == kFp4NaN) s.v1 = u32x4{0u, 0u, 0u, 0u};
+        if (va > kFp4Top) s.v0 = u32x4{0u, 0u, 0u, 0u};
+        if (vb > kFp4Top) s.v1 = u32x4{0u, 0u, 0u, 0u};
       }
-      const float sa = fp4_step(va == kFp4NaN ? 127u : va), sb = fp4_step(vb == kFp4NaN ? 127u : vb);
+      const float sa = fp4_step(va > kFp4Top ? 127u : va), sb = fp4_step(vb > kFp4Top ? 127u : vb);
 #pragma unroll
       for (int c = 0; c < 8; ++c) {
         const uint32_t w = c < 4 ? s.v0[c & 3] : s.v1[c & 3];

@@ -252,6 +252,47 @@ def test_groups_that_are_no_numbers(api, pool):
         np.testing.assert_array_equal(got[~sees], ref[~sees])
 
 
+@pytest.mark.parametrize("t,Hq,Hkv,page,L,window", [(0, 8, 2, 16, 37, 0), (2, 4, 2, 64, 300, 0), (2, 8, 2, 16, 700, 100),
+                                                    (4, 8, 2, 16, 301, 0), (4, 16, 2, 64, 1000, 200), (0, 4, 4, 256, 0, 0)])
+def test_bytes_that_no_row_sees(api, t, Hq, Hkv, page, L, window):
+    """Slots behind the tree, before the window and of other pages hold any bytes, those of infinities and NaN included;
+    the outputs are the same bits."""
+    say("fp4 bytes unseen", t, Hq, Hkv, page, L, window)
+    T, g = len(TREES[t]), np.random.default_rng(t + L)
+    c = make(41, [t], [L], Hq, Hkv, page)
+    seen = np.zeros((c["n_pages"], page), bool)
+    for pos in range(max(0, L - window + 1) if window else 0, L + T):
+        seen[c["table"][0, pos // page], pos % page] = True
+    assert not seen.all()
+    junk = dict(c)
+    for pool in ("kp", "vp"):
+        codes, scales = fo.planes(c[pool])
+        codes, scales = codes.copy(), scales.copy()
+        where = ~np.broadcast_to(seen[:, None], codes.shape[:3])
+        codes[where] = g.integers(0, 256, codes[where].shape)
+        scales[where] = g.choice([0, 1, 127, 252, 253, 254, 255], scales[where].shape)
+        junk[pool] = fo.join(codes, scales)
+    want, got = (unbits(launch(api, x, window=window)["out"]) for x in (c, junk))
+    assert np.isfinite(orc.bf16_to_f64(want)).all()
+    np.testing.assert_array_equal(got, want)
+
+
+@pytest.mark.parametrize("t,Hq", [(0, 8), (2, 4), (4, 8)])
+@pytest.mark.parametrize("byte", [253, 254])
+def test_values_beyond_bf16(api, t, Hq, byte):
+    """A group of values with a scale byte above 252 counts as no number, whatever its codes."""
+    T = len(TREES[t])
+    c = make(43, [t], [90], Hq, 2, 16)
+    clean = unbits(launch(api, c)["out"])
+    c["vp"] = c["vp"].copy()
+    slot = c["table"][0, 33 // 16]
+    c["vp"][slot, 1, (33 % 16) * 64:(33 % 16) * 64 + 64] = 0x11
+    c["vp"][slot, 1, 16 * 64 + 4 * (33 % 16) + 2] = byte
+    got = unbits(launch(api, c)["out"])
+    assert np.isnan(orc.bf16_to_f64(got[:T, Hq // 2:])).all()
+    np.testing.assert_array_equal(got[:, :Hq // 2], clean[:, :Hq // 2])
+
+
 def test_large_and_small_scores(api):
     """Queries of very different sizes within a row, zeros, and one that is not finite."""
     c = make(33, [1, 1], [64, 500], 2, 1, 16)
