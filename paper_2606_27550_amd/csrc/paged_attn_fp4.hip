@@ -27,6 +27,18 @@
 //    (two tiles: two), every fourth block each, which meet in the LDS at the end --
 //    a few rows' blocks are a chain of products, softmax and products that one
 //    wavefront could not walk at memory's rate.
+//  - At most 16 rows: the same on 16 columns of queries, half of the products.
+// The splits' partial outputs are fp16 with a scale a row; another kernel joins them.
+//
+// What bounds it (replayed graphs, 32:8 heads): one token at 63 takes 5.6 us, launch
+// and one chain of loads and products.  32 tokens at 8192 take 60 us, 5 of them the
+// merge: 4.8 TB/s of a plain read's 6.4.  26 nodes at 131000 take 83-87 us, the
+// merge 7: the products (0.66 PFLOP/s as bf16 counts them; the keys' run at twice that
+// rate, three times over), in four tiles of which a head group fills 3.25.  Eight
+// 128-node trees at 8192 take 147 us (0.94 PFLOP/s; 193 with a score cap): for a
+// block a wavefront keeps the matrix pipe for 450 cycles and issues 557 cycles of
+// vector instructions, and two of them share a SIMD.  Over pages of bf16 rows the
+// four take 7.6, 189-196, 110-113 and 160-171 us.
 #include <algorithm>
 #include <type_traits>
 
