@@ -195,8 +195,10 @@ __global__ __launch_bounds__(kLmThreads, 2) void lm_fp4_kernel(LmFp4Args p) {
 
 // ---------------------------------------------------------- whole lines --
 
-// The same where every wavefront has KS whole steps: its part of a tile, 16 rows
-// of 64 KS bytes, is copied to the LDS by whole lines, two tiles ahead.  Against
+// The same for rows of whole steps: a wavefront's part of a tile, 16 rows of 64 KS
+// bytes, is copied to the LDS by whole lines, two tiles ahead.  ALL: every wavefront
+// has KS steps of this pass; otherwise the last ones have fewer or none, and copy
+// the row's first step instead.  Against
 // a lane's own 16 bytes to registers: one row of 32000 logits 16.6 -> 13.7 us, 27
 // rows 21.9 -> 19.0, 128 rows (5120 values) 63 -> 56; 27 rows of 128256 are level
 // (58-60, the plain read's rate is 46), 8 rows 49 -> 50.5.  Three tiles ahead are no
@@ -221,7 +223,7 @@ struct LmPart {
   uint32_t scales[(KS + 3) / 4 * 64];
 };
 
-template <int KS, int NT>
+template <int KS, int NT, bool ALL>
 __global__ __launch_bounds__(kLmThreads, 2) void lm_fp4_stream_kernel(LmFp4Args p) {
   constexpr int kScaleCopies = (KS + 3) / 4, kCopies = KS + kScaleCopies;
   // the LDS: two tiles of W, partial sums of two, logits of kHold
@@ -241,7 +243,8 @@ __global__ __launch_bounds__(kLmThreads, 2) void lm_fp4_stream_kernel(LmFp4Args 
   auto row_of = [&](int i) { return (slice + min(i, n_tiles - 1) * p.slices) * kLmTile; };
   const int row0 = chunk * 16 * NT;
   const int crow = p.hid / 2, srow = p.hid / 32;
-  const int k0 = (p.k0 + wave * KS) * kLmStep;   // of this wavefront's values
+  const int left = p.hid / kLmStep - (p.k0 + wave * KS), n_live = ALL ? KS : max(0, min(left, KS));   // steps
+  const int k0 = n_live > 0 ? (p.k0 + wave * KS) * kLmStep : 0;   // of this wavefront's values
 
   // this lane's part of X: row li of each tile, 32 values of every step
   u32x4 xb[NT][KS][4];
@@ -251,7 +254,7 @@ __global__ __launch_bounds__(kLmThreads, 2) void lm_fp4_stream_kernel(LmFp4Args 
 #pragma unroll
     for (int s = 0; s < KS; ++s)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) xb[n][s][j] = *reinterpret_cast<const u32x4*>(xr + s * kLmStep + 8 * j);
+      for (int j = 0; j < 4; ++j) xb[n][s][j] = *reinterpret_cast<const u32x4*>(xr + (s < n_live ? s : 0) * kLmStep + 8 * j);
   }
 
   // copies of a tile: place q of the part is chunk q % (4 KS) of row q / (4 KS)
@@ -262,12 +265,13 @@ __global__ __launch_bounds__(kLmThreads, 2) void lm_fp4_stream_kernel(LmFp4Args 
     const int q = 64 * j + lane;
     crw[j] = q / (4 * KS);
     coff[j] = 16 * (q % (4 * KS) ^ lm_swz<KS>(crw[j]));
+    if (!ALL && coff[j] >= 64u * n_live) coff[j] = 0;
   }
 #pragma unroll
   for (int j = 0; j < kScaleCopies; ++j) {
     const int q = 64 * j + lane;
     srw[j] = min(q / KS, 15);
-    soff[j] = 4 * (q % KS);
+    soff[j] = 4 * (ALL || q % KS < n_live ? q % KS : 0);
   }
   auto copy = [&](LmPart<KS>& to, int i) {
     // (rows past the last are the last again, as are tiles)
@@ -295,6 +299,7 @@ __global__ __launch_bounds__(kLmThreads, 2) void lm_fp4_stream_kernel(LmFp4Args 
     for (int n = 0; n < NT; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
+      if (!ALL && s >= n_live) break;   // (uniform)
       const float step = fp4_step(sc[s] >> (8 * blk) & 0xffu);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -408,13 +413,14 @@ extern "C" int32_t entmtp_verify_logits_fp4(const entmtp_bf16* hidden, const uin
   for (int pass = 0; pass < passes; ++pass) {
     a.k0 = pass * ks * kLmWaves;
     a.add = pass > 0;
-    // (rows of W of whole words whose wavefronts' parts are alike, and the LDS's
-    // places of 16 bytes of them)
-    const bool whole = hid == passes * ks * kLmWaves * kLmStep && (reinterpret_cast<uintptr_t>(scales) & 3u) == 0;
-    auto go = [&](auto stream_kernel, auto rest) {
-      hipLaunchKernelGGL(whole ? stream_kernel : rest, grid, dim3(kLmThreads), 0, s, a);
+    // (a step's scale bytes are a dword)
+    const bool lines = hid % kLmStep == 0 && (reinterpret_cast<uintptr_t>(scales) & 3u) == 0;
+    const bool all = a.k0 + ks * kLmWaves <= steps;
+    auto go = [&](auto stream_all, auto stream, auto rest) {
+      hipLaunchKernelGGL(lines ? (all ? stream_all : stream) : rest, grid, dim3(kLmThreads), 0, s, a);
     };
-#define LM_FP4(KS, NT) go(lm_fp4_stream_kernel<KS, NT>, lm_fp4_kernel<KS, NT, 2>)
+#define LM_FP4(KS, NT) \
+  go(lm_fp4_stream_kernel<KS, NT, true>, lm_fp4_stream_kernel<KS, NT, false>, lm_fp4_kernel<KS, NT, 2>)
     if (nt == 1) {
       switch (ks) {
         case 1: LM_FP4(1, 1); break;

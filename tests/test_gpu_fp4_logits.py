@@ -48,7 +48,8 @@ def check(x, codes, scales, got, rows=None):
     (31, 96, 64), (32, 8192, 130), (33, 1024, 777), (48, 4096, 300), (64, 2048, 1025), (65, 320, 515), (100, 4096, 400),
     (128, 5120, 513), (129, 1024, 64), (200, 544, 130), (256, 2048, 1000), (300, 128, 48), (1, 12288, 50), (3, 65536, 20),
     (40, 20000, 33), (130, 16384, 40),
-    (33, 128, 129), (64, 256, 127), (65, 384, 1), (128, 512, 300), (129, 4096, 131), (700, 128, 257), (50, 5120, 2100)])
+    (33, 128, 129), (64, 256, 127), (65, 384, 1), (128, 512, 300), (129, 4096, 131), (700, 128, 257), (50, 5120, 2100),
+    (5, 8320, 40), (40, 5248, 100), (1, 3584, 300), (27, 2688, 401), (100, 1536, 77), (20, 4992, 33)])
 def test_against_64_bits(api, T, hid, V):
     say("verify_logits_fp4", T, hid, V)
     codes, scales = weights(T + V, V, hid)
