@@ -13,7 +13,7 @@
 // Up to 32 rows the weights' bytes bound it: one row of 32000 logits of 4096 values
 // takes 14 us (5 TB/s), 8 of 128256 50.5 (5.6), 27 of 128256 60 (4.9), where the bf16
 // LM head reads 3.8 times the bytes.  Beyond, the weights come once more for every
-// 32 rows, from the L2 but at about the same 6 TB/s a chip can take: 128 rows of 32000
+// 32 rows (64 of up to 2048 values), from the L2 but at about the same 6 TB/s a chip can take: 128 rows of 32000
 // (5120 values) 57 us where the products at bf16's rate would take 31, 64 of 128256 85,
 // 256 of 32000 77.  A tile kernel for many rows (64 x 128 and 128 x 128 logits a
 // workgroup, W and X through the LDS) came to 50-55 us for the first and 100-113
@@ -315,12 +315,13 @@ __global__ __launch_bounds__(kLmThreads, 2) void lm_fp4_stream_kernel(LmFp4Args 
   // (a number a thread: by fours it would be two wavefronts' work, for which the
   // others wait at the next barrier)
   auto reduce = [&](int i, int par) {
-    if (tid < NT * 256) {
-      const float* const from = reinterpret_cast<const float*>(s_part[par]) + tid;
+#pragma unroll
+    for (int at = tid; at < NT * 256; at += kLmThreads) {
+      const float* const from = reinterpret_cast<const float*>(s_part[par]) + at;
       float z = from[0];
 #pragma unroll
       for (int v = 1; v < kLmWaves; ++v) z += from[v * NT * 256];
-      reinterpret_cast<float*>(s_out[i % kHold])[tid] = z;
+      reinterpret_cast<float*>(s_out[i % kHold])[at] = z;
     }
   };
   const bool wide = (p.V & 3) == 0;
@@ -403,8 +404,11 @@ extern "C" int32_t entmtp_verify_logits_fp4(const entmtp_bf16* hidden, const uin
   a.tiles = (V + kLmTile - 1) / kLmTile;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const int steps = (hid + kLmStep - 1) / kLmStep;
-  // a pass over hid holds at most 8 steps a wavefront (5 where it has two tiles of X)
-  const int nt = T > 16 ? 2 : 1, most = nt == 2 ? 5 : 8;
+  // a pass over hid holds at most 8 steps a wavefront (5 where it has two tiles of X,
+  // 2 where it has four, which halves the copies of W: of 128256 logits 128 rows of
+  // 1024 values 78 -> 61 us, 100 of 1536 94 -> 78; of 32000 33 of 2048 18.1 -> 16.7)
+  const bool lines = hid % kLmStep == 0 && (reinterpret_cast<uintptr_t>(scales) & 3u) == 0;   // (a step's scale bytes are a dword)
+  const int nt = T > 32 && lines && steps <= 2 * kLmWaves ? 4 : (T > 16 ? 2 : 1), most = nt == 4 ? 2 : (nt == 2 ? 5 : 8);
   const int passes = (steps + most * kLmWaves - 1) / (most * kLmWaves);
   const int ks = ((steps + passes - 1) / passes + kLmWaves - 1) / kLmWaves;
   a.chunks = (T + 16 * nt - 1) / (16 * nt);
@@ -413,15 +417,20 @@ extern "C" int32_t entmtp_verify_logits_fp4(const entmtp_bf16* hidden, const uin
   for (int pass = 0; pass < passes; ++pass) {
     a.k0 = pass * ks * kLmWaves;
     a.add = pass > 0;
-    // (a step's scale bytes are a dword)
-    const bool lines = hid % kLmStep == 0 && (reinterpret_cast<uintptr_t>(scales) & 3u) == 0;
     const bool all = a.k0 + ks * kLmWaves <= steps;
     auto go = [&](auto stream_all, auto stream, auto rest) {
       hipLaunchKernelGGL(lines ? (all ? stream_all : stream) : rest, grid, dim3(kLmThreads), 0, s, a);
     };
 #define LM_FP4(KS, NT) \
   go(lm_fp4_stream_kernel<KS, NT, true>, lm_fp4_stream_kernel<KS, NT, false>, lm_fp4_kernel<KS, NT, 2>)
-    if (nt == 1) {
+#define LM_FP4_LINES(KS) \
+  go(lm_fp4_stream_kernel<KS, 4, true>, lm_fp4_stream_kernel<KS, 4, false>, lm_fp4_stream_kernel<KS, 4, false>)
+    if (nt == 4) {
+      if (ks == 1)
+        LM_FP4_LINES(1);
+      else
+        LM_FP4_LINES(2);
+    } else if (nt == 1) {
       switch (ks) {
         case 1: LM_FP4(1, 1); break;
         case 2: LM_FP4(2, 1); break;
@@ -442,6 +451,7 @@ extern "C" int32_t entmtp_verify_logits_fp4(const entmtp_bf16* hidden, const uin
       }
     }
 #undef LM_FP4
+#undef LM_FP4_LINES
     if (int32_t rc = launch_status("verify_logits_fp4 launch")) return rc;
   }
   return ENTMTP_OK;
