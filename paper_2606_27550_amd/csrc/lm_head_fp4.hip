@@ -1,7 +1,7 @@
 // LM-head logits from 4-bit weights: z = X W^T, W in codes and group scales.
 //
 // The weights stream past the hidden states, which stay in registers.  A
-// workgroup of eight wavefronts takes up to 32 rows of X; wavefront w keeps
+// workgroup of eight wavefronts takes up to 32 rows of X (64 short ones); wavefront w keeps
 // an eighth of their length, in 128-wide steps, and takes the same steps of each
 // 16-row tile of W: a lane's 16 bytes are 32 codes of one group, which become bf16
 // numbers, exactly, on the way into the matrix instruction (16 x 16 x 32), so
