@@ -716,7 +716,8 @@ int32_t entmtp_quantize_fp4(const entmtp_bf16* x, int64_t rows, int32_t n, uint8
  * depth(i) for node i of tree topo[b] (device int32[B] each), -1 in every other
  * row of [0, rows): those of no sequence, of one whose topo[b] lies outside the
  * bank (run in topo's place: of one that is not served), with prefix_len[b] < 0
- * or within ENTMTP_T_MAX of 2^31, and behind a tree's nodes.
+ * or within ENTMTP_T_MAX of 2^31, with row_off[b] < 0 or too few rows for its
+ * tree, and behind a tree's nodes (offsets of any size, in any order).
  * Requirements: rows >= 1; sequences' rows do not overlap.
  * Errors (host-checked): EINVAL, ERANGE, EHIP.
  */

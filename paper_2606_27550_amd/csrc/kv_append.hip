@@ -203,7 +203,7 @@ __global__ __launch_bounds__(kAppendThreads) void kv_append_kernel(AppendArgs p)
   }
 }
 
-// A workgroup a sequence, and one for the rows before the first and behind the last.
+// A workgroup a sequence, and one for the rows that lie in no sequence's range.
 struct PositionArgs {
   TreeTable trees;
   const int* topo;
@@ -214,6 +214,7 @@ struct PositionArgs {
 };
 
 __global__ __launch_bounds__(ENTMTP_T_MAX) void tree_positions_kernel(PositionArgs p) {
+  __shared__ int s_off[kPagedSeqs + 1];
   const int b = blockIdx.x, tid = threadIdx.x;
   // (offsets of any size: as far as there are rows, counted in 64 bits)
   auto clear = [&](long long first, long long end) {
@@ -221,19 +222,32 @@ __global__ __launch_bounds__(ENTMTP_T_MAX) void tree_positions_kernel(PositionAr
   };
   auto within = [&](int r) { return min(max(r, 0), p.rows); };
   if (b == p.B) {
-    clear(0, within(p.row_off[0]));
-    clear(within(p.row_off[p.B]), p.rows);
+    // offsets that never fall leave the rows before the first and behind the last;
+    // others (none that entmtp_page_map makes) are looked up row by row
+    static_assert(ENTMTP_T_MAX >= kPagedSeqs, "a thread per sequence");
+    const int off = p.row_off[min(tid, p.B - 1)], end = p.row_off[min(tid, p.B - 1) + 1];
+    if (tid < p.B) s_off[tid] = off;
+    if (tid == p.B - 1) s_off[p.B] = end;
+    if (__syncthreads_and(off <= end)) {
+      clear(0, within(s_off[0]));
+      clear(within(s_off[p.B]), p.rows);
+      return;
+    }
+    for (long long r = tid; r < p.rows; r += ENTMTP_T_MAX) {
+      bool held = false;
+      for (int k = 0; k < p.B; ++k) held = held || (s_off[k] <= r && r < s_off[k + 1]);
+      if (!held) p.pos[r] = -1;
+    }
     return;
   }
   const int tr = p.topo[b], L = p.len[b], r0 = p.row_off[b], r1 = within(p.row_off[b + 1]);
-  if (r0 < 0) return;
   const bool named = tr >= 0 && tr < p.trees.n;
   const PagedTree& tree = p.trees.t[named ? tr : 0];
   const int* const depth = reinterpret_cast<const int*>(p.trees.arena + tree.off_depth);
   // (r1 - r0 above -2^31: both are at least zero)
-  const int T = named && tree.T <= r1 - r0 && L >= 0 && L <= INT32_MAX - ENTMTP_T_MAX ? tree.T : 0;
+  const int T = named && r0 >= 0 && tree.T <= r1 - r0 && L >= 0 && L <= INT32_MAX - ENTMTP_T_MAX ? tree.T : 0;
   for (int i = tid; i < T; i += ENTMTP_T_MAX) p.pos[r0 + i] = L + depth[i];
-  clear(static_cast<long long>(r0) + T, r1);
+  clear(static_cast<long long>(max(r0, 0)) + T, r1);
 }
 
 template <bool FP4>
