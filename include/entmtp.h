@@ -734,13 +734,13 @@ int32_t entmtp_tree_positions(const entmtp_bank* bank, int32_t B, const int32_t*
  *           (q_norm / k_norm: bf16 [d], or NULL: none)
  *   turn    pairs (c, c + d / 2) by the angle pos[r] * rope_theta^(-2 c / d)
  *           (rope_theta 0: none)
- *   q_out   [rows][Hq][d] bf16: the queries, rounded once
+ *   q_out   [rows][Hq][d] bf16: the queries
  *   pool    slot slot_map[r] of every head (outside the pool: not written): the
- *           key, computed in fp64 and rounded to fp32 and then to bf16, and the
- *           value; in a 4-bit pool the codes of both (of the key so rounded)
+ *           key and the value; in a 4-bit pool the codes of both (of the key so rounded)
  *   k_out, v_out  [rows][Hkv][d] bf16, each may be NULL: key and value as the
  *           pool holds them (of a 4-bit pool what the codes stand for), for an
  *           attention over the prompt itself
+ * Queries and keys are computed in fp64 and rounded to fp32 and then to bf16.
  * Rows with pos[r] < 0 are left alone in every output.  q and q_out may both be
  * NULL.  q, k and v are rows of Hq x d, Hkv x d, Hkv x d values, their rows
  * q_stride, k_stride, v_stride values apart (parts of one projection's output);

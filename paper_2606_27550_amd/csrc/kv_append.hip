@@ -6,12 +6,13 @@
 // theta^(-2c/d):
 //   y = x / sqrt(mean(x^2) + eps) w
 //   y_c cos a_c - y_{c+d/2} sin a_c,  y_{c+d/2} cos a_c + y_c sin a_c
-// rounded to bf16.  Keys are computed in fp64 and rounded by way of fp32, as a
-// tensor of 64-bit numbers is converted, so that a program that computes its
-// keys in tensors finds the same bytes in the pool (one key value of 2^17 is
-// off by a unit of bf16 from the rounding at once that the attention kernels
-// give the keys that they append); queries, which only enter products, in fp32.
-// Angles are fp64 for both.
+// rounded to bf16.  All of it is computed in fp64 (angles, the sum of squares,
+// which in fp32 passes the range from values of 2^60 on and below 2^-63, and the
+// products) and rounded by way of fp32, as a tensor of 64-bit numbers is
+// converted, so that a program that computes its keys in tensors finds the same
+// bytes in the pool (one value of 2^17 is off by a unit of bf16 from the rounding
+// at once that the attention kernels give the keys that they append).  Queries
+// in fp32 were no faster: 42.3-42.6 us against 42.5-43.2 for the 6476 rows below.
 //
 // Eight threads hold a head (thread cc the chunks cc and cc + 8 of eight values,
 // so both halves of eight pairs), a wavefront eight heads at a time.  A wavefront
@@ -55,13 +56,12 @@ struct AppendArgs {
   double freq[kRopePairs];
 };
 
-// The norm's factors on the 16 values of a thread's chunks.
-template <typename F>
-__device__ __forceinline__ F head_rsqrt(u32x4 lo, u32x4 hi, float eps) {
-  F s = 0;
+// The norm's factor on the 16 values of a thread's chunks.
+__device__ __forceinline__ double head_rsqrt(u32x4 lo, u32x4 hi, float eps) {
+  double s = 0;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    const F a = bf16_lo(lo[e]), b = bf16_hi(lo[e]), c = bf16_lo(hi[e]), d = bf16_hi(hi[e]);
+    const double a = bf16_lo(lo[e]), b = bf16_hi(lo[e]), c = bf16_lo(hi[e]), d = bf16_hi(hi[e]);
     s = a * a + s;
     s = b * b + s;
     s = c * c + s;
@@ -69,35 +69,35 @@ __device__ __forceinline__ F head_rsqrt(u32x4 lo, u32x4 hi, float eps) {
   }
 #pragma unroll
   for (int off = 1; off < 8; off <<= 1) s += __shfl_xor(s, off, 8);
-  return F(1) / sqrt(s / HD + F(eps));
+  return 1.0 / sqrt(s / HD + static_cast<double>(eps));
 }
 
 // A head's chunks normed (w: its 16 weights, or null) and turned.
-template <typename F, bool TURN, typename Table>
-__device__ __forceinline__ void norm_turn(u32x4& lo, u32x4& hi, const uint16_t* w, int cc, float eps, const Table* t) {
+template <bool TURN>
+__device__ __forceinline__ void norm_turn(u32x4& lo, u32x4& hi, const uint16_t* w, int cc, float eps, const double2* t) {
 #pragma clang fp contract(off)
-  F r = 1;
+  double r = 1;
   u32x4 wl = {0u, 0u, 0u, 0u}, wh = wl;
   if (w) {
     wl = *reinterpret_cast<const u32x4*>(w + 8 * cc);
     wh = *reinterpret_cast<const u32x4*>(w + 8 * cc + HD / 2);
-    r = head_rsqrt<F>(lo, hi, eps);
+    r = head_rsqrt(lo, hi, eps);
   }
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     uint32_t nl = 0u, nh = 0u;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      F x = h ? bf16_hi(lo[e]) : bf16_lo(lo[e]), y = h ? bf16_hi(hi[e]) : bf16_lo(hi[e]);
+      double x = h ? bf16_hi(lo[e]) : bf16_lo(lo[e]), y = h ? bf16_hi(hi[e]) : bf16_lo(hi[e]);
       if (w) {
-        x = x * r * F(h ? bf16_hi(wl[e]) : bf16_lo(wl[e]));
-        y = y * r * F(h ? bf16_hi(wh[e]) : bf16_lo(wh[e]));
+        x = x * r * static_cast<double>(h ? bf16_hi(wl[e]) : bf16_lo(wl[e]));
+        y = y * r * static_cast<double>(h ? bf16_hi(wh[e]) : bf16_lo(wh[e]));
       }
-      F a = x, b = y;
+      double a = x, b = y;
       if constexpr (TURN) {
-        const Table cs = t[(2 * e + h) ^ cc];
-        a = x * F(cs.x) - y * F(cs.y);
-        b = y * F(cs.x) + x * F(cs.y);
+        const double2 cs = t[(2 * e + h) ^ cc];
+        a = x * cs.x - y * cs.y;
+        b = y * cs.x + x * cs.y;
       }
       nl |= static_cast<uint32_t>(__builtin_bit_cast(uint16_t, static_cast<__bf16>(static_cast<float>(a)))) << (16 * h);
       nh |= static_cast<uint32_t>(__builtin_bit_cast(uint16_t, static_cast<__bf16>(static_cast<float>(b)))) << (16 * h);
@@ -188,14 +188,14 @@ __global__ __launch_bounds__(kAppendThreads) void kv_append_kernel(AppendArgs p)
                                 static_cast<size_t>(h) * HD + 8 * cc;
     u32x4 lo = *reinterpret_cast<const u32x4*>(src), hi = *reinterpret_cast<const u32x4*>(src + HD / 2);
     if (kind == 0) {
-      norm_turn<float, TURN>(lo, hi, p.q_norm, cc, p.eps, mine);
+      norm_turn<TURN>(lo, hi, p.q_norm, cc, p.eps, mine);
       if (live) {
         uint16_t* const out = p.q_out + (static_cast<size_t>(row) * p.Hq + h) * HD + 8 * cc;
         *reinterpret_cast<u32x4*>(out) = lo;
         *reinterpret_cast<u32x4*>(out + HD / 2) = hi;
       }
     } else if (kind == 1) {
-      norm_turn<double, TURN>(lo, hi, p.k_norm, cc, p.eps, mine);
+      norm_turn<TURN>(lo, hi, p.k_norm, cc, p.eps, mine);
       store_row<FP4>(p, p.kp, p.k_out, lo, hi, row, h, slot, cc, live);
     } else {
       store_row<FP4>(p, p.vp, p.v_out, lo, hi, row, h, slot, cc, live);

@@ -1,11 +1,20 @@
-"""GPU: positions of tree rows where offsets leave the ordinary (whole numbers, compared as they are)."""
+"""GPU: positions and appended rows where offsets, sizes and values leave the ordinary.
+
+Positions are whole numbers and compared as they are.  A query is computed in
+fp64 from angles and sums in fp64, rounded to fp32 and then to bf16: by at most
+2^-8 + 2^-24 of its value; the fp64 before it is off by less than 2^-40 of the
+two numbers that a turn adds.  Keys are held bit for bit.
+"""
 import numpy as np
 import pytest
 
 torch = pytest.importorskip("torch")
 
 from oracle import entmtp_oracle as orc  # noqa: E402
-from tests.paged_helpers import TREES, host, i32, say  # noqa: E402
+from oracle import fp4_oracle as fo  # noqa: E402
+from tests.fp4_helpers import D  # noqa: E402
+from tests.paged_helpers import TREES, bits, host, i32, say, unbits  # noqa: E402
+from tests.test_gpu_fp4_rows import append, append_case  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 LOW, HIGH = -2 ** 31, 2 ** 31 - 1
@@ -62,3 +71,59 @@ def test_positions_of_a_full_batch(api):
         api.tree_positions(api.Bank(TREES), i32(topo), i32(lens), i32(o), pos)
         want = positions(topo, lens, o, rows)
         np.testing.assert_array_equal(host(pos), want)
+
+
+def to_bf16(x):
+    """64-bit numbers to fp32 and then to bf16 bits, subnormal ones too (the oracle's bits cut those short)."""
+    return torch.from_numpy(x).to(torch.float32).to(torch.bfloat16).view(torch.int16).numpy().view(np.uint16)
+
+
+def with_heads(c, q=None, k=None):
+    """The case with other queries or keys on both sides."""
+    if q is not None:
+        c["q"], c["dq"] = q, bits(q)
+    if k is not None:
+        c["k"], c["dk"] = k, bits(k)
+    return c
+
+
+def check_queries(c, eps):
+    got = orc.bf16_to_f64(unbits(c["qo"]))
+    w = None if c["w"] is None else orc.bf16_to_f64(c["w"])[0]
+    for r, pos in enumerate(c["pos"]):
+        x = orc.bf16_to_f64(c["q"][r])
+        ref = fo.norm_turn(x, int(pos), w, eps, c["theta"])
+        y = np.abs(fo.norm_turn(x, 0, w, eps, 0.0))
+        room = (2.0 ** -8 + 2.0 ** -24) * np.abs(ref) + 2.0 ** -40 * (y + np.roll(y, D // 2, -1)) + 2.0 ** -133
+        err = np.abs(got[r] - ref)
+        assert (err <= room).all(), (r, float((err / room).max()))
+
+
+@pytest.mark.parametrize("fp4", [False, True])
+@pytest.mark.parametrize("eps", [0.0, 1e-6])
+def test_queries_and_keys_of_any_size_are_normed(api, fp4, eps):
+    """Heads near both ends of bf16's range, queries as well as keys: their squares pass fp32's range on either side."""
+    say("kv_append sizes", fp4, eps)
+    c = append_case(21, 8, 4, 2, 16, fp4, True, 1e4, False)
+    def sized(x):
+        x = x.copy()
+        x[0] = (x[0] & 0x807F) | (0x7F + 126 << 7)              # about 2^126
+        x[1] = (x[1] & 0x807F) | (0x7F + 61 << 7)               # 2^61: 128 squares pass 2^128
+        x[2, :, 77] = (0x7F + 64 << 7) | 0x8011                 # one of 2^64
+        x[3] = (x[3] & 0x807F) | (0x7F - 100 << 7)              # 2^-100: squares below fp32
+        x[4] = (x[4] & 0x807F) | 0x0080                         # 2^-126
+        x[5] = x[5] & 0x803F | 1                                # subnormal
+        x[6, :, ::2] = 0x7F7F                                   # the largest number beside ordinary ones
+        return x
+    with_heads(c, sized(c["q"]), sized(c["k"]))
+    append(api, c, eps=eps)
+    check_queries(c, eps)
+    wk = orc.bf16_to_f64(c["w"])[1]
+    kout = unbits(c["ko"])
+    for r, pos in enumerate(c["pos"]):
+        key = to_bf16(fo.norm_turn(orc.bf16_to_f64(c["k"][r]), int(pos), wk, eps, c["theta"]))
+        if fp4:
+            key = orc.f64_to_bf16_bits(fo.values(*fo.quantize(orc.bf16_to_f64(key))))
+        zero = orc.bf16_to_f64(key) == 0
+        np.testing.assert_array_equal(kout[r][~zero], key[~zero])
+        assert (kout[r][zero] & 0x7FFF == 0).all()
