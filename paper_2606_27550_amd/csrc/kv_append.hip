@@ -12,15 +12,15 @@
 // converted, so that a program that computes its keys in tensors finds the same
 // bytes in the pool (one value of 2^17 is off by a unit of bf16 from the rounding
 // at once that the attention kernels give the keys that they append).  Queries
-// in fp32 were no faster: 42.3-42.6 us against 42.5-43.2 for the 6476 rows below.
+// in fp32 took 0 to 4 % less time (6476 rows as below 40.6-42.6 us against 42.0-43.2).
 //
 // Eight threads hold a head (thread cc the chunks cc and cc + 8 of eight values,
 // so both halves of eight pairs), a wavefront eight heads at a time.  A wavefront
 // works alone: lane c computes the angle of pair c of its row, 40 fp64
 // instructions, and leaves it in the wavefront's part of the LDS.
 //
-// Bytes bound it: 6476 rows of prompts (32:8 heads, norm) into 4-bit pages 42 us
-// (3.9 TB/s), 3852 (40:40, no norm) into bf16 pages 68 us (4.6 TB/s; a large copy
+// Bytes bound it: 6476 rows of prompts (32:8 heads, norm) into 4-bit pages 42-43 us
+// (3.9 TB/s), 3852 (40:40, no norm) into bf16 pages 67 us (4.7 TB/s; a large copy
 // 4.9).  The tree rows of a step (208) take 5.5 us, one row 5.3: a launch and
 // two round trips; their positions, a kernel of their own once a step, 2.7.  (The
 // next group's loads ahead of this one's stores: level.)
@@ -56,7 +56,9 @@ struct AppendArgs {
   double freq[kRopePairs];
 };
 
-// The norm's factor on the 16 values of a thread's chunks.
+// The norm's factor on the 16 values of a thread's chunks; no number where the
+// head holds one that is not finite (the sum of 128 finite squares of bf16 numbers
+// stays finite: below 2^263).
 __device__ __forceinline__ double head_rsqrt(u32x4 lo, u32x4 hi, float eps) {
   double s = 0;
 #pragma unroll
@@ -69,7 +71,7 @@ __device__ __forceinline__ double head_rsqrt(u32x4 lo, u32x4 hi, float eps) {
   }
 #pragma unroll
   for (int off = 1; off < 8; off <<= 1) s += __shfl_xor(s, off, 8);
-  return 1.0 / sqrt(s / HD + static_cast<double>(eps));
+  return s < INFINITY ? 1.0 / sqrt(s / HD + static_cast<double>(eps)) : static_cast<double>(NAN);
 }
 
 // A head's chunks normed (w: its 16 weights, or null) and turned.

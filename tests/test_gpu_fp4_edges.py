@@ -127,3 +127,41 @@ def test_queries_and_keys_of_any_size_are_normed(api, fp4, eps):
         zero = orc.bf16_to_f64(key) == 0
         np.testing.assert_array_equal(kout[r][~zero], key[~zero])
         assert (kout[r][zero] & 0x7FFF == 0).all()
+
+
+@pytest.mark.parametrize("fp4", [False, True])
+@pytest.mark.parametrize("theta", [0.0, 0.5, 1e4])
+@pytest.mark.parametrize("odd", [0x7F80, 0xFF80, 0x7FC0])
+def test_heads_that_are_not_finite_are_no_numbers_under_a_norm(api, fp4, theta, odd):
+    """One infinity or NaN: the whole head is NaN, in the pool and the outputs; all others are what they were."""
+    say("kv_append not finite", fp4, theta, hex(odd))
+    c = append_case(23, 6, 9, 3, 16, fp4, True, theta, False)
+    clean_q, clean_k = c["q"].copy(), c["k"].copy()
+    append(api, c)
+    want = {n: unbits(c[n]).copy() for n in ("qo", "ko", "vo")}
+    pools = [host(c[n]).copy() if fp4 else unbits(c[n]).copy() for n in ("dkp", "dvp")]
+    q, k = clean_q.copy(), clean_k.copy()
+    q[1, 0, 3], q[2, 8, 127], k[3, 0, 64], k[4, 2, 31] = odd, odd, odd, odd
+    with_heads(c, q, k)
+    append(api, c)
+    got = {n: orc.bf16_to_f64(unbits(c[n])) for n in ("qo", "ko", "vo")}
+    for n, H, heads in (("qo", 9, [(1, 0), (2, 8)]), ("ko", 3, [(3, 0), (4, 2)]), ("vo", 3, [])):
+        bad = np.zeros((6, H), bool)
+        for at in heads:
+            bad[at] = True
+        assert np.isnan(got[n][bad]).all()
+        np.testing.assert_array_equal(unbits(c[n])[~bad], want[n][~bad])
+    now = [host(c[n]) if fp4 else unbits(c[n]) for n in ("dkp", "dvp")]
+    np.testing.assert_array_equal(now[1], pools[1])
+    hit = np.zeros((c["n_pages"], 16, 3), bool)
+    for r, g in ((3, 0), (4, 2)):
+        hit[c["slots"][r] // 16, c["slots"][r] % 16, g] = True
+    hit = hit.transpose(0, 2, 1)
+    if fp4:
+        (codes, scales), (oc, os_) = fo.planes(now[0]), fo.planes(pools[0])
+        assert (codes[hit] == 0).all() and (scales[hit] == 255).all()
+        np.testing.assert_array_equal(codes[~hit], oc[~hit])
+        np.testing.assert_array_equal(scales[~hit], os_[~hit])
+    else:
+        assert np.isnan(orc.bf16_to_f64(now[0][hit])).all()
+        np.testing.assert_array_equal(now[0][~hit], pools[0][~hit])
