@@ -787,8 +787,13 @@ int32_t entmtp_tree_attn_paged_fp4_plan(const entmtp_bank* bank, int32_t B, cons
  * One attention layer over 4-bit pools for the batch of a plan: node i of
  * sequence b attends to the prefix and to its root-to-node path, whose rows
  * entmtp_kv_append_paged_fp4 has put at positions prefix_len[b] + node of the
- * block table.  q [rows_cap][Hq][d] bf16 holds the queries as they enter the
- * products (turned already; entmtp_kv_append_paged_fp4's q_out); scale, softcap,
+ * block table.  q [rows_cap][Hq][d] bf16 holds the queries, turned already
+ * (entmtp_kv_append_paged_fp4's q_out).  Of each of their groups of 32 the
+ * values down to 2^-13 of the group's largest enter the products as they are,
+ * smaller ones off by at most 2^-21 of it; the scores are scaled in fp32.  The
+ * softmax's weights are rounded to bf16 (2^-8 of each), the partial outputs of a
+ * prefix that is split to fp16 with a scale a row; maxima and sums are fp32,
+ * whose range values beyond about 2^100 may pass on the way.  scale, softcap,
  * slopes, window, out and workspace (of entmtp_tree_attn_paged_fp4_workspace()
  * bytes) as for entmtp_tree_attn_paged.  A plan of other sizes, another window,
  * another bank or a bf16 pool leaves every output alone.  Groups with scale byte

@@ -9,13 +9,16 @@
 // so that a key block of the tree differs from one of the prefix by its mask
 // alone.  The work list is that of paged_attn.hip: a workgroup takes a KV head's
 // query rows (four tiles of 32) and a range of 32-key blocks.
-//  - Keys enter the matrix instruction (32 x 32 x 64, 4-bit by 6-bit: twice the
-//    rate of bf16) as they lie in the pool, codes and scale bytes.  A query, with
-//    the scale in base 2 taken into it, is the sum of three 6-bit numbers, each what
-//    the one before leaves with a scale 2^3 below: off by at most 2^-10 / 3.75 of the
-//    largest of its 32.  (Two, 2^4 apart, leave outputs 2.9e-3 off in the norm where
-//    three leave 2.3e-3, most of it the weights' rounding; large trees and long
-//    prefixes took 4-7 % less.)
+//  - Keys enter the matrix instruction (32 x 32 x 64, 4-bit by 8-bit: bf16's rate)
+//    as they lie in the pool, codes and scale bytes.  A query is the sum of two 8-bit
+//    numbers, the second what the first leaves at a scale 2^4 below, under a scale of
+//    its group of 32: together they hold bf16's eight bits of every value down to
+//    2^-13 of the group's largest, exactly, and of smaller ones all but 2^-21 of that
+//    largest, so that a channel which stands out costs the others nothing.  Scores
+//    are scaled in fp32.  (Three 6-bit numbers, which share their steps with the
+//    group's largest, run at twice the rate, three times over, and took 2-4 % less in
+//    large trees; beside a channel 64 times the others' size they were off by more
+//    than a rounding to bf16, beside one 1000 times by a third of their values.)
 //  - Values become bf16 numbers, exactly, on their way to the LDS, from which the
 //    products read them transposed.
 //  - Many rows (three or four tiles): the workgroup's wavefronts, a tile each,
@@ -23,22 +26,25 @@
 //    wavefront turns a quarter of a block's values into numbers, a block ahead,
 //    and takes the next block's scores before this one's softmax.
 //  - Few rows: a wavefront streams its blocks by itself, from memory to registers,
-//    three ahead, and no barrier joins it to the others: the range is shared by four
+//    two ahead, and no barrier joins it to the others: the range is shared by four
 //    (two tiles: two), every fourth block each, which meet in the LDS at the end --
 //    a few rows' blocks are a chain of products, softmax and products that one
 //    wavefront could not walk at memory's rate.
 //  - At most 16 rows: the same on 16 columns of queries, half of the products.
 // The splits' partial outputs are fp16 with a scale a row; another kernel joins them.
 //
-// What bounds it (replayed graphs, 32:8 heads): one token at 63 takes 5.6 us, launch
+// What bounds it (replayed graphs, 32:8 heads): one token at 63 takes 5.3 us, launch
 // and one chain of loads and products.  32 tokens at 8192 take 60 us, 5 of them the
-// merge: 4.8 TB/s of a plain read's 6.4.  26 nodes at 131000 take 83-87 us, the
-// merge 7: the products (0.66 PFLOP/s as bf16 counts them; the keys' run at twice that
-// rate, three times over), in four tiles of which a head group fills 3.25.  Eight
-// 128-node trees at 8192 take 147 us (0.94 PFLOP/s; 193 with a score cap): for a
-// block a wavefront keeps the matrix pipe for 450 cycles and issues 557 cycles of
-// vector instructions, and two of them share a SIMD.  Over pages of bf16 rows the
-// four take 7.6, 189-196, 110-113 and 160-171 us.
+// merge: 4.8 TB/s of a plain read's 6.4.  26 nodes at 131000 take 88 us, the merge
+// 7: the products (0.63 PFLOP/s; the keys' twice, once for each part of the query),
+// in four tiles of which a head group fills 3.25.  Eight 128-node trees at 8192 take
+// 154 us (0.90 PFLOP/s; 201 with a score cap): for a block a wavefront keeps the
+// matrix pipe for 513 cycles and issues 611 cycles of vector instructions, of which
+// 206 run beside each other; it waits 516 of its 2173 cycles, and two wavefronts
+// share a SIMD.  Over pages of bf16 rows the four take 7.6, 189-196, 110-113 and
+// 160-171 us.  The instance with cap, bias and window does not fit its 256 registers
+// (nine are spilled; of the loops over blocks the one beside a window's edge and the
+// tree reloads one).
 #include <algorithm>
 #include <type_traits>
 
@@ -66,7 +72,7 @@ struct PagedFp4Args : PagedCall {
   const uint16_t* q;     // [rows_cap][Hq][HD]
   const uint8_t* kp;     // [n_pages][Hkv][P x 68]
   const uint8_t* vp;
-  float q_scale;     // of the products: scale log2(e), or with a cap 2 log2(e) scale / cap
+  float q_scale;     // of the products, in fp32: scale log2(e), or with a cap 2 log2(e) scale / cap
   float cap_log2;    // cap log2(e), 0: no cap
 };
 
@@ -100,47 +106,53 @@ __device__ __forceinline__ void buf_dma4(__amdgpu_buffer_rsrc_t buf, uint32_t vo
   __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lds_void*)lds, 4, voff, 0, 0, 0);
 }
 
-// 32 values (v: their bf16 pairs) times f as the sum of three 6-bit operands of the
-// matrix instruction, a scale of 2^3 between them; returns the largest's scale byte
-// (not a number where a value is not finite).
-struct Query6 {
-  i32x8 part[3];
+// The larger of a lane's number and that of the lane 32 (16) away.
+__device__ __forceinline__ uint32_t top_halves(uint32_t x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return max(r[0], r[1]);
+}
+__device__ __forceinline__ uint32_t top_sixteenths(uint32_t x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  return max(r[0], r[1]);
+}
+
+// A lane's 32 values of a query as the sum of two 8-bit operands of the matrix
+// instruction (a sign, 4 bits of exponent, 3 of mantissa), the second at a scale 2^4
+// below the first's.
+struct Query8 {
+  i32x8 part[2];
 };
-__device__ __forceinline__ uint32_t query6(const u32x4 (&v)[4], float f, Query6& q) {
-  float x[32];
-  uint32_t top = 0u;
+
+// Scale byte of a group of 32 whose largest magnitude has the bf16 bits top: the
+// largest comes to lie in [224, 448) steps; not a number where a value is not finite.
+__device__ __forceinline__ uint32_t query_scale(uint32_t top) {
+  const int e = static_cast<int>((top + 0x20u) >> 7);   // (the carry is that of a mantissa of 1.75 or more)
+  return top >= 0x7f80u ? kFp4NaN : static_cast<uint32_t>(max(e, 12) - 8);
+}
+__device__ __forceinline__ uint32_t second_scale(uint32_t b) { return b == kFp4NaN ? b : b - 4u; }
+
+// Bytes 16 h .. + 15 of both parts from 16 values (v: their bf16 pairs) of a group
+// with scale byte b.
+__device__ __forceinline__ void query8(const u32x4 (&v)[2], uint32_t b, int h, Query8& q) {
+  const float inv = __uint_as_float((254u - (b == kFp4NaN ? 127u : b)) << 23);
 #pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    const uint32_t w = v[e >> 2][e & 3];
-    x[2 * e] = bf16_lo(w) * f;
-    x[2 * e + 1] = bf16_hi(w) * f;
-    top = max(top, max(__float_as_uint(x[2 * e]) & 0x7fffffffu, __float_as_uint(x[2 * e + 1]) & 0x7fffffffu));
-  }
-  // (the largest in [3.75, 7.5) steps of the scale)
-  const int e = static_cast<int>((top + (1u << 20)) >> 23), b = e < 12 ? 10 : (e > 254 ? 252 : e - 2);
-  const float inv = __uint_as_float(static_cast<uint32_t>(254 - b) << 23);
+  for (int w = 0; w < 4; ++w) {   // (four values to a word)
+    float hi[4], lo[4];
 #pragma unroll
-  for (int k = 0; k < 32; ++k) x[k] *= inv;
-#pragma unroll
-  for (int n = 0; n < 3; ++n) {
-    f32x16 even, odd;   // (the instruction takes the even values first, then the odd ones)
-#pragma unroll
-    for (int k = 0; k < 32; ++k) {
-      float r = x[k];   // (the last part: rounded by the instruction)
-      if (n < 2) {
-        // to eighths, then to four bits of mantissa: a number of the format
-        r = (x[k] + 1572864.f) - 1572864.f;   // 1.5 x 2^23 / 8
-        r = __uint_as_float((__float_as_uint(r) + 0x80000u) & 0xfff00000u);
-        x[k] = (x[k] - r) * 8.f;
-      }
-      (k & 1 ? odd : even)[k >> 1] = r;
+    for (int k = 0; k < 4; ++k) {
+      const uint32_t u = v[w >> 1][2 * (w & 1) + (k >> 1)];
+      const float x = (k & 1 ? bf16_hi(u) : bf16_lo(u)) * inv;
+      // to the smallest steps of the format, then to four bits of mantissa: a number of it
+      const float r = (x + 24576.f) - 24576.f;   // 1.5 x 2^23 x 2^-9
+      hi[k] = __uint_as_float((__float_as_uint(r) + 0x80000u) & 0xfff00000u);
+      lo[k] = (x - hi[k]) * 16.f;
     }
-    const auto six = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, 1.f);
-#pragma unroll
-    for (int k = 0; k < 6; ++k) q.part[n][k] = static_cast<int>(six[k]);
-    q.part[n][6] = q.part[n][7] = 0;
+    auto pack = [](const float (&f)[4]) {
+      return __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false), true);
+    };
+    q.part[0][4 * h + w] = pack(hi);
+    q.part[1][4 * h + w] = pack(lo);
   }
-  return top >= 0x7f800000u ? kFp4NaN : static_cast<uint32_t>(b);
 }
 
 // MOD: a score cap, distance bias or window.
@@ -184,21 +196,24 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
 
   // The query row (row r of KV head g: head g G + r / T, node r % T), its depth
   // and mask, all unconditional: rows past the tree read row 0, see every key
-  // and are never stored.  Matrix instruction m of a block takes dims 64 m + 32 lh
-  // .. + 31 (small: the only one dims 32 lq .. + 31).
+  // and are never stored.  Matrix instruction m of a block takes keys' dims 64 m +
+  // 32 lh .. + 31 and queries' 64 m + 16 lh .. + 15 and 64 m + 32 + 16 lh .. + 15
+  // (small: the only one 32 lq .. + 31, and 16 lq .. + 15 and 64 + 16 lq .. + 15),
+  // and a scale byte of dims 64 m + 32 lh .. + 31 (32 lq .. + 31) of either.
   const bool small = GT <= 16;   // (16 columns of queries: lane % 16, groups of 32 dims: lane / 16)
   const int lc = lane & 15, lq = lane >> 4;
   const int qrow = qt * kQTile + (small ? lc : li);
   const bool qlive = live && qrow < GT;
   const int qnode = qlive ? qrow % T : 0;
   const int qhead = g * p.G + (qlive ? qrow / T : 0);
-  u32x4 qf[2][4];
+  u32x4 qf[2][2][2];   // [m][16 values][chunk]
   {
-    const uint16_t* qp = p.q + (static_cast<size_t>(row0 + qnode) * p.Hq + qhead) * HD + 32 * (small ? lq : lh);
+    const uint16_t* qp = p.q + (static_cast<size_t>(row0 + qnode) * p.Hq + qhead) * HD + 16 * (small ? lq : lh);
 #pragma unroll
     for (int m = 0; m < 2; ++m)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) qf[m][e] = *reinterpret_cast<const u32x4*>(qp + (small ? 0 : 64 * m) + 8 * e);
+      for (int e = 0; e < 4; ++e)
+        qf[m][e >> 1][e & 1] = *reinterpret_cast<const u32x4*>(qp + (small ? 0 : 64 * m) + (small ? 64 : 32) * (e >> 1) + 8 * (e & 1));
   }
   const int qdepth = depth[qnode];
   const int tdepth = depth[min(tid, T - 1)];
@@ -210,10 +225,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
 
   // l_run: the sum of this lane's half of the keys (the halves meet at the end)
   float m_run = -INFINITY, l_run = 0.f;
-  // without MOD a block's products start from minus the row's reference (zero
-  // before its first), so that they come out as the exponents themselves; lift:
-  // how far a block's largest may pass the reference
-  float lift = -INFINITY;
+  const float to_log2 = MOD ? 1.f : p.q_scale;   // from a block's scores to logits in base 2 (MOD: bend's work)
   const int qpos = L + qdepth;
   const int w_row = MOD && p.window > 0 ? qpos - p.window + 1 : -1;   // the row's first position
   const int w_hi = MOD && p.window > 0 ? L + D - p.window + 1 : -1;   // from here on every row sees the prefix
@@ -309,10 +321,18 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
       stage_barrier();
     }
     keep_mask();
-    Query6 qs;
-    const uint32_t qb = query6(qf[0], p.q_scale, qs);
-    const int qscale = static_cast<int>(qb == kFp4NaN ? 0xffffffu : qb | (qb - 3) << 8 | (qb - 6) << 16);
-    f32x4 out[8], base = {0.f, 0.f, 0.f, 0.f};   // (base: minus the row's reference)
+    Query8 qs;
+    uint32_t qscale;   // scale bytes of the first part and the second
+    {
+      const uint32_t b0 = query_scale(top_sixteenths(max(bf16_top(qf[0][0][0]), bf16_top(qf[0][0][1]))));   // dims 32 (lq / 2) .. + 31
+      const uint32_t b1 = query_scale(top_sixteenths(max(bf16_top(qf[0][1][0]), bf16_top(qf[0][1][1]))));   // 64 on
+      query8(qf[0][0], b0, 0, qs);
+      query8(qf[0][1], b1, 1, qs);
+      const uint32_t other = static_cast<uint32_t>(__shfl_xor(static_cast<int>(lq < 2 ? b1 : b0), 48, 64));
+      const uint32_t mine = lq == 0 ? b0 : (lq == 3 ? b1 : other);   // dims 32 lq .. + 31
+      qscale = mine | second_scale(mine) << 8;
+    }
+    f32x4 out[8];
 #pragma unroll
     for (int ct = 0; ct < 8; ++ct) out[ct] = f32x4{0.f, 0.f, 0.f, 0.f};
     uint8_t* const stage = s_val[wave];
@@ -328,10 +348,9 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
       for (int j = 0; j < 2; ++j) {
         const i32x8 ka = {static_cast<int>(s.k[j][0]), static_cast<int>(s.k[j][1]), static_cast<int>(s.k[j][2]), static_cast<int>(s.k[j][3]), 0, 0, 0, 0};
         const int kscale = static_cast<int>(s.ks[j] >> (8 * lq));
-        sc[j] = MOD ? f32x4{0.f, 0.f, 0.f, 0.f} : base;
-        sc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ka, qs.part[2], sc[j], 4, 2, 0, kscale, 2, qscale);
-        sc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ka, qs.part[1], sc[j], 4, 2, 0, kscale, 1, qscale);
-        sc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ka, qs.part[0], sc[j], 4, 2, 0, kscale, 0, qscale);
+        sc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        sc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ka, qs.part[1], sc[j], 4, 0, 0, kscale, 1, static_cast<int>(qscale));
+        sc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ka, qs.part[0], sc[j], 4, 0, 0, kscale, 0, static_cast<int>(qscale));
       }
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
@@ -355,6 +374,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
         for (int j = 0; j < 2; ++j)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
+            sc[j][r] *= p.q_scale;
             if (p.cap_log2 > 0.f)
               sc[j][r] = fmaf(-2.f * p.cap_log2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(sc[j][r]) + 1.f), p.cap_log2);
             if (p.slopes) sc[j][r] = fmaf(-slope, static_cast<float>(dist(key_of(j, r))), sc[j][r]);
@@ -388,22 +408,15 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
       }
       float bmax = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])),
                          fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
-      bmax = max_quarters(bmax);
-      const bool need = MOD ? bmax > m_run + kLazyLog2 : bmax > lift;
+      bmax = max_quarters(bmax) * to_log2;
+      const bool need = bmax > m_run + kLazyLog2;
       if (__any(need)) {
-        const float mn = !need ? m_run : (MOD || m_run == -INFINITY ? bmax : m_run + bmax);
+        const float mn = need ? bmax : m_run;
         const float alpha = !need ? 1.f : (m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - mn));
         l_run *= alpha;
 #pragma unroll
         for (int ct = 0; ct < 8; ++ct) out[ct] *= alpha;
         m_run = mn;
-        if constexpr (!MOD) {
-          const float by = need ? bmax : 0.f;
-          sc[0] -= by;
-          sc[1] -= by;
-          base -= by;
-          lift = need ? kLazyLog2 : lift;
-        }
       }
       const float mneg = m_run == -INFINITY ? 0.f : -m_run;
       u32x4 w;
@@ -412,7 +425,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
         float e[4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          e[r] = __builtin_amdgcn_exp2f(MOD ? sc[j][r] + mneg : sc[j][r]);
+          e[r] = __builtin_amdgcn_exp2f(MOD ? sc[j][r] + mneg : fmaf(sc[j][r], to_log2, mneg));
           l_run += e[r];
         }
         w[2 * j] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{e[0], e[1]}), bf16x2));
@@ -502,24 +515,25 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
     return;
   }
 
-  f32x16 ref;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) ref[r] = 0.f;
   f32x16 o[4];
 #pragma unroll
   for (int ct = 0; ct < 4; ++ct)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[ct][r] = 0.f;
-  Query6 qs[2];
-  uint32_t qsc = 0u, qsl = 0u;   // scale bytes of the first part for m = 0, 1, and the second's; the third's
+  Query8 qs[2];
+  uint32_t qsc = 0u;   // scale bytes of the first part for m = 0, 1, and the second's
   auto settle = [&]() __attribute__((always_inline)) {   // (behind the loads of the first blocks)
     keep_mask();
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
-      const uint32_t b = query6(qf[m], p.q_scale, qs[m]);
-      const bool odd = b == kFp4NaN;
-      qsc |= (b | (odd ? b : b - 3) << 16) << (8 * m);
-      qsl |= (odd ? b : b - 6) << (8 * m);
+      uint32_t b[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        b[k] = query_scale(top_halves(max(bf16_top(qf[m][k][0]), bf16_top(qf[m][k][1]))));
+        query8(qf[m][k], b[k], k, qs[m]);
+      }
+      const uint32_t mine = lh ? b[1] : b[0];
+      qsc |= (mine | second_scale(mine) << 16) << (8 * m);
     }
   };
 
@@ -534,25 +548,20 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
     const i32x8 ka = {static_cast<int>(k0[0]), static_cast<int>(k0[1]), static_cast<int>(k0[2]), static_cast<int>(k0[3]), 0, 0, 0, 0};
     const i32x8 kc = {static_cast<int>(k1[0]), static_cast<int>(k1[1]), static_cast<int>(k1[2]), static_cast<int>(k1[3]), 0, 0, 0, 0};
     const int kscale = static_cast<int>(lh ? ks >> 8 : ks), qscale = static_cast<int>(qsc);
-    if constexpr (MOD) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) sacc[r] = 0.f;
-    } else {
-      sacc = ref;
-    }
-    const int kl = static_cast<int>(qsl);
-    sacc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qs[0].part[2], sacc, 4, 2, 0, kscale, 0, kl);
-    sacc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kc, qs[1].part[2], sacc, 4, 2, 2, kscale, 1, kl);
-    sacc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qs[0].part[1], sacc, 4, 2, 0, kscale, 2, qscale);
-    sacc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kc, qs[1].part[1], sacc, 4, 2, 2, kscale, 3, qscale);
-    sacc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qs[0].part[0], sacc, 4, 2, 0, kscale, 0, qscale);
-    sacc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kc, qs[1].part[0], sacc, 4, 2, 2, kscale, 1, qscale);
+    for (int r = 0; r < 16; ++r) sacc[r] = 0.f;
+    sacc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qs[0].part[1], sacc, 4, 0, 0, kscale, 2, qscale);
+    sacc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kc, qs[1].part[1], sacc, 4, 0, 2, kscale, 3, qscale);
+    sacc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qs[0].part[0], sacc, 4, 0, 0, kscale, 0, qscale);
+    sacc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kc, qs[1].part[0], sacc, 4, 0, 2, kscale, 1, qscale);
   };
   auto key_of = [&](int r) { return 8 * (r >> 2) + 4 * lh + (r & 3); };   // accumulator r's key of the block
-  // MOD: the block's products (scaled by the query) as logits in base 2, key r at
+  // MOD: the block's products as logits in base 2, key r at
   // distance dist(r).  tanh(u) = 1 - 2 / (e^2u + 1) with 2 u / ln 2 from the
   // products: 0 and infinity of the exponential give -1 and 1.
   auto bend = [&](f32x16& sacc, auto dist) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sacc[r] *= p.q_scale;
     if (p.cap_log2 > 0.f) {
 #pragma unroll
       for (int r = 0; r < 16; ++r)
@@ -565,9 +574,8 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
   };
   // The softmax of the block at key kb (lazily raised maximum) and O^T += V^T P^T
   // from its staged values; odd: its keys whose values are no numbers; prefix: the
-  // caller knows that every row sees every key; ahead: the next block's scores,
-  // which move with the reference they started from.
-  auto attend = [&](int kb, const uint8_t* stage, uint32_t odd, f32x16& sacc, auto& ahead, auto prefix) __attribute__((always_inline)) {
+  // caller knows that every row sees every key.
+  auto attend = [&](int kb, const uint8_t* stage, uint32_t odd, f32x16& sacc, auto prefix) __attribute__((always_inline)) {
     uint32_t vis = ~0u;
     if (decltype(prefix)::value || (kb + KB <= L && !(MOD && kb < w_hi))) {   // (uniform)
       if constexpr (MOD) bend(sacc, [&](int r) { return qpos - (kb + key_of(r)); });
@@ -598,10 +606,10 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
     float bmax = -INFINITY;
 #pragma unroll
     for (int r = 0; r < 16; ++r) bmax = fmaxf(bmax, sacc[r]);
-    bmax = max_halves(bmax);
-    const bool need = MOD ? bmax > m_run + kLazyLog2 : bmax > lift;
+    bmax = max_halves(bmax) * to_log2;
+    const bool need = bmax > m_run + kLazyLog2;
     if (__any(need)) {
-      const float mn = !need ? m_run : (MOD || m_run == -INFINITY ? bmax : m_run + bmax);
+      const float mn = need ? bmax : m_run;
       const float alpha = !need ? 1.f : (m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - mn));
       l_run *= alpha;
 #pragma unroll
@@ -609,23 +617,13 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[ct][r] *= alpha;
       m_run = mn;
-      if constexpr (!MOD) {
-        const float by = need ? bmax : 0.f;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          sacc[r] -= by;
-          if constexpr (!std::is_null_pointer_v<std::remove_cv_t<std::remove_reference_t<decltype(ahead)>>>) ahead[r] -= by;
-          ref[r] -= by;
-        }
-        lift = need ? kLazyLog2 : lift;
-      }
     }
     const float mneg = m_run == -INFINITY ? 0.f : -m_run;
     float pr[16];
     float rsum = 0.f;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      pr[r] = __builtin_amdgcn_exp2f(MOD ? sacc[r] + mneg : sacc[r]);
+      pr[r] = __builtin_amdgcn_exp2f(MOD ? sacc[r] + mneg : fmaf(sacc[r], to_log2, mneg));
       rsum += pr[r];
     }
     l_run += rsum;
@@ -723,7 +721,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
         f32x16& ahead = k & 1 ? sa : sb;
         score(ring[(k + 1) % kFp4Ring], ahead);
         const uint32_t odd = __builtin_amdgcn_readfirstlane(s_odd[k]);
-        attend((blk_lo + i) * KB, s_val[k & 1], odd, cur, ahead, prefix);
+        attend((blk_lo + i) * KB, s_val[k & 1], odd, cur, prefix);
       }
       turn(ring[(k + 1) % kFp4Ring], s_val[(k + 1) & 1], k + 1);
     };
@@ -825,8 +823,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void paged_attn_fp4_kernel(PagedFp
         const uint32_t w = c < 4 ? s.v0[c & 3] : s.v1[c & 3];
         *reinterpret_cast<u32x4*>(srow + (((8 * lh + c) ^ sx) << 4)) = fp4_values(w, c < 4 ? sa : sb);
       }
-      std::nullptr_t none{};   // (no scores ahead)
-      attend(key_at(i), stage, odd, sacc, none, std::false_type{});
+      attend(key_at(i), stage, odd, sacc, std::false_type{});
     };
     for (int i = 0; i < nb; i += kFp4Ahead) {
 #pragma unroll

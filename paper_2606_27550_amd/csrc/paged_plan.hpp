@@ -75,8 +75,9 @@ struct PagedCall {
   // error against 64 bits is 3.4-3.5e-3 instead of 3.7-3.9e-3 (the weights' and the
   // query's roundings stay), and the bytes cost 3-6 % of long prefixes and windows,
   // 15 % of 26 nodes at 8192 (21.5 -> 24.7 us).  Of 4-bit pools in fp16, the
-  // row's largest scaled to [2^14, 2^15): 1.9e-3 instead of 2.9e-3 with bf16 (the
-  // output's own rounding being 1.7e-3 of it), at the same bytes.
+  // row's largest scaled to [2^14, 2^15): the output of split calls is then off by
+  // 2.2-2.3e-3 instead of 2.7-2.9e-3 with bf16 (1.7e-3 of it its own rounding, the
+  // rest the weights'), at the same bytes.
   void* part_o;
   float* part_ml;        // [part rows][2]: max, sum; of 4-bit pools [4]: what undoes the scaling, too
   uint16_t* out;         // [rows_cap][Hq][HD]
