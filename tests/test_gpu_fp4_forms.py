@@ -1,6 +1,6 @@
 """GPU: what each of the three forms of the attention over 4-bit pages (at most 16
 query rows of a KV head, at most 64, more) does with queries whose values differ
-much in size.
+much in size, with groups that are no numbers and with bytes that a window hides.
 
 Bounds.  A query's value of at least 2^-13 of the largest of its 32 enters the
 products as it is; a smaller one is off by at most 2^-21 of that largest.  The
@@ -24,7 +24,7 @@ from oracle import entmtp_oracle as orc  # noqa: E402
 from oracle import fp4_oracle as fo  # noqa: E402
 from tests.fp4_helpers import D, make, pool_bits  # noqa: E402
 from tests.paged_helpers import TREES, say, unbits  # noqa: E402
-from tests.test_gpu_fp4_attn import SCALE, launch  # noqa: E402
+from tests.test_gpu_fp4_attn import SCALE, launch, nan_row  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 FORMS = [(0, 8, 2), (1, 4, 2), (2, 4, 2), (1, 16, 2), (4, 8, 2)]   # 4, 14, 52, 56, 256 rows
@@ -127,3 +127,57 @@ def test_queries_of_extreme_size(api, t, Hq, Hkv, size):
     got = orc.bf16_to_f64(unbits(launch(api, c)["out"]))[:len(ref)]
     err = np.abs(got - ref)
     assert (err <= room).all(), float((err / room).max())
+
+
+@pytest.mark.parametrize("t,Hq,Hkv", [(1, 2, 2), (1, 4, 2), (2, 8, 4), (4, 8, 2), (4, 4, 2)])
+@pytest.mark.parametrize("pool", ["kp", "vp"])
+def test_groups_that_are_no_numbers_in_every_form(api, t, Hq, Hkv, pool):
+    """A bad group makes NaN of the rows that see its key, whole, and of no others, whichever half or block it lies in."""
+    L, T, group = 300, len(TREES[t]), Hq // Hkv
+    say("fp4 no numbers", t, Hq, Hkv, pool)
+    c = make(71 + t, [t], [L], Hq, Hkv, 16)
+    ref = orc.bf16_to_f64(unbits(launch(api, c)["out"]))
+    clean = c[pool].copy()
+    # (at 300: the block of 32 keys from 288 on holds prefix and tree; a node in its second half, others in later blocks)
+    nodes = sorted({0, 1, T // 2, T - 1} | {n for n in (4, 20, 36) if n < T})
+    for k, node in enumerate(nodes):
+        c[pool] = clean.copy()
+        nan_row(c, pool, 0, L + node, k % Hkv, group=k % 4)
+        got = orc.bf16_to_f64(unbits(launch(api, c)["out"]))
+        want = np.zeros((T, Hq), bool)
+        heirs = [i for i in range(T) if node in orc.ancestors_or_self(TREES[t], i)]
+        want[heirs, (k % Hkv) * group:(k % Hkv + 1) * group] = True
+        np.testing.assert_array_equal(np.isnan(got).any(2), want)
+        assert np.isnan(got[want]).all()
+        np.testing.assert_array_equal(got[~want], ref[~want])
+    # several at once, in one block and in neighbouring ones, beside a prefix key of another head
+    c[pool] = clean.copy()
+    want = np.zeros((T, Hq), bool)
+    for k, node in enumerate(nodes):
+        nan_row(c, pool, 0, L + node, 0, group=k % 4)
+        want[[i for i in range(T) if node in orc.ancestors_or_self(TREES[t], i)], :group] = True
+    for pos in (0, 17, 31, 32, 150):
+        nan_row(c, pool, 0, pos, 1, group=3)
+    want[:, group:2 * group] = True
+    got = orc.bf16_to_f64(unbits(launch(api, c)["out"]))
+    np.testing.assert_array_equal(np.isnan(got).any(2), want)
+    assert np.isnan(got[want]).all()
+    np.testing.assert_array_equal(got[~want], ref[~want])
+
+
+@pytest.mark.parametrize("t,Hq,Hkv,L,window", [(0, 8, 2, 301, 20), (0, 4, 4, 1000, 64), (1, 4, 2, 700, 33), (1, 2, 1, 90, 1)])
+@pytest.mark.parametrize("pool", ["kp", "vp"])
+def test_bytes_before_a_window_of_few_rows(api, t, Hq, Hkv, L, window, pool):
+    """Slots before every row's window hold any bytes, in the window's own blocks too; the outputs are the same bits."""
+    say("fp4 window bytes", t, Hq, Hkv, L, window, pool)
+    c, g = make(81 + L, [t], [L], Hq, Hkv, 16), np.random.default_rng(L)
+    want = unbits(launch(api, c, window=window)["out"])
+    codes, scales = (x.copy() for x in fo.planes(c[pool]))
+    for pos in range(L - window + 1):
+        at = (c["table"][0, pos // 16], slice(None), pos % 16)
+        codes[at] = g.integers(0, 256, codes[at].shape)
+        scales[at] = g.choice([0, 1, 127, 252, 253, 254, 255], scales[at].shape)
+    c[pool] = fo.join(codes, scales)
+    got = unbits(launch(api, c, window=window)["out"])
+    assert np.isfinite(orc.bf16_to_f64(want)).all()
+    np.testing.assert_array_equal(got, want)
