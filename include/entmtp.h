@@ -288,10 +288,11 @@ int32_t entmtp_verify_logits(const entmtp_bf16* hidden, const entmtp_bf16* w_lm,
  * entmtp_quantize_fp4, which makes them): codes [V][hid / 2] and scales
  * [V][hid / 32] bytes, those of entmtp_quantize_fp4 (others up to 254 too, as long
  * as the values are bf16 numbers; below its smallest normal one they may count as
- * zero).  The weights enter the products as the numbers they stand for, sums are fp32.  A weight row with a scale
- * byte 255 has NaN logits.
+ * zero).  The weights enter the products as the numbers they stand for, sums are
+ * fp32.  A weight row with a scale byte 255 has NaN logits.
  * Requirements: 1 <= T <= 4096, 32 <= hid <= 65536, hid % 32 == 0, V >= 1, hidden,
- * codes and logits 16-byte aligned.
+ * codes and logits 16-byte aligned.  Fastest where hid is a multiple of 128 and
+ * scales 4-byte aligned.
  * Errors (host-checked): EINVAL, EHIP.
  */
 int32_t entmtp_verify_logits_fp4(const entmtp_bf16* hidden, const uint8_t* codes,

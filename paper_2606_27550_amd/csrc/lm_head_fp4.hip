@@ -21,6 +21,7 @@
 #include <algorithm>
 
 #include "fp4.hpp"
+#include "paged.hpp"
 #include "stream_pipe.hpp"
 
 namespace entmtp {
@@ -210,12 +211,6 @@ __device__ __forceinline__ int lm_swz(int r) {
   return KS % 4 == 0 ? r & 15 : (KS % 2 == 0 ? r >> 1 & 7 : r >> 2 & 3);
 }
 
-// Four bytes a lane to the LDS, as buf_dma16.
-__device__ __forceinline__ void buf_dma4(__amdgpu_buffer_rsrc_t buf, uint32_t voff, void* lds) {
-  typedef __attribute__((address_space(3))) void lds_void;
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lds_void*)lds, 4, voff, 0, 0, 0);
-}
-
 // A wavefront's part of a tile: codes, and a dword of scale bytes a row and step.
 template <int KS>
 struct LmPart {
@@ -391,8 +386,6 @@ extern "C" int32_t entmtp_verify_logits_fp4(const entmtp_bf16* hidden, const uin
   ENTMTP_CHECK_ARG(V >= 1 && V <= INT32_MAX - 4096, ENTMTP_EINVAL, "V = %d out of range", V);
   ENTMTP_CHECK_ARG(aligned16(hidden) && aligned16(codes) && aligned16(logits), ENTMTP_EINVAL,
                    "hidden, codes and logits must be 16-byte aligned");
-  int cus = 256, dev = 0;
-  if (hipGetDevice(&dev) == hipSuccess) (void)hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
   LmFp4Args a{};
   a.x = hidden;
   a.codes = codes;
@@ -406,30 +399,31 @@ extern "C" int32_t entmtp_verify_logits_fp4(const entmtp_bf16* hidden, const uin
   const int steps = (hid + kLmStep - 1) / kLmStep;
   // a pass over hid holds at most 8 steps a wavefront (5 where it has two tiles of X,
   // 2 where it has four, which halves the copies of W: of 128256 logits 128 rows of
-  // 1024 values 78 -> 61 us, 100 of 1536 94 -> 78; of 32000 33 of 2048 18.1 -> 16.7)
+  // 1024 values 78 -> 61 us, 100 of 1536 94 -> 78; of 32000 33 of 2048 18.1 -> 16.7;
+  // 64 rows of 50257 of 2048 lose by it, 30.9 -> 32.0)
   const bool lines = hid % kLmStep == 0 && (reinterpret_cast<uintptr_t>(scales) & 3u) == 0;   // (a step's scale bytes are a dword)
   const int nt = T > 32 && lines && steps <= 2 * kLmWaves ? 4 : (T > 16 ? 2 : 1), most = nt == 4 ? 2 : (nt == 2 ? 5 : 8);
   const int passes = (steps + most * kLmWaves - 1) / (most * kLmWaves);
   const int ks = ((steps + passes - 1) / passes + kLmWaves - 1) / kLmWaves;
   a.chunks = (T + 16 * nt - 1) / (16 * nt);
-  a.slices = std::min(std::max(1, cus / a.chunks / 8) * 8, a.tiles);
+  a.slices = std::min(std::max(1, device_cus() / a.chunks / 8) * 8, a.tiles);
   const dim3 grid(static_cast<uint32_t>((a.slices + 7) / 8 * 8 * a.chunks));
   for (int pass = 0; pass < passes; ++pass) {
     a.k0 = pass * ks * kLmWaves;
     a.add = pass > 0;
     const bool all = a.k0 + ks * kLmWaves <= steps;
-    auto go = [&](auto stream_all, auto stream, auto rest) {
-      hipLaunchKernelGGL(lines ? (all ? stream_all : stream) : rest, grid, dim3(kLmThreads), 0, s, a);
-    };
-#define LM_FP4(KS, NT) \
-  go(lm_fp4_stream_kernel<KS, NT, true>, lm_fp4_stream_kernel<KS, NT, false>, lm_fp4_kernel<KS, NT, 2>)
-#define LM_FP4_LINES(KS) \
-  go(lm_fp4_stream_kernel<KS, 4, true>, lm_fp4_stream_kernel<KS, 4, false>, lm_fp4_stream_kernel<KS, 4, false>)
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kLmThreads), 0, s, a); };
+#define LM_FP4_LINES(KS, NT) go(all ? lm_fp4_stream_kernel<KS, NT, true> : lm_fp4_stream_kernel<KS, NT, false>)
+#define LM_FP4(KS, NT)             \
+  if (lines)                       \
+    LM_FP4_LINES(KS, NT);          \
+  else                             \
+    go(lm_fp4_kernel<KS, NT, 2>)
     if (nt == 4) {
       if (ks == 1)
-        LM_FP4_LINES(1);
+        LM_FP4_LINES(1, 4);
       else
-        LM_FP4_LINES(2);
+        LM_FP4_LINES(2, 4);
     } else if (nt == 1) {
       switch (ks) {
         case 1: LM_FP4(1, 1); break;

@@ -100,12 +100,6 @@ __device__ __forceinline__ uint32_t buf_load4(__amdgpu_buffer_rsrc_t buf, uint32
   return __builtin_bit_cast(uint32_t, buf_load(buf, voff));
 }
 
-// Four bytes a lane to the LDS, as buf_dma16.
-__device__ __forceinline__ void buf_dma4(__amdgpu_buffer_rsrc_t buf, uint32_t voff, void* lds) {
-  typedef __attribute__((address_space(3))) void lds_void;
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lds_void*)lds, 4, voff, 0, 0, 0);
-}
-
 // The larger of a lane's number and that of the lane 32 (16) away.
 __device__ __forceinline__ uint32_t top_halves(uint32_t x) {
   const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);

@@ -54,6 +54,12 @@ __device__ __forceinline__ void buf_dma16(__amdgpu_buffer_rsrc_t buf, uint32_t v
   buf_dma16_at(buf, voff, 0, lds);
 }
 
+// The same with four bytes a lane, lane l's at lds + 4 * l.
+__device__ __forceinline__ void buf_dma4(__amdgpu_buffer_rsrc_t buf, uint32_t voff, void* lds) {
+  typedef __attribute__((address_space(3))) void lds_void;
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lds_void*)lds, 4, voff, 0, 0, 0);
+}
+
 // Four bytes at byte voff of the buffer (zero past its end).  The range check
 // is relied on for the per-lane offset alone: the scalar offset, which it need
 // not cover, stays zero.
