@@ -13,11 +13,13 @@
 // Up to 32 rows the weights' bytes bound it: one row of 32000 logits of 4096 values
 // takes 14 us (5 TB/s), 8 of 128256 50.5 (5.6), 27 of 128256 60 (4.9), where the bf16
 // LM head reads 3.8 times the bytes.  Beyond, the weights come once more for every
-// 32 rows (64 of up to 2048 values), from the L2 but at about the same 6 TB/s a chip can take: 128 rows of 32000
-// (5120 values) 57 us where the products at bf16's rate would take 31, 64 of 128256 85,
-// 256 of 32000 77.  A tile kernel for many rows (64 x 128 and 128 x 128 logits a
-// workgroup, W and X through the LDS) came to 50-55 us for the first and 100-113
-// for the second: its copies of W are 64 bytes a row and a dword of scales.
+// 32 rows (64 of up to 2048 values), from the L2 but at about the same 6 TB/s a chip
+// can take, and are turned into bf16 once more: 128 rows of 32000 (5120 values) 57 us
+// where the products at bf16's rate would take 31, 64 of 128256 87, 256 of 32000 79.
+// A tile kernel for many rows (64 x 128 and 128 x 128 logits a workgroup, W and X
+// through the LDS) came to 50-55 us for the first and 100-113 for the second: its
+// copies of W are 64 bytes a row and a dword of scales.  (Hidden sizes that are no
+// multiple of 128 and scales at odd addresses take lm_fp4_kernel, 10-30 % slower.)
 #include <algorithm>
 
 #include "fp4.hpp"
